@@ -34,8 +34,9 @@ extern "C" {
 enum { MOE_OK = 0, MOE_INVALID_ARG = 1, MOE_UNSUPPORTED = 2, MOE_WORKSPACE_TOO_SMALL = 3, MOE_HIP_ERROR = 4,
        MOE_SCRATCH_TOO_SMALL = 5 };
 enum { MOE_F32 = 0, MOE_BF16 = 1 };
-enum { MOE_ACT_RELU = 0, MOE_ACT_GELU = 1, MOE_ACT_SILU = 2 };
+enum { MOE_ACT_NONE = -1, MOE_ACT_RELU = 0, MOE_ACT_GELU = 1, MOE_ACT_SILU = 2 };   /* NONE: moe_matmul8 only */
 enum { MOE_ROUTER_LINEAR = 0, MOE_ROUTER_COSINE = 1 };
+enum { MOE_SCALE_ROWS = 0, MOE_SCALE_BLOCKS = 1 };
 
 /* Number of events moe_layer_forward records when `stage_events` is given:
  * [0] start, [1] after gate logits, [2] after top-k + slot assignment, [3] after encode,
@@ -330,6 +331,86 @@ int moe_layer_backward(const void* x, const void* Wg, const void* W1, const void
                        int64_t H, int64_t E, int k, double f, int normalize, int act, int dtype, const void* d_out, void* state,
                        size_t state_bytes, void* dx, void* dWg, float* dgate_bias, void* dW1, void* db1, void* dW2, void* db2,
                        void* stream);
+
+/* RMS norm with the residual's addition, in the storage type (for the gate) and in 8 bits (for the experts):
+ *   h = x + residual;   y = h / sqrt(mean(h^2) + eps) * weight     per row of M values.
+ *   x, residual, h, y [T,M] and weight [M] in `dtype`; residual NULL: h = x; weight NULL: ones.  h (required with a residual), y and q may be NULL,
+ *   but not both of y and q.  q / q_scales: y in the 8-bit format (moe_quantize8, MOE_SCALE_ROWS).
+ * Statistics and y are computed in fp32 from the fp32 sum, before h is rounded; y and q are each rounded once from it.  The sum of the squares of a
+ * row has to be finite in fp32.  eps > 0 (in fp32); M <= 16384 and T < 2^22, else MOE_UNSUPPORTED.  h may be x or residual. */
+int moe_rms_norm(const void* x, const void* residual, const void* weight, double eps, int dtype, int64_t T, int64_t M, void* h, void* y,
+                 void* q, uint8_t* q_scales, void* stream);
+
+/* Its gradient, from dy = dLoss/dy and dh, the gradient that reaches h past the norm (the residual stream's; NULL: none):
+ *   g = dy * weight;   dx = r * (g - h * r^2 * mean(g * h)) + dh;   dweight = sum over the rows of dy * h * r;   r = 1 / sqrt(mean(h^2) + eps).
+ *   dy, dh, h (as moe_rms_norm stored it), dx [T,M], weight and dweight [M] in `dtype`; dx is the gradient of x and of residual both.
+ * fp32 sums, in an order that the sizes fix.  dweight may be NULL, then ws too; ws: moe_rms_norm_backward_workspace_bytes (0 on invalid arguments),
+ * 256-byte aligned.  dx may be dy or dh.  Limits as moe_rms_norm. */
+size_t moe_rms_norm_backward_workspace_bytes(int64_t T, int64_t M);
+int moe_rms_norm_backward(const void* dy, const void* dh, const void* h, const void* weight, double eps, int dtype, int64_t T, int64_t M,
+                          void* ws, size_t ws_bytes, void* dx, void* dweight, void* stream);
+
+/* The 8-bit format: e4m3 values (OCP: largest 448, no infinities) in blocks of 128 along the axis that a product sums over, each block with one power of two
+ * 2^e, kept as the byte e + 127: the smallest with max |v| <= 448 * 2^e, and at least 2^-126.  A block with an infinity or NaN has the byte 255 and only NaNs.
+ * A matrix of R rows and K columns is values [R, moe_row_bytes8(K)] (K rounded up to whole blocks, zeros past the end) and exponents:
+ *   MOE_SCALE_ROWS    [R, moe_row_scales8(K)], one for 128 values of a row (tokens, gradients);
+ *   MOE_SCALE_BLOCKS  [ceil(R / 128), moe_row_scales8(K)], one for 128 x 128 values (weights: the same values serve both orientations);
+ *   moe_row_scales8(K) is the number of blocks rounded up to a multiple of four, 127 past the end.
+ * Both helpers return -1 where K is not in 1 .. 2^30. */
+int64_t moe_row_bytes8(int64_t K);
+int64_t moe_row_scales8(int64_t K);
+
+/* E matrices src [E,R,K] in `dtype` to that format: as they are (q, scales), transposed (qt [E,K,moe_row_bytes8(R)], scales_t, blocks along R), or both from
+ * one read; either pair may be NULL.  Round to nearest even.
+ *   counts [E] int32 or NULL: only the first min(counts[e], R) rows of a matrix exist.  q and scales of other rows are left untouched; qt has zeros for
+ *   them up to the end of the block of 128 that the last one is in and is left untouched beyond it (moe_matmul8's k_counts stops there).
+ * E <= 65535, fewer than 2^24 tiles of 128 x 128 to a matrix. */
+int moe_quantize8(const void* src, int dtype, const int32_t* counts, int64_t E, int64_t R, int64_t K, int scale_mode, void* q, uint8_t* scales,
+                  void* qt, uint8_t* scales_t, void* stream);
+
+/* Back: out [E,R,K] in `dtype`.  bf16 holds every value of the format. */
+int moe_dequantize8(const void* q, const uint8_t* scales, int scale_mode, int64_t E, int64_t R, int64_t K, int dtype, void* out, void* stream);
+
+/* Products of 8-bit matrices on the matrix cores, which apply the blocks' exponents themselves, with fp32 sums:
+ *   out[e][r, n] = act(sum_k A[e][r, k] * B[e][n, k] + bias[e][n])        (both operands have the summed axis contiguous)
+ *   A [E,C,K] with MOE_SCALE_ROWS; B [E,N,K] with B_scale_mode; bias [E,N] in `dtype` or NULL; act: MOE_ACT_*, or MOE_ACT_NONE.
+ *   Exactly one of out [E,C,N] in `dtype`, rounded once, and out8 / out8_scales (the 8-bit format with MOE_SCALE_ROWS, rounded once) is given.
+ *   counts [E] int32 or NULL: only the first min(counts[e], C) rows of each expert are computed, the others are left untouched.
+ *   k_counts [E] int32 or NULL: only the blocks of 128 that hold the first min(k_counts[e], K) k are summed; what they hold past those k has to be zero.
+ *   gather [E,C] int32 or NULL: row c of expert e is row gather[e,c] of one matrix A [gather_rows, K]; rows out of range stand for row 0.
+ * An orientation each for y = x W (B = W transposed), dx = dy W^T (B = W as it is) and dW = x^T dy (both transposed, k_counts = the fills).
+ * N a multiple of 8, K anything; N * moe_row_bytes8(K) < 2^32; the exponents 4-byte aligned. */
+int moe_matmul8(const void* A, const uint8_t* A_scales, const void* B, const uint8_t* B_scales, int B_scale_mode, const void* bias, int act,
+                int dtype, const int32_t* counts, const int32_t* k_counts, const int32_t* gather, int64_t gather_rows, int64_t E, int64_t C,
+                int64_t K, int64_t N, void* out, void* out8, uint8_t* out8_scales, void* stream);
+
+/* moe_expert_ffn (or, with slot_src, moe_expert_ffn_gather) on 8-bit tokens and weights:
+ *   Y[e] = act(Z[e] W1[e] + b1[e]) W2[e] + b2[e], the activations rounded once, to the 8-bit format (hidden8, hidden_scales: scratch).
+ *   x8 / x_scales: Z [E,C,M], or with slot_src [E,C] the tokens [T,M]; W1 as [E,H,M], W2 as [E,M,H] (moe_quantize8's transposed form of [E,M,H] and
+ *   [E,H,M]) with MOE_SCALE_BLOCKS; b1 [E,H], b2 [E,M], Y [E,C,M] in `dtype`.  counts, unfilled rows and act as moe_expert_ffn_gather. */
+int moe_expert_ffn8(const void* x8, const uint8_t* x_scales, const int32_t* slot_src, int64_t T, const void* W1, const uint8_t* s1, const void* b1,
+                    const void* W2, const uint8_t* s2, const void* b2, int act, int dtype, const int32_t* counts, int64_t E, int64_t C, int64_t M,
+                    int64_t H, void* hidden8, uint8_t* hidden_scales, void* Y, void* stream);
+
+/* moe_layer_forward with 8-bit experts: the gate reads x [T,M] in `dtype`, the experts the same tokens in 8 bits (x8, x_scales: moe_rms_norm gives both).
+ * Weights as moe_expert_ffn8, everything else as moe_layer_forward.  ws: moe_layer8_workspace_bytes with C = moe_capacity(T,E,k,f), 256-byte
+ * aligned. */
+size_t moe_layer8_workspace_bytes(int64_t T, int64_t M, int64_t H, int64_t E, int k, int64_t C, int dtype);
+int moe_layer_forward8(const void* x, const void* x8, const uint8_t* x_scales, const void* Wg, const float* gate_bias, const void* W1,
+                       const uint8_t* s1, const void* b1, const void* W2, const uint8_t* s2, const void* b2, int64_t T, int64_t M, int64_t H,
+                       int64_t E, int k, double f, int normalize, int act, int dtype, void* out, int32_t* idx, int32_t* loc, float* gate_w,
+                       int32_t* counts, float* logits, void* ws, size_t ws_bytes, void* stream);
+
+/* moe_layer_forward for at most MOE_FEW_MAX_TOKENS tokens (decode steps of a serving batch), where reading the chosen experts' weights is all the time
+ * there is.  Routing is the same, bit for bit; out sums a token's choices in fp32 without a rounding in between.
+ *   s1 = s2 = NULL: W1 [E,M,H], W2 [E,H,M] in `dtype`.  Else 8-bit weights as moe_expert_ffn8 takes them, the tokens and activations staying in `dtype`.
+ *   ws: moe_layer_few_workspace_bytes, 256-byte aligned.  Everything else as moe_layer_forward. */
+#define MOE_FEW_MAX_TOKENS 64
+size_t moe_layer_few_workspace_bytes(int64_t T, int64_t M, int64_t H, int64_t E, int k, int dtype);
+int moe_layer_forward_few(const void* x, const void* Wg, const float* gate_bias, const void* W1, const uint8_t* s1, const void* b1, const void* W2,
+                          const uint8_t* s2, const void* b2, int64_t T, int64_t M, int64_t H, int64_t E, int k, double f, int normalize, int act,
+                          int dtype, void* out, int32_t* idx, int32_t* loc, float* gate_w, int32_t* counts, float* logits, void* ws,
+                          size_t ws_bytes, void* stream);
 
 /* Thin wrappers over HIP events so that a caller without HIP headers can time on the library's stream.
  * moe_event_create stores a new hipEvent_t in *event; moe_event_elapsed_ms needs both events completed. */

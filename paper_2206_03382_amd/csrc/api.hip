@@ -2,33 +2,15 @@
 #include <cmath>
 #include <mutex>
 
-#include "common.h"
+#include "api_checks.h"
 #include "gate_rules.h"
 
 namespace moe {
 namespace {
 
-inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-inline bool dtype_ok(int d) { return d == MOE_F32 || d == MOE_BF16; }
-inline bool act_ok(int a) { return a == MOE_ACT_RELU || a == MOE_ACT_GELU || a == MOE_ACT_SILU; }
-inline size_t esize(int d) { return d == MOE_F32 ? 4 : 2; }
-constexpr int64_t kMaxDim = (int64_t)1 << 30;
-
-inline int gate_shape_status(int64_t T, int64_t E, int k) {
-  if (T < 1 || E < 1 || k < 1 || k > E || T > kMaxDim) return MOE_INVALID_ARG;
-  if (E > 512 || (int64_t)k * E > 16384) return MOE_UNSUPPORTED;
-  return MOE_OK;
-}
-
 // rows an expert holds on average: every choice is one row, so the experts hold no more than E times this in all, wherever the
 // choices go
 inline int64_t mean_fill(int64_t T, int64_t E, int k) { return ceil_div(T * k, E); }
-
-inline int row_shape_status(int64_t M) {
-  if (M < 1 || M > kMaxDim) return MOE_INVALID_ARG;
-  if (M % 8 != 0) return MOE_UNSUPPORTED;
-  return MOE_OK;
-}
 
 // The gating function from the tokens: logits, then decisions and slots.  bf16 gates take the fast logits kernel and
 // the top-k kernel's exact repair of near-ties; everything else the fp64 logits kernel.  Workspace: the arrival

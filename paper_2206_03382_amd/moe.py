@@ -8,14 +8,16 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Tuple, Dict, Optional, Sequence
+from typing import Tuple, Dict, NamedTuple, Optional, Sequence
 
 import torch
 
 OK, INVALID_ARG, UNSUPPORTED, WORKSPACE_TOO_SMALL, HIP_ERROR, SCRATCH_TOO_SMALL = range(6)
 F32, BF16 = 0, 1
-ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = -1, 0, 1, 2
 ROUTER_LINEAR, ROUTER_COSINE = 0, 1
+SCALE_ROWS, SCALE_BLOCKS = 0, 1
+FEW_MAX_TOKENS = 64
 NUM_STAGE_EVENTS = 7
 STAGE_NAMES = ("gate_logits", "gate_topk", "encode", "ffn_gemm1", "ffn_gemm2", "decode")
 
@@ -66,6 +68,19 @@ SIGNATURES = {
                                        _vp, _vp, _sz, _vp]),
     "moe_layer_backward": (_i32, [_vp, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _i64, _i32, _dbl, _i32, _i32, _i32, _vp, _vp, _sz,
                                   _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "moe_rms_norm": (_i32, [_vp, _vp, _vp, _dbl, _i32, _i64, _i64, _vp, _vp, _vp, _vp, _vp]),
+    "moe_rms_norm_backward_workspace_bytes": (_sz, [_i64, _i64]),
+    "moe_rms_norm_backward": (_i32, [_vp, _vp, _vp, _vp, _dbl, _i32, _i64, _i64, _vp, _sz, _vp, _vp, _vp]),
+    "moe_row_bytes8": (_i64, [_i64]),
+    "moe_row_scales8": (_i64, [_i64]),
+    "moe_quantize8": (_i32, [_vp, _i32, _vp, _i64, _i64, _i64, _i32, _vp, _vp, _vp, _vp, _vp]),
+    "moe_dequantize8": (_i32, [_vp, _vp, _i32, _i64, _i64, _i64, _i32, _vp, _vp]),
+    "moe_matmul8": (_i32, [_vp, _vp, _vp, _vp, _i32, _vp, _i32, _i32, _vp, _vp, _vp, _i64, _i64, _i64, _i64, _i64, _vp, _vp, _vp, _vp]),
+    "moe_expert_ffn8": (_i32, [_vp, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _vp, _i64, _i64, _i64, _i64, _vp, _vp, _vp, _vp]),
+    "moe_layer8_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64, _i32, _i64, _i32]),
+    "moe_layer_forward8": (_i32, [_vp] * 11 + [_i64, _i64, _i64, _i64, _i32, _dbl, _i32, _i32, _i32] + [_vp] * 7 + [_sz, _vp]),
+    "moe_layer_few_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64, _i32, _i32]),
+    "moe_layer_forward_few": (_i32, [_vp] * 9 + [_i64, _i64, _i64, _i64, _i32, _dbl, _i32, _i32, _i32] + [_vp] * 7 + [_sz, _vp]),
     "moe_event_create": (_i32, [_c.POINTER(_vp)]),
     "moe_event_destroy": (_i32, [_vp]),
     "moe_event_record": (_i32, [_vp, _vp]),
@@ -506,3 +521,255 @@ class MoELayer:
                      _p(self.out), _p(r.get("idx")), _p(r.get("loc")), _p(r.get("gate_w")), _p(r.get("counts")),
                      _p(r.get("logits")), _p(self.ws), self.ws.numel(), _stream(), ev), "moe_layer_forward")
         return self.out
+
+
+class Block8(NamedTuple):
+    """Matrices in the 8-bit block format: q [.., R, row_bytes8(K)] float8_e4m3fn, exponents s [.., R or ceil(R / 128), row_scales8(K)]
+    uint8, K = width; blocks: one exponent for 128 x 128 values (weights) instead of 128 of a row."""
+    q: torch.Tensor
+    s: torch.Tensor
+    width: int
+    blocks: bool
+
+
+def _alloc8(lead: Tuple[int, ...], R: int, K: int, blocks: bool, device) -> Block8:
+    row, sc = -(-K // 128) * 128, -(-K // 512) * 4             # moe_row_bytes8, moe_row_scales8
+    q = torch.empty((*lead, R, row), dtype=torch.float8_e4m3fn, device=device)
+    return Block8(q, torch.empty((*lead, -(-R // 128) if blocks else R, sc), dtype=torch.uint8, device=device), K, blocks)
+
+
+def _check8(m: Block8, what: str) -> None:
+    R, row = m.q.shape[-2:]
+    scales = (*m.q.shape[:-2], -(-R // 128) if m.blocks else R, -(-m.width // 512) * 4)
+    if m.q.dtype != torch.float8_e4m3fn or m.s.dtype != torch.uint8 or row != -(-m.width // 128) * 128 or tuple(m.s.shape) != scales:
+        raise ValueError(f"{what}: not a matrix in the 8-bit block format")
+
+
+def _check_storage(code: int, *tensors: Optional[torch.Tensor]) -> None:
+    for t in tensors:
+        if t is not None and _dtype_code(t) != code:
+            raise ValueError("tensors must share the storage dtype")
+
+
+def _check_int32(t: Optional[torch.Tensor], *shape: int) -> None:
+    if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != shape):
+        raise ValueError(f"counts and indices must be int32 {list(shape)}")
+
+
+def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float, residual: Optional[torch.Tensor] = None, want_y: bool = True,
+             want_8: bool = False, out: Optional[Dict] = None) -> Dict:
+    """h = x + residual (x itself without one), y = RMS norm of h times weight, y8 = the same in 8 bits; `out`: an earlier result of the same
+    shapes to write into."""
+    T, M = x.shape
+    code = _dtype_code(x)
+    if (residual is not None and residual.shape != x.shape) or (weight is not None and weight.numel() != M):
+        raise ValueError("residual must have x's shape and weight its width")
+    _check_storage(code, residual, weight)
+    if out is None:
+        out = dict(h=torch.empty_like(x) if residual is not None else x, y=torch.empty_like(x) if want_y else None,
+                   y8=_alloc8((), T, M, False, x.device) if want_8 else None)
+    h, y, y8 = out["h"], out["y"], out["y8"]
+    _check(lib().moe_rms_norm(_p(x), _p(residual), _p(weight), eps, code, T, M, _p(h) if residual is not None else None, _p(y),
+                              _p(y8.q) if y8 is not None else None, _p(y8.s) if y8 is not None else None, _stream()), "moe_rms_norm")
+    return out
+
+
+def rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: Optional[torch.Tensor], eps: float, dh: Optional[torch.Tensor] = None,
+                      out: Optional[Dict] = None) -> Dict:
+    """dx (of x and of the residual) and dweight; dh: the gradient that reaches h past the norm."""
+    T, M = h.shape
+    code = _dtype_code(h)
+    if dy.shape != h.shape or (dh is not None and dh.shape != h.shape) or (weight is not None and weight.numel() != M):
+        raise ValueError("dy and dh must have h's shape and weight its width")
+    _check_storage(code, dy, dh, weight)
+    nbytes = int(lib().moe_rms_norm_backward_workspace_bytes(T, M))
+    if nbytes == 0:
+        raise MoEError(UNSUPPORTED, "moe_rms_norm_backward_workspace_bytes")
+    ws = torch.empty((nbytes,), dtype=torch.uint8, device=h.device)
+    if out is None:
+        out = dict(dx=torch.empty_like(h), dweight=torch.empty((M,), dtype=h.dtype, device=h.device))
+    _check(lib().moe_rms_norm_backward(_p(dy), _p(dh), _p(h), _p(weight), eps, code, T, M, _p(ws), nbytes, _p(out["dx"]),
+                                       _p(out["dweight"]), _stream()), "moe_rms_norm_backward")
+    return out
+
+
+def quantize8(src: torch.Tensor, blocks: bool = False, rows: bool = True, transposed: bool = False,
+              counts: Optional[torch.Tensor] = None) -> Tuple[Optional[Block8], Optional[Block8]]:
+    """(src [E,R,K] or [R,K] in 8 bits, its transpose in 8 bits): what is asked for, from one read."""
+    lead, (R, K) = tuple(src.shape[:-2]), src.shape[-2:]
+    E = lead[0] if lead else 1
+    _check_int32(counts, E)
+    q = _alloc8(lead, R, K, blocks, src.device) if rows else None
+    qt = _alloc8(lead, K, R, blocks, src.device) if transposed else None
+    _check(lib().moe_quantize8(_p(src), _dtype_code(src), _p(counts), E, R, K, SCALE_BLOCKS if blocks else SCALE_ROWS,
+                               _p(q.q) if rows else None, _p(q.s) if rows else None, _p(qt.q) if transposed else None,
+                               _p(qt.s) if transposed else None, _stream()), "moe_quantize8")
+    return q, qt
+
+
+def dequantize8(m: Block8, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    _check8(m, "m")
+    lead, R = tuple(m.q.shape[:-2]), m.q.shape[-2]
+    out = torch.empty((*lead, R, m.width), dtype=dtype, device=m.q.device)
+    _check(lib().moe_dequantize8(_p(m.q), _p(m.s), SCALE_BLOCKS if m.blocks else SCALE_ROWS, lead[0] if lead else 1, R, m.width,
+                                 _dtype_code(out), _p(out), _stream()), "moe_dequantize8")
+    return out
+
+
+def matmul8(A: Block8, B: Block8, bias: Optional[torch.Tensor] = None, act: int = ACT_NONE, dtype: torch.dtype = torch.bfloat16,
+            counts: Optional[torch.Tensor] = None, k_counts: Optional[torch.Tensor] = None, gather: Optional[torch.Tensor] = None,
+            out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """out[e] = act(A[e] B[e]^T + bias[e]): A [E,C,K] (rows gathered from [rows,K] with gather [E,C]), B [E,N,K].  Rows past an expert's count are
+    zero, or what `out` holds."""
+    _check8(A, "A")
+    _check8(B, "B")
+    E, N = B.q.shape[:2]
+    C = gather.shape[1] if gather is not None else A.q.shape[1]
+    if A.blocks or A.width != B.width or (gather is None and A.q.shape[0] != E) or (gather is not None and (A.q.dim() != 2 or gather.shape[0] != E)):
+        raise ValueError("A must have one exponent per row and block, and A, B and gather must agree in shape")
+    _check_int32(counts, E)
+    _check_int32(k_counts, E)
+    _check_int32(gather, E, C)
+    if out is None:
+        out = (torch.empty if counts is None else torch.zeros)((E, C, N), dtype=dtype, device=B.q.device)
+    _check_storage(_dtype_code(out), bias)
+    _check(lib().moe_matmul8(_p(A.q), _p(A.s), _p(B.q), _p(B.s), SCALE_BLOCKS if B.blocks else SCALE_ROWS, _p(bias), act, _dtype_code(out),
+                             _p(counts), _p(k_counts), _p(gather), A.q.shape[0] if gather is not None else 0, E, C, A.width, N, _p(out),
+                             None, None, _stream()), "moe_matmul8")
+    return out
+
+
+def expert_linear8_train(x: torch.Tensor, W: torch.Tensor, counts: Optional[torch.Tensor] = None):
+    """One projection of the experts in 8 bits for a training step: y[e] = x[e] W[e] (x [E,C,K], W [E,K,N]), and what the backward needs of
+    them.  Every operand is quantised along the axis that its product sums over; W's blocks serve both directions."""
+    x8, xt8 = quantize8(x, rows=True, transposed=True, counts=counts)
+    W8, Wt8 = quantize8(W, blocks=True, rows=True, transposed=True)
+    return matmul8(x8, Wt8, dtype=x.dtype, counts=counts), (xt8, W8, counts)
+
+
+def expert_linear8_backward(dy: torch.Tensor, kept) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(dx, dW) of expert_linear8_train from dy [E,C,N] and what it kept."""
+    xt8, W8, counts = kept
+    dy8, dyt8 = quantize8(dy, rows=True, transposed=True, counts=counts)
+    return matmul8(dy8, W8, dtype=dy.dtype, counts=counts), matmul8(xt8, dyt8, dtype=dy.dtype, k_counts=counts)
+
+
+def _check_ffn8(W1: Block8, b1, W2: Block8, b2, code: int) -> Tuple[int, int, int]:
+    _check8(W1, "W1")
+    _check8(W2, "W2")
+    E, H, M = W1.q.shape[0], W1.q.shape[1], W1.width
+    if not W1.blocks or not W2.blocks or W2.q.shape[:2] != (E, M) or W2.width != H:
+        raise ValueError("W1 must be [E,H,M] and W2 [E,M,H] with one exponent for 128 x 128 values")
+    if (b1 is not None and tuple(b1.shape) != (E, H)) or (b2 is not None and tuple(b2.shape) != (E, M)):
+        raise ValueError("b1 must be [E,H] and b2 [E,M]")
+    _check_storage(code, b1, b2)
+    return E, M, H
+
+
+def expert_ffn8(x8: Block8, W1: Block8, b1: Optional[torch.Tensor], W2: Block8, b2: Optional[torch.Tensor], act: int,
+                dtype: torch.dtype = torch.bfloat16, counts: Optional[torch.Tensor] = None,
+                slot_src: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The experts' layer on 8-bit tokens and weights (quantize8's transposed forms of W1 [E,M,H] and W2 [E,H,M], blocks=True): x8 [E,C,M], or
+    the tokens [T,M] with slot_src [E,C]."""
+    _check8(x8, "x8")
+    dev = x8.q.device
+    code = F32 if dtype == torch.float32 else BF16
+    E, M, H = _check_ffn8(W1, b1, W2, b2, code)
+    C = slot_src.shape[1] if slot_src is not None else x8.q.shape[1]
+    if x8.blocks or x8.width != M or (slot_src is None and x8.q.shape[0] != E) or (slot_src is not None and (x8.q.dim() != 2 or slot_src.shape[0] != E)):
+        raise ValueError("x8 must be [E,C,M], or [T,M] with slot_src [E,C]")
+    _check_int32(counts, E)
+    _check_int32(slot_src, E, C)
+    hidden = _alloc8((E,), C, H, False, dev)
+    Y = torch.empty((E, C, M), dtype=dtype, device=dev)
+    _check(lib().moe_expert_ffn8(_p(x8.q), _p(x8.s), _p(slot_src), x8.q.shape[0] if slot_src is not None else 0, _p(W1.q), _p(W1.s), _p(b1),
+                                 _p(W2.q), _p(W2.s), _p(b2), act, _dtype_code(Y), _p(counts), E, C, M, H, _p(hidden.q), _p(hidden.s), _p(Y),
+                                 _stream()), "moe_expert_ffn8")
+    return Y
+
+
+def _routing_buffers(T: int, E: int, k: int, dev) -> Dict[str, torch.Tensor]:
+    return dict(idx=torch.empty((T, k), dtype=torch.int32, device=dev), loc=torch.empty((T, k), dtype=torch.int32, device=dev),
+                gate_w=torch.empty((T, k), dtype=torch.float32, device=dev), counts=torch.empty((E,), dtype=torch.int32, device=dev),
+                logits=torch.empty((T, E), dtype=torch.float32, device=dev))
+
+
+class FewTokenLayer:
+    """The layer for at most FEW_MAX_TOKENS tokens (moe_layer_forward_few); W1, W2 in the storage dtype ([E,M,H], [E,H,M]) or Block8 as
+    expert_ffn8 takes them.  Owns workspace and outputs: `forward` allocates nothing."""
+
+    def __init__(self, Wg, gate_bias, W1, b1, W2, b2, T: int, k: int, f: float, normalize: int, act: int, keep_routing: bool = False):
+        self.weights = (Wg, gate_bias, W1, b1, W2, b2)          # kept alive: the call below holds their addresses
+        self.T, self.k, self.act = T, k, int(act)
+        code = _dtype_code(Wg)
+        self.dtype = code
+        if isinstance(W1, Block8):
+            self.E, self.M, self.H = _check_ffn8(W1, b1, W2, b2, code)
+            w1, s1, w2, s2 = W1.q, W1.s, W2.q, W2.s
+        else:
+            self.E, self.M, self.H = W1.shape
+            _check_storage(code, W1, b1, W2, b2)
+            w1, s1, w2, s2 = W1, None, W2, None
+        if tuple(Wg.shape) != (self.M, self.E) or (s1 is None and tuple(W2.shape) != (self.E, self.H, self.M)):
+            raise ValueError("Wg must be [M,E], W1 [E,M,H] and W2 [E,H,M]")
+        dev = Wg.device
+        nbytes = int(lib().moe_layer_few_workspace_bytes(T, self.M, self.H, self.E, k, code))
+        if nbytes == 0:
+            raise MoEError(UNSUPPORTED, "moe_layer_few_workspace_bytes")
+        self.ws = torch.empty((nbytes,), dtype=torch.uint8, device=dev)
+        self.out = torch.empty((T, self.M), dtype=Wg.dtype, device=dev)
+        self.routing = _routing_buffers(T, self.E, k, dev) if keep_routing else None
+        r = self.routing or {}
+        self._args = (_p(Wg), _p(gate_bias), _p(w1), _p(s1), _p(b1), _p(w2), _p(s2), _p(b2), T, self.M, self.H, self.E, k, float(f),
+                      int(normalize), self.act, code, _p(self.out), _p(r.get("idx")), _p(r.get("loc")), _p(r.get("gate_w")),
+                      _p(r.get("counts")), _p(r.get("logits")), _p(self.ws), nbytes)
+
+    def forward(self, x: torch.Tensor) -> torch.Tensor:
+        if tuple(x.shape) != (self.T, self.M) or _dtype_code(x) != self.dtype:
+            raise ValueError(f"x must be [{self.T}, {self.M}] in the layer's storage dtype")
+        _check(lib().moe_layer_forward_few(_p(x), *self._args, _stream()), "moe_layer_forward_few")
+        return self.out
+
+
+class NormMoELayer8:
+    """A pre-norm block around 8-bit experts: h = x + residual, out = MoE(RMS norm of h).  The norm writes the tokens once for the gate and once in 8 bits
+    for the experts; few tokens go through moe_layer_forward_few on the same weights.  Owns workspace and outputs."""
+
+    def __init__(self, norm_weight, eps: float, Wg, gate_bias, W1: Block8, b1, W2: Block8, b2, T: int, k: int, f: float, normalize: int, act: int,
+                 keep_routing: bool = False):
+        self.norm_weight, self.eps = norm_weight, float(eps)
+        self.few = FewTokenLayer(Wg, gate_bias, W1, b1, W2, b2, T, k, f, normalize, act, keep_routing) if T <= FEW_MAX_TOKENS else None
+        code = _dtype_code(Wg)
+        E, M, H = _check_ffn8(W1, b1, W2, b2, code)
+        if tuple(Wg.shape) != (M, E):
+            raise ValueError("Wg must be [M,E]")
+        dev = Wg.device
+        self.normed = dict(h=torch.empty((T, M), dtype=Wg.dtype, device=dev), y=torch.empty((T, M), dtype=Wg.dtype, device=dev),
+                           y8=None if self.few else _alloc8((), T, M, False, dev))
+        if self.few:
+            self.out, self.routing = self.few.out, self.few.routing
+            return
+        C = capacity(T, E, k, f)
+        if C < 1:
+            raise MoEError(INVALID_ARG, "moe_capacity")
+        nbytes = int(lib().moe_layer8_workspace_bytes(T, M, H, E, k, C, code))
+        if nbytes == 0:
+            raise MoEError(UNSUPPORTED, "moe_layer8_workspace_bytes")
+        self.weights = (Wg, gate_bias, W1, b1, W2, b2)
+        self.ws = torch.empty((nbytes,), dtype=torch.uint8, device=dev)
+        self.out = torch.empty((T, M), dtype=Wg.dtype, device=dev)
+        self.routing = _routing_buffers(T, E, k, dev) if keep_routing else None
+        r = self.routing or {}
+        self._args = (_p(Wg), _p(gate_bias), _p(W1.q), _p(W1.s), _p(b1), _p(W2.q), _p(W2.s), _p(b2), T, M, H, E, k, float(f), int(normalize),
+                      int(act), code, _p(self.out), _p(r.get("idx")), _p(r.get("loc")), _p(r.get("gate_w")), _p(r.get("counts")),
+                      _p(r.get("logits")), _p(self.ws), nbytes)
+
+    def forward(self, x: torch.Tensor, residual: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+        """(out, h): h is the residual of the next block."""
+        if x.shape != self.normed["h"].shape:
+            raise ValueError(f"x must be {tuple(self.normed['h'].shape)}")
+        n = rms_norm(x, self.norm_weight, self.eps, residual=residual, out=self.normed)
+        if self.few:
+            return self.few.forward(n["y"]), n["h"]
+        _check(lib().moe_layer_forward8(_p(n["y"]), _p(n["y8"].q), _p(n["y8"].s), *self._args, _stream()), "moe_layer_forward8")
+        return self.out, n["h"]
