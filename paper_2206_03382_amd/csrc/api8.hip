@@ -9,6 +9,7 @@ namespace moe {
 namespace {
 
 constexpr int64_t kNormMaxWidth = 16384, kNormMaxRows = (int64_t)1 << 22;
+constexpr int64_t kFewMaxWidth = (int64_t)1 << 22;
 constexpr int64_t kMaxGrid = (int64_t)1 << 24;                      // blocks of 256 threads in a grid dimension
 
 int norm_shape_status(int64_t T, int64_t M) {
@@ -60,7 +61,7 @@ Layer8Workspace layer8_layout(int64_t T, int64_t M, int64_t H, int64_t E, int k,
 }
 
 struct FewWorkspace {
-  size_t logits, idx, loc, gate_w, counts, gate_ws, hidden, total;
+  size_t logits, idx, loc, gate_w, counts, gate_ws, logit_parts, plan, hidden, partial, arrived, total;
 };
 
 FewWorkspace few_layout(int64_t T, int64_t M, int64_t H, int64_t E, int k, int dtype) {
@@ -72,10 +73,23 @@ FewWorkspace few_layout(int64_t T, int64_t M, int64_t H, int64_t E, int k, int d
   w.loc = take((size_t)T * k * 4);
   w.gate_w = take((size_t)T * k * 4);
   w.counts = take((size_t)E * 4);
-  w.gate_ws = take(moe_gate_route_workspace_bytes(T, M, E, k, dtype));
+  const int slices = few_gate_slices(T, M, E, k);
+  w.gate_ws = take(slices > 0 ? 0 : moe_gate_route_workspace_bytes(T, M, E, k, dtype));
+  w.logit_parts = take((size_t)slices * T * E * 8);
+  w.plan = take((size_t)(E < T * k ? E : T * k) * kFewPlan * 4);
   w.hidden = take((size_t)T * k * H * esize(dtype));
+  w.partial = take((size_t)T * k * M * 4);
+  w.arrived = take(few_arrivals_bytes(M));
   w.total = off;
   return w;
+}
+
+// a layer of few tokens: offsets inside a step of a weight matrix, and inside an expert's 8-bit weights, fit 32 bits
+int few_shape_status(int64_t M, int64_t H, bool weights8) {
+  if (M > kFewMaxWidth || H > kFewMaxWidth) return MOE_UNSUPPORTED;
+  if (!weights8) return MOE_OK;
+  if (int st = weights8_status(M, H)) return st;
+  return weights8_status(H, M);
 }
 
 int layer_shape_status(int64_t T, int64_t M, int64_t H, int64_t E, int k, int dtype) {
@@ -210,7 +224,7 @@ int moe_layer_forward8(const void* x, const void* x8, const uint8_t* x_scales, c
 }
 
 size_t moe_layer_few_workspace_bytes(int64_t T, int64_t M, int64_t H, int64_t E, int k, int dtype) {
-  if (T > MOE_FEW_MAX_TOKENS || layer_shape_status(T, M, H, E, k, dtype) != MOE_OK) return 0;
+  if (T > MOE_FEW_MAX_TOKENS || layer_shape_status(T, M, H, E, k, dtype) != MOE_OK || few_shape_status(M, H, false) != MOE_OK) return 0;
   return few_layout(T, M, H, E, k, dtype).total;
 }
 
@@ -221,6 +235,7 @@ int moe_layer_forward_few(const void* x, const void* Wg, const float* gate_bias,
   if (!x || !Wg || !W1 || !W2 || !out || !ws || (!s1) != (!s2) || !act_ok(act) || !(f > 0.0)) return MOE_INVALID_ARG;
   if (int st = layer_shape_status(T, M, H, E, k, dtype)) return st;
   if (T > MOE_FEW_MAX_TOKENS) return MOE_UNSUPPORTED;
+  if (int st = few_shape_status(M, H, s1 != nullptr)) return st;
   const int64_t C = moe_capacity(T, E, k, f);
   if (C < 1 || C > kMaxDim) return MOE_INVALID_ARG;
   if (!all_aligned16({x, W1, b1, W2, b2, out, logits}) || !aligned(ws, 256)) return MOE_UNSUPPORTED;
@@ -232,10 +247,14 @@ int moe_layer_forward_few(const void* x, const void* Wg, const float* gate_bias,
   gate_w = gate_w ? gate_w : (float*)(base + w.gate_w);
   counts = counts ? counts : (int32_t*)(base + w.counts);
   logits = logits ? logits : (float*)(base + w.logits);
-  if (int st = moe_gate_route(x, Wg, gate_bias, dtype, T, M, E, k, C, normalize, logits, idx, gate_w, loc, counts, nullptr, base + w.gate_ws,
-                              moe_gate_route_workspace_bytes(T, M, E, k, dtype), stream))
-    return st;
-  const FewTokens p = {x, W1, b1, W2, b2, s1, s2, idx, loc, counts, gate_w, T, M, H, E, C, k, act, dtype, base + w.hidden, out};
+  const int slices = few_gate_slices(T, M, E, k);
+  if (slices == 0)
+    if (int st = moe_gate_route(x, Wg, gate_bias, dtype, T, M, E, k, C, normalize, logits, idx, gate_w, loc, counts, nullptr, base + w.gate_ws,
+                                moe_gate_route_workspace_bytes(T, M, E, k, dtype), stream))
+      return st;
+  const FewTokens p = {x, Wg, W1, b1, W2, b2, gate_bias, s1, s2, idx, loc, counts, gate_w, logits, T, M, H, E, C, k, act, dtype, normalize, slices,
+                       (double*)(base + w.logit_parts), (int32_t*)(base + w.plan), base + w.hidden, (float*)(base + w.partial),
+                       (int32_t*)(base + w.arrived), out};
   return status_of(launch_few_tokens(p, (hipStream_t)stream));
 }
 

@@ -79,15 +79,23 @@ struct Matmul8 {
 hipError_t launch_matmul8(const Matmul8& p, hipStream_t s);
 
 struct FewTokens {
-  const void *x, *W1, *b1, *W2, *b2;
+  const void *x, *Wg, *W1, *b1, *W2, *b2;
+  const float* gate_bias;
   const uint8_t *s1, *s2;         // 8-bit weights [E, N, row_bytes8(K)] (blocks of 128 x 128), or null: [E, K, N] in dtype
-  const int32_t *idx, *loc, *counts;
-  const float* gate_w;
+  int32_t *idx, *loc, *counts;    // the gate's decisions: outputs if slices > 0, else idx is given
+  float *gate_w, *logits;
   int64_t T, M, H, E, C;
-  int k, act, dtype;
-  void* hidden;
+  int k, act, dtype, normalize, slices;      // slices: few_gate_slices
+  double* logit_parts;            // [slices, T, E]
+  int32_t* plan;                  // [min(E, T k), kFewPlan]
+  void* hidden;                   // [T k, H]
+  float* partial;                 // [T k, M]
+  int32_t* arrived;               // few_arrivals_bytes(M)
   void* out;
 };
+constexpr int kFewPlan = 2 + MOE_FEW_MAX_TOKENS;
+int few_gate_slices(int64_t T, int64_t M, int64_t E, int k);
+size_t few_arrivals_bytes(int64_t M);
 hipError_t launch_few_tokens(const FewTokens& p, hipStream_t s);
 
 }  // namespace moe
