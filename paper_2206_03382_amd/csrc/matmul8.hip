@@ -241,7 +241,34 @@ hipError_t launch_tile(const Matmul8& p, hipStream_t s) {
 
 }  // namespace
 
+#include "matmul8_large.h"
+
+namespace {
+
+// The forms that the large tile has: a plain product, with either form of B's exponents, and the experts' first one, which applies the activation and rounds to 8 bits.
+bool large_covers(const Matmul8& p) {
+  const int64_t tiles = p.E * ceil_div(p.C, kBig) * ceil_div(p.N, kBig);
+  return p.dtype == MOE_BF16 && p.E <= kMaxExperts && tiles < kMaxBlocks && (p.out ? p.act < 0 : p.act >= 0 && p.b_blocks);
+}
+
+hipError_t launch_large(const Matmul8& p, hipStream_t s) {
+  Args8 a = {p, row_bytes8(p.K), row_scales8(p.K), row_bytes8(p.N), row_scales8(p.N), (int)ceil_div(p.C, kBig), (int)ceil_div(p.N, kBig), 0};
+  const int64_t all = p.E * p.C, total = p.counts && p.rows_hint ? (p.E * p.rows_hint < all ? p.E * p.rows_hint : all) : all;
+  const dim3 grid((unsigned)tile_grid(a.NT, live_row_tiles(p.E, p.C, total, kBig), true)), block(256);
+#define MOE_BIG(ACT, OUT8, BLOCKS) matmul8_large_kernel<ACT, OUT8, BLOCKS><<<grid, block, 0, s>>>(a)
+  if (!p.b_blocks) MOE_BIG(-1, false, false);
+  else if (p.out) MOE_BIG(-1, false, true);
+  else if (p.act == MOE_ACT_RELU) MOE_BIG(MOE_ACT_RELU, true, true);
+  else if (p.act == MOE_ACT_GELU) MOE_BIG(MOE_ACT_GELU, true, true);
+  else MOE_BIG(MOE_ACT_SILU, true, true);
+#undef MOE_BIG
+  return hipGetLastError();
+}
+
+}  // namespace
+
 hipError_t launch_matmul8(const Matmul8& p, hipStream_t s) {
+  if (large_covers(p) && p.C >= 512 && p.N >= 256) return launch_large(p, s);
   return p.dtype == MOE_F32 ? launch_tile<128, 128, 2, 2, 2, true>(p, s) : launch_tile<128, 128, 2, 2, 2, false>(p, s);
 }
 

@@ -1,0 +1,264 @@
+// The 8-bit products' large tile: 256 x 256 to a block of four waves, 128 x 128 each.  Included by matmul8.hip (same arguments and results).
+//
+// K advances by 128, a block of the format: 64 products of 16 x 16 x 128 a wave, 2048 cycles, for 64 KB of LDS that direct loads fill one K-step ahead (two
+// stages).  A wave's rows are four pairs of 16-row fragments, 64 rows apart, so that both waves of a column share what a ragged tile has: NI of the pairs
+// exist, the others are neither loaded nor multiplied.  A K-step runs in two halves of 8 NI products.  The first uses the fragments 0 .. NI - 1 of A and reads the
+// others; then the next stage has to have landed (one wait, one barrier); the second half uses the others and reads the next K-step's B, each fragment into the registers of
+// the one that its four products have just used, and the next first half of A.  Its direct loads go out between the second half's products: the stage that they fill has been read by
+// every wave at the barrier.
+namespace {
+
+constexpr int kBig = 256, kBigStage = 2 * kBig * kBlock8;           // 64 KB
+
+// The body has no branch but the one around the exponents' fetch: past the reduction's end the direct loads bring the last K-step again and the reads what nobody uses.  With
+// conditions around them the compiler moved accumulators about at every one (hundreds of moves and spills a K-step).
+// BLOCKS: B has one exponent for 128 x 128 values.  The exponents of four K-steps are a word, fetched in the first half of the last of them and taken at the next barrier, where
+// every load has landed anyway: the compiler, which does not know of the direct loads, would have it wait for them as well.
+template <int NI, bool BLOCKS>
+__device__ __forceinline__ void big_loop(char* smem, const char* (&a_at)[8], const char* b_base, const uint32_t (&b_at)[8], const uint8_t* a_scales,
+                                         const uint32_t (&a_sc)[8], const uint8_t* b_scales, int b_first, int b_last, int row_sc, int KT, int a_off, int b_off,
+                                         int wave, f32x4 (&acc)[8][8]) {
+  constexpr int NB = BLOCKS ? 1 : 8, LOADS = 8 + 2 * NI;
+  const uint32_t smem_addr = (uint32_t)(uintptr_t)LDS_PTR(char, smem);
+  i32x8 a[2 * NI], b[8];
+  uint32_t sa[2 * NI], sb[NB], wa[2 * NI], wb[NB];                  // exponents of this K-step (in the low byte), words of four
+  const char* b_src = b_base;
+  uint32_t fill = smem_addr + wave * 1024;                          // where the next direct loads go
+  int ahead = KT - 1;                                               // K-steps after the one that is loaded next
+  auto load = [&](int q) {                                          // q-th of a K-step's: 2 NI of A, 8 of B
+    if (q < 2 * NI) global_to_lds_16(a_at[q], fill + q * 4096);
+    else global_to_lds_16(b_src, b_at[q - 2 * NI], fill + kBig * kBlock8 + (q - 2 * NI) * 4096);
+  };
+  auto loaded = [&]() {
+    const int step = ahead > 0 ? kBlock8 : 0;
+    --ahead;
+#pragma unroll
+    for (int q = 0; q < 2 * NI; ++q) a_at[q] += step;
+    b_src += step;
+    fill ^= kBigStage;
+  };
+  auto read = [&](const char* at, int off) -> i32x8 {
+    const u32x4 lo = *LDS_PTR(u32x4, at + off), hi = *LDS_PTR(u32x4, at + (off ^ 64));
+    return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+  };
+  auto read_a = [&](const char* st, int i) { a[i] = read(st + (i >> 1) * 8192 + (i & 1) * 2048, a_off); };
+  auto read_b = [&](const char* st, int j) { b[j] = read(st + j * 2048, b_off); };
+  auto product = [&](int i, int j) {
+    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j], a[i], acc[i][j], 0, 0, 0, (int)sb[BLOCKS ? 0 : j], 0, (int)sa[i]);
+  };
+  auto fetch_scales = [&](int word) {
+#pragma unroll
+    for (int i = 0; i < 2 * NI; ++i) wa[i] = *reinterpret_cast<const uint32_t*>(a_scales + a_sc[i] + word * 4);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const int n = b_first + 16 * j;
+      wb[j] = *reinterpret_cast<const uint32_t*>(b_scales + (uint32_t)((BLOCKS || n < b_last ? n : b_last) * row_sc) + word * 4);
+    }
+  };
+  fetch_scales(0);
+#pragma unroll
+  for (int q = 0; q < LOADS; ++q) load(q);
+  loaded();
+  asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 2 * NI; ++i) sa[i] = wa[i];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) sb[j] = wb[j];
+#pragma unroll
+  for (int i = 0; i < 2 * NI; ++i) asm volatile("" : "+v"(sa[i]));
+#pragma unroll
+  for (int j = 0; j < NB; ++j) asm volatile("" : "+v"(sb[j]));
+#pragma unroll
+  for (int q = 0; q < LOADS; ++q) load(q);
+  loaded();
+#pragma unroll
+  for (int i = 0; i < NI; ++i) read_a(smem, i);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) read_b(smem, j);
+#pragma unroll 1
+  for (int kt = 0; kt < KT; ++kt) {
+    const char* cur = smem + (kt & 1) * kBigStage;
+    const char* nxt = smem + ((kt + 1) & 1) * kBigStage;
+    if ((kt & 3) == 3 && kt + 1 < KT) fetch_scales((kt + 1) >> 2);
+    PIN();
+#pragma unroll
+    for (int m = 0; m < 8 * NI; ++m) {
+      product(m % NI, m / NI);
+      PIN();
+      if (m < NI) read_a(cur, NI + m);
+      PIN();
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    PIN();
+    const int shift = ((kt + 1) & 3) * 8;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) sa[i] = wa[i] >> shift;
+#pragma unroll
+    for (int i = NI; i < 2 * NI; ++i) asm volatile("" : "+v"(wa[i]));
+#pragma unroll
+    for (int j = 0; j < NB; ++j) asm volatile("" : "+v"(wb[j]));
+    PIN();
+#pragma unroll
+    for (int m = 0; m < 8 * NI; ++m) {
+      const int i = m % NI, j = m / NI;
+      product(NI + i, j);
+      PIN();
+      if (i == NI - 1) {
+        read_b(nxt, j);
+        if constexpr (!BLOCKS) sb[j] = wb[j] >> shift;
+      }
+      if (NI == 1 ? m == 0 : (m % NI == 0 && m / NI < NI)) read_a(nxt, m / NI);
+#pragma unroll
+      for (int q = m * LOADS / (8 * NI); q < (m + 1) * LOADS / (8 * NI); ++q) load(q);       // evenly
+      PIN();
+    }
+    loaded();
+#pragma unroll
+    for (int i = NI; i < 2 * NI; ++i) sa[i] = wa[i] >> shift;
+    if (BLOCKS) sb[0] = wb[0] >> shift;
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                  // what was loaded past the end must not land in the epilogue's LDS
+}
+
+}  // namespace
+
+template <int ACT, bool OUT8, bool BLOCKS>
+__global__ __launch_bounds__(256, 1) void matmul8_large_kernel(const Args8 args) {
+  __shared__ __attribute__((aligned(1024))) char smem[2 * kBigStage];
+  const Matmul8& p = args.p;
+  const int lane = threadIdx.x & 63;
+  int e, mt, nt, rows;
+  if (!find_tile<kBig, false, 0, true>(blockIdx.x, lane, (int)p.E, p.C, p.counts, args.NT, e, mt, nt, rows)) return;
+  const int64_t m0 = (int64_t)mt * kBig;
+  if (m0 >= rows) return;
+  const int n0 = nt * kBig;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave >> 1, wn = wave & 1, fr = lane & 15, g = lane >> 4;
+  const int N = (int)p.N;
+  int KT = (int)(args.row8 / kBlock8);
+  if (p.k_counts) {
+    const int64_t c = p.k_counts[e], most = c < p.K ? (c > 0 ? c : 0) : p.K;
+    KT = (int)((most + kBlock8 - 1) / kBlock8);
+  }
+  const int live = (int)(rows - m0 < kBig ? rows - m0 : kBig), ni = (live + 63) >> 6;
+  auto a_row = [&](int r) -> int64_t {                              // without a gather: of the expert's slab
+    const int64_t c = r < live ? m0 + r : rows - 1;                 // rows past the fill repeat the last one (never stored)
+    if (!p.gather) return c;
+    const int t = p.gather[(int64_t)e * p.C + c];
+    return (unsigned)t < (uint64_t)p.gather_rows ? t : 0;
+  };
+  const int64_t slab = p.gather ? 0 : (int64_t)e * p.C;
+  const char* a_at[8];
+  uint32_t b_at[8], a_sc[8];
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    const int r = (q * 4 + wave) * 8 + (lane >> 3), piece = ((lane & 7) ^ ((r >> 1) & 7)) << 4;
+    a_at[q] = (const char*)p.A + (slab + a_row(r)) * args.row8 + piece;
+    b_at[q] = (uint32_t)((int64_t)(n0 + r < N ? n0 + r : N - 1) * args.row8 + piece);
+    a_sc[q] = (uint32_t)(a_row(((q >> 1) * 2 + wm) * 32 + (q & 1) * 16 + fr) * args.row_sc);
+  }
+  const char* b_base = (const char*)p.B + (int64_t)e * N * args.row8;
+  const uint8_t* a_scales = p.A_scales + slab * args.row_sc;
+  const int NB = (N + kBlock8 - 1) / kBlock8, nw = n0 + wn * 128;
+  const uint8_t* b_scales = p.B_scales + (int64_t)e * (BLOCKS ? NB : N) * args.row_sc;
+  const int b_first = BLOCKS ? (nw / kBlock8 < NB ? nw / kBlock8 : NB - 1) : nw + fr;
+  const int sw = (fr >> 1) & 7;
+  const int a_off = wm * 4096 + fr * kBlock8 + ((g ^ sw) << 4), b_off = kBig * kBlock8 + wn * 16384 + fr * kBlock8 + ((g ^ sw) << 4);
+  f32x4 acc[8][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (KT > 0) {
+#define MOE_BIG_LOOP(NI) \
+  big_loop<NI, BLOCKS>(smem, a_at, b_base, b_at, a_scales, a_sc, b_scales, b_first, N - 1, (int)args.row_sc, KT, a_off, b_off, wave, acc)
+    switch (ni) {
+      case 4: MOE_BIG_LOOP(4); break;
+      case 3: MOE_BIG_LOOP(3); break;
+      case 2: MOE_BIG_LOOP(2); break;
+      default: MOE_BIG_LOOP(1); break;
+    }
+#undef MOE_BIG_LOOP
+  }
+  // Lane (16 g + fr) has row fr of fragment i and columns 16 j + 4 g .. + 3 of the wave's 128: through LDS, 32 KB to a wave, to whole row pieces.
+  float bias[8][4];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int n = nw + 16 * j + 4 * g;
+    u32x2 w = {0, 0};
+    if (p.bias && n < N) w = *reinterpret_cast<const u32x2*>((const uint16_t*)p.bias + (int64_t)e * N + n);
+    bias[j][0] = __uint_as_float(w.x << 16);
+    bias[j][1] = __uint_as_float(w.x & 0xffff0000u);
+    bias[j][2] = __uint_as_float(w.y << 16);
+    bias[j][3] = __uint_as_float(w.y & 0xffff0000u);
+  }
+  __syncthreads();                                                  // every wave is done with the stages
+  char* own = smem + wave * 32768;
+  const int64_t blocks = args.out_row8 / kBlock8, nb = nw / kBlock8;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (i >= 2 * ni) break;
+    PIN();
+    float v[8][4];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        v[j][c] = acc[i][j][c] + bias[j][c];
+        if (ACT >= 0) v[j][c] = apply_act(v[j][c], ACT);
+        if (OUT8 && nw + 16 * j + 4 * g >= N) v[j][c] = 0.f;        // N is a multiple of 8
+      }
+    const int r = i * 16 + fr;
+    if constexpr (!OUT8) {
+      // two halves of 64 columns: [128 rows][8 pieces of 8 columns], piece c of row r at c ^ r % 8
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        *LDS_PTR(u32x2, own + (j >> 2) * 16384 + r * 128 + (((2 * (j & 3) + (g >> 1)) ^ (r & 7)) << 4) + 8 * (g & 1)) =
+            u32x2{pack_bf16x2(v[j][0], v[j][1]), pack_bf16x2(v[j][2], v[j][3])};
+    } else {
+      // the wave's 128 columns are one block of the format
+      uint32_t top = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) top = max(top, magnitude_bits(v[j][c]));
+      top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+      top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+      const uint32_t sc = scale_of_amax(top);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) *LDS_PTR(uint32_t, own + r * 128 + ((j ^ (r & 7)) << 4) + 4 * g) = pack8x4(v[j][0], v[j][1], v[j][2], v[j][3], sc);
+      const int row = ((i >> 1) * 2 + wm) * 32 + (i & 1) * 16 + fr;
+      if (g == 0 && row < live && nb < blocks) {
+        uint8_t* to = p.out8_scales + ((int64_t)e * p.C + m0 + row) * args.out_row_sc;
+        to[nb] = (uint8_t)sc;
+        if (nb == blocks - 1)
+          for (int64_t b = blocks; b < args.out_row_sc; ++b) to[b] = (uint8_t)kScaleOne;
+      }
+    }
+  }
+  // stores of 8 rows x 128 bytes
+  if constexpr (!OUT8) {
+    uint16_t* oute = (uint16_t*)p.out + ((int64_t)e * p.C + m0) * N;
+#pragma unroll 2
+    for (int it = 0; it < 4 * ni; ++it) {
+      const int r = it * 8 + (lane >> 3), c = (lane & 7) ^ (r & 7);
+      const int row = ((r >> 5) * 2 + wm) * 32 + (r & 31);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const u32x4 w = *LDS_PTR(u32x4, own + h * 16384 + r * 128 + ((lane & 7) << 4));
+        const int n = nw + h * 64 + c * 8;
+        if (row < live && n < N) *reinterpret_cast<u32x4*>(oute + (int64_t)row * N + n) = w;
+      }
+    }
+  } else {
+    uint8_t* oute = (uint8_t*)p.out8 + ((int64_t)e * p.C + m0) * args.out_row8;
+#pragma unroll 4
+    for (int it = 0; it < 4 * ni; ++it) {
+      const int r = it * 8 + (lane >> 3), c = (lane & 7) ^ (r & 7);
+      const int row = ((r >> 5) * 2 + wm) * 32 + (r & 31);
+      const u32x4 w = *LDS_PTR(u32x4, own + r * 128 + ((lane & 7) << 4));
+      const int n = nw + c * 16;
+      if (row < live && n < args.out_row8) *reinterpret_cast<u32x4*>(oute + (int64_t)row * args.out_row8 + n) = w;
+    }
+  }
+}
