@@ -33,6 +33,11 @@ template <bool STREAM = false> __device__ __forceinline__ void global_to_lds_16(
   else asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(addr), "s"(lds_addr) : "memory", "m0");
 }
 
+// 4 bytes per lane.
+__device__ __forceinline__ void global_to_lds_4(const void* addr, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" : : "v"(addr), "s"(lds_addr) : "memory", "m0");
+}
+
 // Inclusive prefix sum over the 64 lanes with data-parallel primitives (shifts inside rows of 16 lanes, then the rows'
 // totals broadcast forward): no trip through the LDS crossbar, a few cycles per step.
 __device__ __forceinline__ int wave_inclusive_scan(int v) {

@@ -9,19 +9,20 @@
 namespace {
 
 constexpr int kBig = 256, kBigStage = 2 * kBig * kBlock8;           // 64 KB
+constexpr int kScaleWords = 16, kScaleBytes = kScaleWords * 2 * kBig * 4;    // words of four exponents of A's and B's rows: K = 8192; 32 KB
 
 // The body has no branch but the one around the exponents' fetch: past the reduction's end the direct loads bring the last K-step again and the reads what nobody uses.  With
 // conditions around them the compiler moved accumulators about at every one (hundreds of moves and spills a K-step).
-// BLOCKS: B has one exponent for 128 x 128 values.  The exponents of four K-steps are a word, fetched in the first half of the last of them and taken at the next barrier, where
-// every load has landed anyway: the compiler, which does not know of the direct loads, would have it wait for them as well.
+// The exponents of up to 64 K-steps are brought into LDS before the first of them, [word of four][row] of A and then of B: a load that goes out in between would have to come all the
+// way from memory before the K-step's own loads count as landed.
+// BLOCKS: B has one exponent for 128 x 128 values.
 template <int NI, bool BLOCKS>
-__device__ __forceinline__ void big_loop(char* smem, const char* (&a_at)[8], const char* b_base, const uint32_t (&b_at)[8], const uint8_t* a_scales,
-                                         const uint32_t (&a_sc)[8], const uint8_t* b_scales, int b_first, int b_last, int row_sc, int KT, int a_off, int b_off,
-                                         int wave, f32x4 (&acc)[8][8]) {
+__device__ __forceinline__ void big_loop(char* smem, const char* (&a_at)[8], const char* b_base, const uint32_t (&b_at)[8], const uint8_t* a_sc, const uint8_t* b_sc,
+                                         int row_sc, int KT, int a_off, int b_off, int sa_off, int sb_off, int wave, f32x4 (&acc)[8][8]) {
   constexpr int NB = BLOCKS ? 1 : 8, LOADS = 8 + 2 * NI;
   const uint32_t smem_addr = (uint32_t)(uintptr_t)LDS_PTR(char, smem);
   i32x8 a[2 * NI], b[8];
-  uint32_t sa[2 * NI], sb[NB], wa[2 * NI], wb[NB];                  // exponents of this K-step (in the low byte), words of four
+  uint32_t sa[2 * NI], sb[NB];                                      // exponents of this K-step
   const char* b_src = b_base;
   uint32_t fill = smem_addr + wave * 1024;                          // where the next direct loads go
   int ahead = KT - 1;                                               // K-steps after the one that is loaded next
@@ -37,85 +38,92 @@ __device__ __forceinline__ void big_loop(char* smem, const char* (&a_at)[8], con
     b_src += step;
     fill ^= kBigStage;
   };
+  auto load_scales = [&](int first) {                               // of the K-steps from `first`, a multiple of 64
+    const int words = (row_sc - first) / 4 < kScaleWords ? (row_sc - first) / 4 : kScaleWords;
+    for (int w = 0; w < words; ++w) {
+      const uint32_t to = smem_addr + 2 * kBigStage + w * 2048 + wave * 256;
+      global_to_lds_4(a_sc + first + 4 * w, to);
+      global_to_lds_4(b_sc + first + 4 * w, to + 1024);
+    }
+  };
   auto read = [&](const char* at, int off) -> i32x8 {
     const u32x4 lo = *LDS_PTR(u32x4, at + off), hi = *LDS_PTR(u32x4, at + (off ^ 64));
     return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
   };
   auto read_a = [&](const char* st, int i) { a[i] = read(st + (i >> 1) * 8192 + (i & 1) * 2048, a_off); };
   auto read_b = [&](const char* st, int j) { b[j] = read(st + j * 2048, b_off); };
+  const char* scales = smem + 2 * kBigStage;                        // of the K-step whose exponents are read next
+  auto read_sa = [&](int i) { sa[i] = *LDS_PTR(uint8_t, scales + sa_off + (i >> 1) * 256 + (i & 1) * 64); };
+  auto read_sb = [&](int j) { sb[j] = *LDS_PTR(uint8_t, scales + sb_off + j * 64); };
   auto product = [&](int i, int j) {
     acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j], a[i], acc[i][j], 0, 0, 0, (int)sb[BLOCKS ? 0 : j], 0, (int)sa[i]);
   };
-  auto fetch_scales = [&](int word) {
-#pragma unroll
-    for (int i = 0; i < 2 * NI; ++i) wa[i] = *reinterpret_cast<const uint32_t*>(a_scales + a_sc[i] + word * 4);
-#pragma unroll
-    for (int j = 0; j < NB; ++j) {
-      const int n = b_first + 16 * j;
-      wb[j] = *reinterpret_cast<const uint32_t*>(b_scales + (uint32_t)((BLOCKS || n < b_last ? n : b_last) * row_sc) + word * 4);
-    }
-  };
-  fetch_scales(0);
+  load_scales(0);
 #pragma unroll
   for (int q = 0; q < LOADS; ++q) load(q);
   loaded();
   asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
-  for (int i = 0; i < 2 * NI; ++i) sa[i] = wa[i];
-#pragma unroll
-  for (int j = 0; j < NB; ++j) sb[j] = wb[j];
-#pragma unroll
-  for (int i = 0; i < 2 * NI; ++i) asm volatile("" : "+v"(sa[i]));
-#pragma unroll
-  for (int j = 0; j < NB; ++j) asm volatile("" : "+v"(sb[j]));
-#pragma unroll
   for (int q = 0; q < LOADS; ++q) load(q);
   loaded();
+#pragma unroll
+  for (int i = 0; i < 2 * NI; ++i) read_sa(i);
+#pragma unroll
+  for (int j = 0; j < NB; ++j) read_sb(j);
 #pragma unroll
   for (int i = 0; i < NI; ++i) read_a(smem, i);
 #pragma unroll
   for (int j = 0; j < 8; ++j) read_b(smem, j);
+  for (int first = 0; first < KT; first += 4 * kScaleWords) {
+    if (first > 0) {
+      // the last K-step of the part before has read this one's first exponents too early: all of them again
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      load_scales(first);
+      asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+      scales = smem + 2 * kBigStage;
+#pragma unroll
+      for (int i = 0; i < 2 * NI; ++i) read_sa(i);
+#pragma unroll
+      for (int j = 0; j < NB; ++j) read_sb(j);
+    }
+    const int last = KT - first < 4 * kScaleWords ? KT : first + 4 * kScaleWords;
 #pragma unroll 1
-  for (int kt = 0; kt < KT; ++kt) {
-    const char* cur = smem + (kt & 1) * kBigStage;
-    const char* nxt = smem + ((kt + 1) & 1) * kBigStage;
-    if ((kt & 3) == 3 && kt + 1 < KT) fetch_scales((kt + 1) >> 2);
-    PIN();
-#pragma unroll
-    for (int m = 0; m < 8 * NI; ++m) {
-      product(m % NI, m / NI);
+    for (int kt = first; kt < last; ++kt) {
+      const char* cur = smem + (kt & 1) * kBigStage;
+      const char* nxt = smem + ((kt + 1) & 1) * kBigStage;
+      scales = smem + 2 * kBigStage + ((kt + 1) >> 2 & (kScaleWords - 1)) * 2048 + ((kt + 1) & 3);
       PIN();
-      if (m < NI) read_a(cur, NI + m);
-      PIN();
-    }
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    PIN();
-    const int shift = ((kt + 1) & 3) * 8;
 #pragma unroll
-    for (int i = 0; i < NI; ++i) sa[i] = wa[i] >> shift;
-#pragma unroll
-    for (int i = NI; i < 2 * NI; ++i) asm volatile("" : "+v"(wa[i]));
-#pragma unroll
-    for (int j = 0; j < NB; ++j) asm volatile("" : "+v"(wb[j]));
-    PIN();
-#pragma unroll
-    for (int m = 0; m < 8 * NI; ++m) {
-      const int i = m % NI, j = m / NI;
-      product(NI + i, j);
-      PIN();
-      if (i == NI - 1) {
-        read_b(nxt, j);
-        if constexpr (!BLOCKS) sb[j] = wb[j] >> shift;
+      for (int m = 0; m < 8 * NI; ++m) {
+        product(m % NI, m / NI);
+        PIN();
+        if (m < NI) read_a(cur, NI + m);
+        PIN();
       }
-      if (NI == 1 ? m == 0 : (m % NI == 0 && m / NI < NI)) read_a(nxt, m / NI);
-#pragma unroll
-      for (int q = m * LOADS / (8 * NI); q < (m + 1) * LOADS / (8 * NI); ++q) load(q);       // evenly
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
       PIN();
-    }
-    loaded();
 #pragma unroll
-    for (int i = NI; i < 2 * NI; ++i) sa[i] = wa[i] >> shift;
-    if (BLOCKS) sb[0] = wb[0] >> shift;
+      for (int m = 0; m < 8 * NI; ++m) {
+        const int i = m % NI, j = m / NI;
+        product(NI + i, j);
+        PIN();
+        if (i == NI - 1) {
+          read_b(nxt, j);
+          if constexpr (!BLOCKS) read_sb(j);
+        }
+        if (NI == 1 ? m == 0 : (m % NI == 0 && m / NI < NI)) {
+          read_a(nxt, m / NI);
+          read_sa(m / NI);
+        }
+#pragma unroll
+        for (int q = m * LOADS / (8 * NI); q < (m + 1) * LOADS / (8 * NI); ++q) load(q);       // evenly
+        PIN();
+      }
+      loaded();
+#pragma unroll
+      for (int i = NI; i < 2 * NI; ++i) read_sa(i);
+      if constexpr (BLOCKS) read_sb(0);
+    }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                  // what was loaded past the end must not land in the epilogue's LDS
 }
@@ -124,7 +132,7 @@ __device__ __forceinline__ void big_loop(char* smem, const char* (&a_at)[8], con
 
 template <int ACT, bool OUT8, bool BLOCKS>
 __global__ __launch_bounds__(256, 1) void matmul8_large_kernel(const Args8 args) {
-  __shared__ __attribute__((aligned(1024))) char smem[2 * kBigStage];
+  __shared__ __attribute__((aligned(1024))) char smem[2 * kBigStage + kScaleBytes];
   const Matmul8& p = args.p;
   const int lane = threadIdx.x & 63;
   int e, mt, nt, rows;
@@ -149,21 +157,22 @@ __global__ __launch_bounds__(256, 1) void matmul8_large_kernel(const Args8 args)
   };
   const int64_t slab = p.gather ? 0 : (int64_t)e * p.C;
   const char* a_at[8];
-  uint32_t b_at[8], a_sc[8];
+  uint32_t b_at[8];
 #pragma unroll
   for (int q = 0; q < 8; ++q) {
     const int r = (q * 4 + wave) * 8 + (lane >> 3), piece = ((lane & 7) ^ ((r >> 1) & 7)) << 4;
     a_at[q] = (const char*)p.A + (slab + a_row(r)) * args.row8 + piece;
     b_at[q] = (uint32_t)((int64_t)(n0 + r < N ? n0 + r : N - 1) * args.row8 + piece);
-    a_sc[q] = (uint32_t)(a_row(((q >> 1) * 2 + wm) * 32 + (q & 1) * 16 + fr) * args.row_sc);
   }
   const char* b_base = (const char*)p.B + (int64_t)e * N * args.row8;
-  const uint8_t* a_scales = p.A_scales + slab * args.row_sc;
   const int NB = (N + kBlock8 - 1) / kBlock8, nw = n0 + wn * 128;
-  const uint8_t* b_scales = p.B_scales + (int64_t)e * (BLOCKS ? NB : N) * args.row_sc;
-  const int b_first = BLOCKS ? (nw / kBlock8 < NB ? nw / kBlock8 : NB - 1) : nw + fr;
+  // exponents: thread t has row t of A and column t of B
+  const int64_t bn = n0 + (int)threadIdx.x < N ? n0 + threadIdx.x : N - 1;
+  const uint8_t* a_sc = p.A_scales + (slab + a_row(threadIdx.x)) * args.row_sc;
+  const uint8_t* b_sc = p.B_scales + (BLOCKS ? (int64_t)e * NB + bn / kBlock8 : (int64_t)e * N + bn) * args.row_sc;
   const int sw = (fr >> 1) & 7;
   const int a_off = wm * 4096 + fr * kBlock8 + ((g ^ sw) << 4), b_off = kBig * kBlock8 + wn * 16384 + fr * kBlock8 + ((g ^ sw) << 4);
+  const int sa_off = (wm * 32 + fr) * 4, sb_off = 1024 + (wn * 128 + (BLOCKS ? 0 : fr)) * 4;
   f32x4 acc[8][8];
 #pragma unroll
   for (int i = 0; i < 8; ++i)
@@ -171,7 +180,7 @@ __global__ __launch_bounds__(256, 1) void matmul8_large_kernel(const Args8 args)
     for (int j = 0; j < 8; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   if (KT > 0) {
 #define MOE_BIG_LOOP(NI) \
-  big_loop<NI, BLOCKS>(smem, a_at, b_base, b_at, a_scales, a_sc, b_scales, b_first, N - 1, (int)args.row_sc, KT, a_off, b_off, wave, acc)
+  big_loop<NI, BLOCKS>(smem, a_at, b_base, b_at, a_sc, b_sc, (int)args.row_sc, KT, a_off, b_off, sa_off, sb_off, wave, acc)
     switch (ni) {
       case 4: MOE_BIG_LOOP(4); break;
       case 3: MOE_BIG_LOOP(3); break;
