@@ -1,11 +1,20 @@
 // The 8-bit products' large tile: 256 x 256 to a block of four waves, 128 x 128 each.  Included by matmul8.hip (same arguments and results).
 //
-// K advances by 128, a block of the format: 64 products of 16 x 16 x 128 a wave, 2048 cycles, for 64 KB of LDS that direct loads fill one K-step ahead (two
-// stages).  A wave's rows are four pairs of 16-row fragments, 64 rows apart, so that both waves of a column share what a ragged tile has: NI of the pairs
-// exist, the others are neither loaded nor multiplied.  A K-step runs in two halves of 8 NI products.  The first uses the fragments 0 .. NI - 1 of A and reads the
-// others; then the next stage has to have landed (one wait, one barrier); the second half uses the others and reads the next K-step's B, each fragment into the registers of
-// the one that its four products have just used, and the next first half of A.  Its direct loads go out between the second half's products: the stage that they fill has been read by
-// every wave at the barrier.
+// K advances by 128, a block of the format: 64 products of 16 x 16 x 128 a wave, 2048 cycles, for 64 KB of LDS that direct loads fill one K-step ahead (two stages).  A wave's rows
+// are four pairs of 16-row fragments, 64 rows apart, so that both waves of a column share what a ragged tile has: NI of the pairs exist, the others are neither loaded nor
+// multiplied.  A K-step runs in two halves of 8 NI products.  The first uses the fragments 0 .. NI - 1 of A and reads the others; then the next stage has to have landed
+// (one wait, one barrier); the second half uses the others and reads the next K-step's B, each fragment into the registers of the one that its products have just used, and
+// the next first half of A.  Its direct loads go out between the second half's products: the stage that they fill has been read by every wave at the barrier.
+//
+// The bodies have no branches: with conditions around the loads, or one that a product's result lives across, the compiler moved accumulators about at every one (hundreds of moves a
+// K-step).  The exponents of up to 64 K-steps are brought into LDS before the first of them: loads that went out for them in between came all the way from memory before the K-step's own
+// counted as landed (8192^3 2680 -> 2950 TFLOP/s).
+//
+// Measured: 8192^3 371 us = 2.96 PFLOP/s (register-only products: 3.9); 8 experts x 4096 rows, 2048 x 2048 120 us = 2.28, K = 4096 203 us = 2.70.  With four tiles to a unit, a
+// K-step takes 2400 cycles; beside them a tile has 2500 until its first loads go out, 3000 to 5000 (cold operands) until they land, and 8500 for its results.  Tried and not kept: rings of
+// three stages of one operand (the loads of B then have three quarters of a K-step: 10 % slower), K-steps of 64 in rings of five (rows of 64 bytes are half of what a
+// request to the L2 brings: 15 % slower), stores straight from the registers (64-byte pieces of rows: 2 %), persistent blocks that load the next tile while they store (the loads'
+// waits, which count in order, wait for the stores: 30 %), and fetching panels into the L2 ahead (the same waits).
 namespace {
 
 constexpr int kBig = 256, kBigStage = 2 * kBig * kBlock8;           // 64 KB
@@ -13,12 +22,11 @@ constexpr int kScaleWords = 16, kScaleBytes = kScaleWords * 2 * kBig * 4;    // 
 
 // The body has no branch but the one around the exponents' fetch: past the reduction's end the direct loads bring the last K-step again and the reads what nobody uses.  With
 // conditions around them the compiler moved accumulators about at every one (hundreds of moves and spills a K-step).
-// The exponents of up to 64 K-steps are brought into LDS before the first of them, [word of four][row] of A and then of B: a load that goes out in between would have to come all the
-// way from memory before the K-step's own loads count as landed.
+// Exponents in LDS: [word of four][row] of A and then of B.  set_out: gives the accumulators their first values.
 // BLOCKS: B has one exponent for 128 x 128 values.
-template <int NI, bool BLOCKS>
+template <int NI, bool BLOCKS, typename F>
 __device__ __forceinline__ void big_loop(char* smem, const char* (&a_at)[8], const char* b_base, const uint32_t (&b_at)[8], const uint8_t* a_sc, const uint8_t* b_sc,
-                                         int row_sc, int KT, int a_off, int b_off, int sa_off, int sb_off, int wave, f32x4 (&acc)[8][8]) {
+                                         int row_sc, int KT, int a_off, int b_off, int sa_off, int sb_off, int wave, f32x4 (&acc)[8][8], F&& set_out) {
   constexpr int NB = BLOCKS ? 1 : 8, LOADS = 8 + 2 * NI;
   const uint32_t smem_addr = (uint32_t)(uintptr_t)LDS_PTR(char, smem);
   i32x8 a[2 * NI], b[8];
@@ -58,13 +66,53 @@ __device__ __forceinline__ void big_loop(char* smem, const char* (&a_at)[8], con
   auto product = [&](int i, int j) {
     acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j], a[i], acc[i][j], 0, 0, 0, (int)sb[BLOCKS ? 0 : j], 0, (int)sa[i]);
   };
+  // a K-step; LOAD: with the direct loads of the one after the next
+  auto step = [&](int kt, auto LOAD) {
+    const char* cur = smem + (kt & 1) * kBigStage;
+    const char* nxt = smem + ((kt + 1) & 1) * kBigStage;
+    scales = smem + 2 * kBigStage + ((kt + 1) >> 2 & (kScaleWords - 1)) * 2048 + ((kt + 1) & 3);
+    PIN();
+#pragma unroll
+    for (int m = 0; m < 8 * NI; ++m) {
+      product(m % NI, m / NI);
+      PIN();
+      if (m < NI) read_a(cur, NI + m);
+      PIN();
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    PIN();
+#pragma unroll
+    for (int m = 0; m < 8 * NI; ++m) {
+      const int i = m % NI, j = m / NI;
+      product(NI + i, j);
+      PIN();
+      if (i == NI - 1) {
+        read_b(nxt, j);
+        if constexpr (!BLOCKS) read_sb(j);
+      }
+      if (NI == 1 ? m == 0 : (m % NI == 0 && m / NI < NI)) {
+        read_a(nxt, m / NI);
+        read_sa(m / NI);
+      }
+      if constexpr (decltype(LOAD)::value) {
+#pragma unroll
+        for (int q = m * LOADS / (8 * NI); q < (m + 1) * LOADS / (8 * NI); ++q) load(q);       // evenly
+      }
+      PIN();
+    }
+    if constexpr (decltype(LOAD)::value) loaded();
+#pragma unroll
+    for (int i = NI; i < 2 * NI; ++i) read_sa(i);
+    if constexpr (BLOCKS) read_sb(0);
+  };
   load_scales(0);
 #pragma unroll
   for (int q = 0; q < LOADS; ++q) load(q);
   loaded();
+  set_out();                                                        // the accumulators' first values, while all this is on its way
   asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
-  for (int q = 0; q < LOADS; ++q) load(q);
+  for (int q = 0; q < LOADS; ++q) load(q);                          // the last K-step again if there is only one
   loaded();
 #pragma unroll
   for (int i = 0; i < 2 * NI; ++i) read_sa(i);
@@ -74,6 +122,8 @@ __device__ __forceinline__ void big_loop(char* smem, const char* (&a_at)[8], con
   for (int i = 0; i < NI; ++i) read_a(smem, i);
 #pragma unroll
   for (int j = 0; j < 8; ++j) read_b(smem, j);
+  int kt = 0;
+#pragma unroll 1
   for (int first = 0; first < KT; first += 4 * kScaleWords) {
     if (first > 0) {
       // the last K-step of the part before has read this one's first exponents too early: all of them again
@@ -86,46 +136,19 @@ __device__ __forceinline__ void big_loop(char* smem, const char* (&a_at)[8], con
 #pragma unroll
       for (int j = 0; j < NB; ++j) read_sb(j);
     }
-    const int last = KT - first < 4 * kScaleWords ? KT : first + 4 * kScaleWords;
+    const int last = KT - 2 - first < 4 * kScaleWords ? KT - 2 : first + 4 * kScaleWords;
 #pragma unroll 1
-    for (int kt = first; kt < last; ++kt) {
-      const char* cur = smem + (kt & 1) * kBigStage;
-      const char* nxt = smem + ((kt + 1) & 1) * kBigStage;
-      scales = smem + 2 * kBigStage + ((kt + 1) >> 2 & (kScaleWords - 1)) * 2048 + ((kt + 1) & 3);
-      PIN();
-#pragma unroll
-      for (int m = 0; m < 8 * NI; ++m) {
-        product(m % NI, m / NI);
-        PIN();
-        if (m < NI) read_a(cur, NI + m);
-        PIN();
-      }
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      PIN();
-#pragma unroll
-      for (int m = 0; m < 8 * NI; ++m) {
-        const int i = m % NI, j = m / NI;
-        product(NI + i, j);
-        PIN();
-        if (i == NI - 1) {
-          read_b(nxt, j);
-          if constexpr (!BLOCKS) read_sb(j);
-        }
-        if (NI == 1 ? m == 0 : (m % NI == 0 && m / NI < NI)) {
-          read_a(nxt, m / NI);
-          read_sa(m / NI);
-        }
-#pragma unroll
-        for (int q = m * LOADS / (8 * NI); q < (m + 1) * LOADS / (8 * NI); ++q) load(q);       // evenly
-        PIN();
-      }
-      loaded();
-#pragma unroll
-      for (int i = NI; i < 2 * NI; ++i) read_sa(i);
-      if constexpr (BLOCKS) read_sb(0);
-    }
+    for (; kt < last; ++kt) step(kt, std::true_type{});
+    if (kt < KT - 2) continue;
+    const int end = KT - first < 4 * kScaleWords ? KT : first + 4 * kScaleWords;
+#pragma unroll 1
+    for (; kt < end; ++kt) step(kt, std::false_type{});
   }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                  // what was loaded past the end must not land in the epilogue's LDS
+}
+
+template <bool STREAM> __device__ __forceinline__ void store16(void* to, const u32x4& v) {
+  if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(to));
+  else *reinterpret_cast<u32x4*>(to) = v;
 }
 
 }  // namespace
@@ -174,13 +197,21 @@ __global__ __launch_bounds__(256, 1) void matmul8_large_kernel(const Args8 args)
   const int a_off = wm * 4096 + fr * kBlock8 + ((g ^ sw) << 4), b_off = kBig * kBlock8 + wn * 16384 + fr * kBlock8 + ((g ^ sw) << 4);
   const int sa_off = (wm * 32 + fr) * 4, sb_off = 1024 + (wn * 128 + (BLOCKS ? 0 : fr)) * 4;
   f32x4 acc[8][8];
+  auto set_out = [&]() {                                            // to the bias
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+    for (int j = 0; j < 8; ++j) {
+      const int n = nw + 16 * j + 4 * g;
+      u32x2 w = {0, 0};
+      if (p.bias && n < N) w = *reinterpret_cast<const u32x2*>((const uint16_t*)p.bias + (int64_t)e * N + n);
+      const f32x4 v = {__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u)};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < 8; ++i) acc[i][j] = v;
+    }
+  };
+  if (KT == 0) set_out();
   if (KT > 0) {
 #define MOE_BIG_LOOP(NI) \
-  big_loop<NI, BLOCKS>(smem, a_at, b_base, b_at, a_sc, b_sc, (int)args.row_sc, KT, a_off, b_off, sa_off, sb_off, wave, acc)
+  big_loop<NI, BLOCKS>(smem, a_at, b_base, b_at, a_sc, b_sc, (int)args.row_sc, KT, a_off, b_off, sa_off, sb_off, wave, acc, set_out)
     switch (ni) {
       case 4: MOE_BIG_LOOP(4); break;
       case 3: MOE_BIG_LOOP(3); break;
@@ -190,18 +221,7 @@ __global__ __launch_bounds__(256, 1) void matmul8_large_kernel(const Args8 args)
 #undef MOE_BIG_LOOP
   }
   // Lane (16 g + fr) has row fr of fragment i and columns 16 j + 4 g .. + 3 of the wave's 128: through LDS, 32 KB to a wave, to whole row pieces.
-  float bias[8][4];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int n = nw + 16 * j + 4 * g;
-    u32x2 w = {0, 0};
-    if (p.bias && n < N) w = *reinterpret_cast<const u32x2*>((const uint16_t*)p.bias + (int64_t)e * N + n);
-    bias[j][0] = __uint_as_float(w.x << 16);
-    bias[j][1] = __uint_as_float(w.x & 0xffff0000u);
-    bias[j][2] = __uint_as_float(w.y << 16);
-    bias[j][3] = __uint_as_float(w.y & 0xffff0000u);
-  }
-  __syncthreads();                                                  // every wave is done with the stages
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");          // every wave is done with the stages, and nothing is on its way into them
   char* own = smem + wave * 32768;
   const int64_t blocks = args.out_row8 / kBlock8, nb = nw / kBlock8;
 #pragma unroll
@@ -213,7 +233,7 @@ __global__ __launch_bounds__(256, 1) void matmul8_large_kernel(const Args8 args)
     for (int j = 0; j < 8; ++j)
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        v[j][c] = acc[i][j][c] + bias[j][c];
+        v[j][c] = acc[i][j][c];
         if (ACT >= 0) v[j][c] = apply_act(v[j][c], ACT);
         if (OUT8 && nw + 16 * j + 4 * g >= N) v[j][c] = 0.f;        // N is a multiple of 8
       }
@@ -246,28 +266,33 @@ __global__ __launch_bounds__(256, 1) void matmul8_large_kernel(const Args8 args)
     }
   }
   // stores of 8 rows x 128 bytes
-  if constexpr (!OUT8) {
-    uint16_t* oute = (uint16_t*)p.out + ((int64_t)e * p.C + m0) * N;
-#pragma unroll 2
-    for (int it = 0; it < 4 * ni; ++it) {
-      const int r = it * 8 + (lane >> 3), c = (lane & 7) ^ (r & 7);
-      const int row = ((r >> 5) * 2 + wm) * 32 + (r & 31);
+  auto store = [&](auto STREAM) {
+    constexpr bool stream = decltype(STREAM)::value;
+    if constexpr (!OUT8) {
+      uint16_t* oute = (uint16_t*)p.out + ((int64_t)e * p.C + m0) * N;
+#pragma unroll 4
+      for (int it = 0; it < 4 * ni; ++it) {
+        const int r = it * 8 + (lane >> 3), c = (lane & 7) ^ (r & 7);
+        const int row = ((r >> 5) * 2 + wm) * 32 + (r & 31);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const u32x4 w = *LDS_PTR(u32x4, own + h * 16384 + r * 128 + ((lane & 7) << 4));
-        const int n = nw + h * 64 + c * 8;
-        if (row < live && n < N) *reinterpret_cast<u32x4*>(oute + (int64_t)row * N + n) = w;
+        for (int half = 0; half < 2; ++half) {
+          const u32x4 w = *LDS_PTR(u32x4, own + half * 16384 + r * 128 + ((lane & 7) << 4));
+          const int n = nw + half * 64 + c * 8;
+          if (row < live && n < N) store16<stream>(oute + (int64_t)row * N + n, w);
+        }
+      }
+    } else {
+      uint8_t* oute = (uint8_t*)p.out8 + ((int64_t)e * p.C + m0) * args.out_row8;
+#pragma unroll 4
+      for (int it = 0; it < 4 * ni; ++it) {
+        const int r = it * 8 + (lane >> 3), c = (lane & 7) ^ (r & 7);
+        const int row = ((r >> 5) * 2 + wm) * 32 + (r & 31);
+        const u32x4 w = *LDS_PTR(u32x4, own + r * 128 + ((lane & 7) << 4));
+        const int n = nw + c * 16;
+        if (row < live && n < args.out_row8) store16<stream>(oute + (int64_t)row * args.out_row8 + n, w);
       }
     }
-  } else {
-    uint8_t* oute = (uint8_t*)p.out8 + ((int64_t)e * p.C + m0) * args.out_row8;
-#pragma unroll 4
-    for (int it = 0; it < 4 * ni; ++it) {
-      const int r = it * 8 + (lane >> 3), c = (lane & 7) ^ (r & 7);
-      const int row = ((r >> 5) * 2 + wm) * 32 + (r & 31);
-      const u32x4 w = *LDS_PTR(u32x4, own + r * 128 + ((lane & 7) << 4));
-      const int n = nw + c * 16;
-      if (row < live && n < args.out_row8) *reinterpret_cast<u32x4*>(oute + (int64_t)row * args.out_row8 + n) = w;
-    }
-  }
+  };
+  if (args.stream) store(std::true_type{});
+  else store(std::false_type{});
 }
