@@ -9,6 +9,7 @@
 // the values widened to bf16, which holds them all, exponent included: 1e-7, at less than half the rate.
 #include "block8.h"
 #include "ffn_device.h"
+#include "matmul8_rules.h"
 
 namespace moe {
 namespace {
@@ -34,209 +35,221 @@ struct Args8 {
   bool stream;                    // the large tile's results are not kept in the caches
 };
 
-// BM x BN to a block of WM x WN waves; NS stages of a K-step in LDS.  LDS: rows of 128 bytes, 16-byte piece g of row r at g ^ (r / 2) % 8.
-template <int BM, int BN, int WM, int WN, int NS, bool EXACT>
-__global__ __launch_bounds__(256) void matmul8_kernel(const Args8 a) {
-  constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 16, TN = WTN / 16;
-  constexpr int LA = BM / 32, LB = BN / 32, STAGE = (BM + BN) * kBlock8;
-  static_assert(WM * WN == 4 && BN % kBlock8 == 0 && NS * STAGE <= 163840, "four waves, whole blocks of the output format, stages that fit a unit");
-  __shared__ __attribute__((aligned(1024))) char smem[NS * STAGE];
+// The exponents of up to 64 K-steps in LDS, [word of four][row of A, then of B]: loads for them in the loop would hold up the direct loads' waits, which count in order, by all the way
+// from memory.
+constexpr int kScaleWords = 16;
+
+// 128 x 128 to a block of four waves, 64 x 64 each; two blocks share a unit, one's products cover the other's waits.  Two stages of a K-step in LDS: rows of 128 bytes, 16-byte piece g of row r
+// at g ^ (r / 2) % 8.  Fragments whose rows are all past the expert's fill are skipped.
+// EXACT: fp32 results.  ACT: of 8-bit results; others apply p.act in its full form.
+template <bool EXACT, bool OUT8, int ACT>
+__global__ __launch_bounds__(256, 2) void matmul8_kernel(const Args8 a) {
+  constexpr int kTile = 128, kStage = 2 * kTile * kBlock8, F = 4;
+  __shared__ __attribute__((aligned(1024))) char smem[2 * kStage + kScaleWords * 2 * kTile * 4];
   const Matmul8& p = a.p;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = wave / WN, wn = wave % WN;
+  const int wm = wave >> 1, wn = wave & 1, fr = lane & 15, g = lane >> 4;
   int e, mt, nt, rows;
   if (!a.plain) {
-    if (!find_tile<BM>(blockIdx.x, lane, (int)p.E, p.C, p.counts, a.NT, e, mt, nt, rows)) return;
+    if (!find_tile<kTile>(blockIdx.x, lane, (int)p.E, p.C, p.counts, a.NT, e, mt, nt, rows)) return;
   } else {
     e = blockIdx.y;
     mt = blockIdx.x / a.NT;
     nt = blockIdx.x % a.NT;
     rows = live_rows_of(e, p.C, p.counts);
   }
-  const int64_t m0 = (int64_t)mt * BM, n0 = (int64_t)nt * BN;
+  const int64_t m0 = (int64_t)mt * kTile, n0 = (int64_t)nt * kTile;
   if (m0 >= rows) return;
-  const int N = (int)p.N;
+  const int N = (int)p.N, live = (int)(rows - m0 < kTile ? rows - m0 : kTile);
+  const int own = (live - wm * 64 + 15) >> 4, frags = own < 0 ? 0 : (own < F ? own : F);       // of the wave's row fragments
   int KT = (int)(a.row8 / kBlock8);
   if (p.k_counts) {
     const int64_t c = p.k_counts[e];
     const int64_t most = c < p.K ? (c > 0 ? c : 0) : p.K;
     KT = (int)ceil_div(most, kBlock8);
   }
-  auto a_row = [&](int64_t r) -> int64_t {                          // rows past the fill repeat the last one (never stored)
-    r = m0 + r < rows ? m0 + r : rows - 1;
-    if (!p.gather) return (int64_t)e * p.C + r;
-    const int t = p.gather[(int64_t)e * p.C + r];
+  auto a_row = [&](int r) -> int64_t {                              // rows past the fill repeat the last one (never stored)
+    const int64_t c = (int64_t)e * p.C + (r < live ? m0 + r : rows - 1);
+    if (!p.gather) return c;
+    const int t = p.gather[c];
     return (unsigned)t < (uint64_t)p.gather_rows ? t : 0;
   };
   auto b_row = [&](int n) -> int64_t { return n0 + n < N ? n0 + n : N - 1; };      // so do columns past N
 
   // direct loads: wave w's load q brings 8 rows, lane l the piece l % 8 of row l / 8, from where the swizzle wants it
-  const char* a_at[LA];
-  uint32_t b_at[LB];
+  const char* a_at[4];
+  uint32_t b_at[4];
   const char* b_base = (const char*)p.B + (int64_t)e * N * a.row8;
 #pragma unroll
-  for (int q = 0; q < LA; ++q) {
-    const int r = (q * 4 + wave) * 8 + (lane >> 3);
-    a_at[q] = (const char*)p.A + a_row(r) * a.row8 + (((lane & 7) ^ ((r >> 1) & 7)) << 4);
-  }
-#pragma unroll
-  for (int q = 0; q < LB; ++q) {
-    const int r = (q * 4 + wave) * 8 + (lane >> 3);
-    b_at[q] = (uint32_t)(b_row(r) * a.row8 + (((lane & 7) ^ ((r >> 1) & 7)) << 4));
+  for (int q = 0; q < 4; ++q) {
+    const int r = (q * 4 + wave) * 8 + (lane >> 3), piece = ((lane & 7) ^ ((r >> 1) & 7)) << 4;
+    a_at[q] = (const char*)p.A + a_row(r) * a.row8 + piece;
+    b_at[q] = (uint32_t)(b_row(r) * a.row8 + piece);
   }
   const uint32_t smem_addr = (uint32_t)(uintptr_t)LDS_PTR(char, smem);
   auto load_step = [&](int kt) {
-    const uint32_t to = smem_addr + (kt % NS) * STAGE + wave * 1024;
+    const uint32_t to = smem_addr + (kt & 1) * kStage + wave * 1024;
     const char* b_src = b_base + (int64_t)kt * kBlock8;
 #pragma unroll
-    for (int q = 0; q < LA; ++q) global_to_lds_16(a_at[q] + (int64_t)kt * kBlock8, to + q * 4096);
+    for (int q = 0; q < 4; ++q)
+      if (q * 32 < live) global_to_lds_16(a_at[q] + (int64_t)kt * kBlock8, to + q * 4096);
 #pragma unroll
-    for (int q = 0; q < LB; ++q) global_to_lds_16(b_src, b_at[q], to + BM * kBlock8 + q * 4096);
+    for (int q = 0; q < 4; ++q) global_to_lds_16(b_src, b_at[q], to + kTile * kBlock8 + q * 4096);
   };
-  // exponents: a word for four K-steps, of the fragment row that the lane holds
-  const uint32_t* a_sc[TM];
-  const uint32_t* b_sc[TN];
-  const int fr = lane & 15, g = lane >> 4;
-#pragma unroll
-  for (int i = 0; i < TM; ++i) a_sc[i] = (const uint32_t*)(p.A_scales + a_row(wm * WTM + i * 16 + fr) * a.row_sc);
-#pragma unroll
-  for (int j = 0; j < TN; ++j) {
-    const int64_t n = b_row(wn * WTN + j * 16 + fr);
-    b_sc[j] = (const uint32_t*)(p.B_scales + (p.b_blocks ? (int64_t)e * ceil_div(N, kBlock8) + n / kBlock8 : (int64_t)e * N + n) * a.row_sc);
+  // thread t has row t of A, or column t - 128 of B
+  const uint8_t* sc_at;
+  if (threadIdx.x < kTile) {
+    sc_at = p.A_scales + a_row(threadIdx.x) * a.row_sc;
+  } else {
+    const int64_t n = b_row(threadIdx.x - kTile);
+    sc_at = p.B_scales + (p.b_blocks ? (int64_t)e * ceil_div(N, kBlock8) + n / kBlock8 : (int64_t)e * N + n) * a.row_sc;
   }
-  f32x4 acc[TM][TN];
+  auto load_scales = [&](int first) {                               // of the K-steps from `first`, a multiple of 64
+    const int left = (int)(a.row_sc - first) / 4, words = left < kScaleWords ? left : kScaleWords;
+    for (int w = 0; w < words; ++w) global_to_lds_4(sc_at + first + 4 * w, smem_addr + 2 * kStage + w * 1024 + wave * 256);
+  };
+  f32x4 acc[F][F];
+  if (KT > 0) {
+    load_scales(0);
+    load_step(0);
+  }
 #pragma unroll
-  for (int i = 0; i < TM; ++i)
+  for (int j = 0; j < F; ++j) {
+    const int64_t n = n0 + wn * 64 + j * 16 + 4 * g;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (p.bias && n < N) {
+      const int64_t at = (int64_t)e * N + n;
+      if (p.dtype == MOE_F32) v = *reinterpret_cast<const f32x4*>((const float*)p.bias + at);
+      else {
+        const u32x2 w = *reinterpret_cast<const u32x2*>((const uint16_t*)p.bias + at);
+        v = f32x4{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u)};
+      }
+    }
 #pragma unroll
-    for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  uint32_t sa[TM], sb[TN];
-#pragma unroll
-  for (int t = 0; t < NS - 1; ++t) if (t < KT) load_step(t);
+    for (int i = 0; i < F; ++i) acc[i][j] = v;
+  }
   for (int kt = 0; kt < KT; ++kt) {
-    if (kt % 4 == 0) {
-#pragma unroll
-      for (int i = 0; i < TM; ++i) sa[i] = a_sc[i][kt / 4];
-#pragma unroll
-      for (int j = 0; j < TN; ++j) sb[j] = b_sc[j][kt / 4];
+    if (kt > 0 && kt % (4 * kScaleWords) == 0) {
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      load_scales(kt);
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (kt + NS - 1 < KT) load_step(kt + NS - 1);
-    const char* as = smem + (kt % NS) * STAGE + wm * WTM * kBlock8;
-    const char* bs = smem + (kt % NS) * STAGE + (BM + wn * WTN) * kBlock8;
+    if (kt + 1 < KT) load_step(kt + 1);
+    const char* as = smem + (kt & 1) * kStage + wm * 64 * kBlock8;
+    const char* bs = smem + (kt & 1) * kStage + (kTile + wn * 64) * kBlock8;
+    const char* sc = smem + 2 * kStage + (kt >> 2 & (kScaleWords - 1)) * 1024 + (kt & 3) + fr * 4;
     auto fragment = [&](const char* at, int i) -> i32x8 {
-      const int sw = ((i * 16 + fr) >> 1) & 7;
+      const int sw = (fr >> 1) & 7;
       const u32x4 lo = *LDS_PTR(u32x4, at + (i * 16 + fr) * kBlock8 + ((g ^ sw) << 4));
       const u32x4 hi = *LDS_PTR(u32x4, at + (i * 16 + fr) * kBlock8 + (((g + 4) ^ sw) << 4));
       return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
     };
-    i32x8 av[TM];
+    i32x8 bv[F];
+    uint32_t sb[F];
 #pragma unroll
-    for (int i = 0; i < TM; ++i) av[i] = fragment(as, i);
+    for (int j = 0; j < F; ++j) {
+      bv[j] = fragment(bs, j);
+      sb[j] = *LDS_PTR(uint8_t, sc + (kTile + wn * 64 + j * 16) * 4);
+    }
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      const i32x8 bv = fragment(bs, j);
+    for (int i = 0; i < F; ++i) {
+      if (i >= frags) break;
+      const i32x8 av = fragment(as, i);
+      const uint32_t sa = *LDS_PTR(uint8_t, sc + (wm * 64 + i * 16) * 4);
 #pragma unroll
-      for (int i = 0; i < TM; ++i) {
+      for (int j = 0; j < F; ++j) {
         if constexpr (EXACT) {
 #pragma unroll
           for (int c = 0; c < 8; c += 2)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(bv[c], bv[c + 1], scale_value(sb[j] & 255)),
-                                                                widen8(av[i][c], av[i][c + 1], scale_value(sa[i] & 255)), acc[i][j], 0, 0, 0);
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(bv[j][c], bv[j][c + 1], scale_value(sb[j])), widen8(av[c], av[c + 1], scale_value(sa)), acc[i][j], 0, 0, 0);
         } else {
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bv, av[i], acc[i][j], 0, 0, 0, (int)sb[j], 0, (int)sa[i]);
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bv[j], av, acc[i][j], 0, 0, 0, (int)sb[j], 0, (int)sa);
         }
       }
     }
-#pragma unroll
-    for (int i = 0; i < TM; ++i) sa[i] >>= 8;
-#pragma unroll
-    for (int j = 0; j < TN; ++j) sb[j] >>= 8;
   }
-  // epilogue: the lane has row 16 i + l % 16 and columns 16 j + 4 (l / 16) .. + 3 of its wave's part
+  // lane (16 g + fr) has row fr of fragment i and columns 16 j + 4 g .. + 3 of its wave's part
+  if constexpr (!OUT8) {
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
+    for (int i = 0; i < F; ++i) {
+      if (i >= frags) break;
+      const int r = wm * 64 + i * 16 + fr;
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      const int64_t n = n0 + wn * WTN + j * 16 + 4 * g;
+      for (int j = 0; j < F; ++j) {
+        const int64_t n = n0 + wn * 64 + j * 16 + 4 * g, at = ((int64_t)e * p.C + m0 + r) * N + n;
+        f32x4 v = acc[i][j];
+        if (p.act >= 0)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        float f = acc[i][j][v];
-        if (n >= N) f = 0.f;                                        // N is a multiple of 8
-        else {
-          if (p.bias) f += p.dtype == MOE_F32 ? ((const float*)p.bias)[(int64_t)e * N + n + v] : bf16_bits_to_f32(((const uint16_t*)p.bias)[(int64_t)e * N + n + v]);
-          if (p.act >= 0) f = apply_act(f, p.act);
-        }
-        acc[i][j][v] = f;
-      }
-    }
-  }
-  if (p.out) {
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const int64_t r = m0 + wm * WTM + i * 16 + fr;
-      if (r >= rows) continue;
-#pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        const int64_t n = n0 + wn * WTN + j * 16 + 4 * g;
-        if (n >= N) continue;
-        const int64_t at = ((int64_t)e * p.C + r) * N + n;
-        if (p.dtype == MOE_F32) *reinterpret_cast<f32x4*>((float*)p.out + at) = acc[i][j];
-        else *reinterpret_cast<uint2*>((uint16_t*)p.out + at) = make_uint2(pack_bf16x2(acc[i][j][0], acc[i][j][1]), pack_bf16x2(acc[i][j][2], acc[i][j][3]));
+          for (int c = 0; c < 4; ++c) v[c] = apply_act(v[c], p.act);
+        if (r >= live || n >= N) continue;                          // N is a multiple of 8
+        if (p.dtype == MOE_F32) *reinterpret_cast<f32x4*>((float*)p.out + at) = v;
+        else *reinterpret_cast<uint2*>((uint16_t*)p.out + at) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
       }
     }
     return;
   }
-  // 8-bit output: the block's largest magnitude over the wave's columns, then over the waves that share the block of 128
-  uint32_t* tops = (uint32_t*)smem;                                 // [BM][WN]
-  __syncthreads();
-  constexpr int WPB = kBlock8 > WTN ? kBlock8 / WTN : 1, BPW = WTN > kBlock8 ? WTN / kBlock8 : 1, JB = TN / BPW;
-  static_assert(BPW == 1, "a wave's columns lie in one block");
+  // 8-bit output: the block's largest magnitude over the wave's columns, then over the two waves that share the 128
+  uint32_t* tops = (uint32_t*)smem;                                 // [128][2]
+  __syncthreads();                                                  // every wave is done with the stages
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
+  for (int i = 0; i < F; ++i) {
+    if (i >= frags) break;
     uint32_t top = 0;
 #pragma unroll
-    for (int j = 0; j < JB; ++j)
+    for (int j = 0; j < F; ++j)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) top = max(top, magnitude_bits(acc[i][j][v]));
+      for (int c = 0; c < 4; ++c) {
+        float v = acc[i][j][c];
+        if constexpr (EXACT) v = p.act >= 0 ? apply_act(v, p.act) : v;
+        else v = act8<ACT>(v);
+        if (n0 + wn * 64 + j * 16 + 4 * g >= N) v = 0.f;
+        acc[i][j][c] = v;
+        top = max(top, magnitude_bits(v));
+      }
     top = max(top, (uint32_t)__shfl_xor((int)top, 16));
     top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-    if (g == 0) tops[(wm * WTM + i * 16 + fr) * WN + wn] = top;
+    if (g == 0) tops[(wm * 64 + i * 16 + fr) * 2 + wn] = top;
   }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    const int rl = wm * WTM + i * 16 + fr;
-    const int64_t r = m0 + rl;
-    uint32_t top = 0;
+  for (int i = 0; i < F; ++i) {
+    if (i >= frags) break;
+    const int r = wm * 64 + i * 16 + fr;
+    const uint32_t sc = scale_of_amax(max(tops[2 * r], tops[2 * r + 1]));
+    if (r >= live) continue;
+    const int64_t row = (int64_t)e * p.C + m0 + r;
 #pragma unroll
-    for (int w = 0; w < WPB; ++w) top = max(top, tops[rl * WN + wn / WPB * WPB + w]);
-    const uint32_t sc = scale_of_amax(top);
-    if (r >= rows) continue;
-    const int64_t row = (int64_t)e * p.C + r;
-#pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      const int64_t n = n0 + wn * WTN + j * 16 + 4 * g;
-      if (n < a.out_row8) *reinterpret_cast<uint32_t*>((uint8_t*)p.out8 + row * a.out_row8 + n) = pack8x4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3], sc);
+    for (int j = 0; j < F; ++j) {
+      const int64_t n = n0 + wn * 64 + j * 16 + 4 * g;              // the block of 128 exists as a whole
+      *reinterpret_cast<uint32_t*>((uint8_t*)p.out8 + row * a.out_row8 + n) = pack8x4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3], sc);
     }
-    const int64_t nb = (n0 + wn * WTN) / kBlock8;
-    if (wn % WPB == 0 && g == 0) {
-      const int64_t blocks = a.out_row8 / kBlock8;
-      if (nb < blocks) p.out8_scales[row * a.out_row_sc + nb] = (uint8_t)sc;
-      if (nb == blocks - 1) for (int64_t b = blocks; b < a.out_row_sc; ++b) p.out8_scales[row * a.out_row_sc + b] = (uint8_t)kScaleOne;
+    if (wn == 0 && g == 0) {
+      uint8_t* to = p.out8_scales + row * a.out_row_sc;
+      to[nt] = (uint8_t)sc;
+      if (nt == a.NT - 1)
+        for (int64_t b = a.NT; b < a.out_row_sc; ++b) to[b] = (uint8_t)kScaleOne;
     }
   }
 }
 
-template <int BM, int BN, int WM, int WN, int NS, bool EXACT>
-hipError_t launch_tile(const Matmul8& p, hipStream_t s) {
-  Args8 a = {p, row_bytes8(p.K), row_scales8(p.K), row_bytes8(p.N), row_scales8(p.N), (int)ceil_div(p.C, BM), (int)ceil_div(p.N, BN), 0, false};
+hipError_t launch_small(const Matmul8& p, hipStream_t s) {
+  constexpr int kTile = 128;
+  Args8 a = {p, row_bytes8(p.K), row_scales8(p.K), row_bytes8(p.N), row_scales8(p.N), (int)ceil_div(p.C, kTile), (int)ceil_div(p.N, kTile), 0, false};
   const int64_t all = p.E * p.C, total = p.counts && p.rows_hint ? (p.E * p.rows_hint < all ? p.E * p.rows_hint : all) : all;
-  int64_t blocks = tile_grid(a.NT, live_row_tiles(p.E, p.C, total, BM));
+  int64_t blocks = tile_grid(a.NT, live_row_tiles(p.E, p.C, total, kTile));
   a.plain = p.E > kMaxExperts || blocks >= kMaxBlocks;
   if (a.plain) blocks = (int64_t)a.MT * a.NT;
   if (blocks >= kMaxBlocks) return hipErrorInvalidValue;
-  matmul8_kernel<BM, BN, WM, WN, NS, EXACT><<<dim3((unsigned)blocks, a.plain ? (unsigned)p.E : 1), dim3(256), 0, s>>>(a);
+  const dim3 grid((unsigned)blocks, a.plain ? (unsigned)p.E : 1), block(256);
+#define MOE_SMALL8(EXACT, OUT8, ACT) matmul8_kernel<EXACT, OUT8, ACT><<<grid, block, 0, s>>>(a)
+  if (p.out) { if (p.dtype == MOE_F32) MOE_SMALL8(true, false, -1); else MOE_SMALL8(false, false, -1); }
+  else if (p.dtype == MOE_F32) MOE_SMALL8(true, true, -1);
+  else if (p.act < 0) MOE_SMALL8(false, true, -1);
+  else if (p.act == MOE_ACT_RELU) MOE_SMALL8(false, true, MOE_ACT_RELU);
+  else if (p.act == MOE_ACT_GELU) MOE_SMALL8(false, true, MOE_ACT_GELU);
+  else MOE_SMALL8(false, true, MOE_ACT_SILU);
+#undef MOE_SMALL8
   return hipGetLastError();
 }
 
@@ -273,8 +286,9 @@ hipError_t launch_large(const Matmul8& p, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_matmul8(const Matmul8& p, hipStream_t s) {
-  if (large_covers(p) && p.C >= 512 && p.N >= 256) return launch_large(p, s);
-  return p.dtype == MOE_F32 ? launch_tile<128, 128, 2, 2, 2, true>(p, s) : launch_tile<128, 128, 2, 2, 2, false>(p, s);
+  const int64_t rows = p.counts && p.rows_hint > 0 && p.rows_hint < p.C ? p.rows_hint : p.C;
+  if (large_covers(p) && matmul8_takes_large_tile(p.E, (double)rows, p.K, p.N)) return launch_large(p, s);
+  return launch_small(p, s);
 }
 
 }  // namespace moe

@@ -7,8 +7,7 @@
 // the next first half of A.  Its direct loads go out between the second half's products: the stage that they fill has been read by every wave at the barrier.
 //
 // The bodies have no branches: with conditions around the loads, or one that a product's result lives across, the compiler moved accumulators about at every one (hundreds of moves a
-// K-step).  The exponents of up to 64 K-steps are brought into LDS before the first of them: loads that went out for them in between came all the way from memory before the K-step's own
-// counted as landed (8192^3 2680 -> 2950 TFLOP/s).
+// K-step).  The exponents are in LDS before the first K-step (fetched in the loop, every four: 8192^3 2680 TFLOP/s instead of 2950).
 //
 // Measured: 8192^3 371 us = 2.96 PFLOP/s (register-only products: 3.9); 8 experts x 4096 rows, 2048 x 2048 120 us = 2.28, K = 4096 203 us = 2.70.  With four tiles to a unit, a
 // K-step takes 2400 cycles; beside them a tile has 2500 until its first loads go out, 3000 to 5000 (cold operands) until they land, and 8500 for its results.  Tried and not kept: rings of
@@ -18,7 +17,7 @@
 namespace {
 
 constexpr int kBig = 256, kBigStage = 2 * kBig * kBlock8;           // 64 KB
-constexpr int kScaleWords = 16, kScaleBytes = kScaleWords * 2 * kBig * 4;    // words of four exponents of A's and B's rows: K = 8192; 32 KB
+constexpr int kScaleBytes = kScaleWords * 2 * kBig * 4;             // 32 KB
 
 // The body has no branch but the one around the exponents' fetch: past the reduction's end the direct loads bring the last K-step again and the reads what nobody uses.  With
 // conditions around them the compiler moved accumulators about at every one (hundreds of moves and spills a K-step).
@@ -234,7 +233,7 @@ __global__ __launch_bounds__(256, 1) void matmul8_large_kernel(const Args8 args)
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         v[j][c] = acc[i][j][c];
-        if (ACT >= 0) v[j][c] = apply_act(v[j][c], ACT);
+        v[j][c] = act8<ACT>(v[j][c]);
         if (OUT8 && nw + 16 * j + 4 * g >= N) v[j][c] = 0.f;        // N is a multiple of 8
       }
     const int r = i * 16 + fr;
