@@ -11,7 +11,7 @@
 namespace moe {
 
 constexpr int kBlock8 = 128;
-constexpr uint32_t kScaleOne = 127, kScaleNaN = 255, kNaN8 = 0x7f7f7f7fu;
+constexpr uint32_t kScaleOne = 127, kScaleNaN = 255;
 
 static inline __host__ __device__ int64_t row_bytes8(int64_t K) { return ceil_div(K, kBlock8) * kBlock8; }
 static inline __host__ __device__ int64_t row_scales8(int64_t K) { return ceil_div(ceil_div(K, kBlock8), 4) * 4; }
@@ -23,12 +23,12 @@ __device__ __forceinline__ uint32_t scale_of_amax(uint32_t amax_bits) {
   const int e = (int)(amax_bits >> 23) - 8 + ((amax_bits & 0x7fffffu) > 0x600000u ? 1 : 0);   // 448 = 1.75 * 2^8
   return e < 1 ? 1u : (uint32_t)e;
 }
-__device__ __forceinline__ float inverse_scale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }   // 2^-e; byte <= 247
+__device__ __forceinline__ float inverse_scale(uint32_t byte) {     // 2^-e; the finite ones are at most 247
+  return __uint_as_float(byte == kScaleNaN ? 0x7fc00000u : (254u - byte) << 23);
+}
 
-// four values -> four e4m3 bytes, round to nearest even
-__device__ __forceinline__ uint32_t pack8x4(float a, float b, float c, float d, uint32_t scale) {
-  if (scale == kScaleNaN) return kNaN8;
-  const float m = inverse_scale(scale);
+// four values times m = inverse_scale(their block's exponent) -> four e4m3 bytes, round to nearest even
+__device__ __forceinline__ uint32_t pack8x4(float a, float b, float c, float d, float m) {
   int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * m, b * m, 0, false);
   w = __builtin_amdgcn_cvt_pk_fp8_f32(c * m, d * m, w, true);
   return (uint32_t)w;

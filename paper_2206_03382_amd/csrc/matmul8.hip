@@ -217,12 +217,13 @@ __global__ __launch_bounds__(256, 2) void matmul8_kernel(const Args8 a) {
     if (i >= frags) break;
     const int r = wm * 64 + i * 16 + fr;
     const uint32_t sc = scale_of_amax(max(tops[2 * r], tops[2 * r + 1]));
+    const float inverse = inverse_scale(sc);
     if (r >= live) continue;
     const int64_t row = (int64_t)e * p.C + m0 + r;
 #pragma unroll
     for (int j = 0; j < F; ++j) {
       const int64_t n = n0 + wn * 64 + j * 16 + 4 * g;              // the block of 128 exists as a whole
-      *reinterpret_cast<uint32_t*>((uint8_t*)p.out8 + row * a.out_row8 + n) = pack8x4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3], sc);
+      *reinterpret_cast<uint32_t*>((uint8_t*)p.out8 + row * a.out_row8 + n) = pack8x4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3], inverse);
     }
     if (wn == 0 && g == 0) {
       uint8_t* to = p.out8_scales + row * a.out_row_sc;

@@ -253,8 +253,9 @@ __global__ __launch_bounds__(256, 1) void matmul8_large_kernel(const Args8 args)
       top = max(top, (uint32_t)__shfl_xor((int)top, 16));
       top = max(top, (uint32_t)__shfl_xor((int)top, 32));
       const uint32_t sc = scale_of_amax(top);
+      const float inverse = inverse_scale(sc);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) *LDS_PTR(uint32_t, own + r * 128 + ((j ^ (r & 7)) << 4) + 4 * g) = pack8x4(v[j][0], v[j][1], v[j][2], v[j][3], sc);
+      for (int j = 0; j < 8; ++j) *LDS_PTR(uint32_t, own + r * 128 + ((j ^ (r & 7)) << 4) + 4 * g) = pack8x4(v[j][0], v[j][1], v[j][2], v[j][3], inverse);
       const int row = ((i >> 1) * 2 + wm) * 32 + (i & 1) * 16 + fr;
       if (g == 0 && row < live && nb < blocks) {
         uint8_t* to = p.out8_scales + ((int64_t)e * p.C + m0 + row) * args.out_row_sc;

@@ -94,10 +94,11 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_norm_kernel(con
     top = max16(top);
     if (N == 4) top = max(top, (uint32_t)__shfl_xor((int)top, 16));
     const uint32_t scale = scale_of_amax(top);
+    const float inverse = inverse_scale(scale);
     if (p * N < row8) {
       uint8_t* to = q + row * row8 + p * N;
-      const uint32_t lo = pack8x4(v[i][0], v[i][1], v[i][2], v[i][3], scale);
-      if constexpr (N == 8) *reinterpret_cast<uint2*>(to) = make_uint2(lo, pack8x4(v[i][4], v[i][5], v[i][6], v[i][7], scale));
+      const uint32_t lo = pack8x4(v[i][0], v[i][1], v[i][2], v[i][3], inverse);
+      if constexpr (N == 8) *reinterpret_cast<uint2*>(to) = make_uint2(lo, pack8x4(v[i][4], v[i][5], v[i][6], v[i][7], inverse));
       else *reinterpret_cast<uint32_t*>(to) = lo;
       if (p * N % kBlock8 == 0) scales[row * rows_scales + p * N / kBlock8] = (uint8_t)scale;
     }

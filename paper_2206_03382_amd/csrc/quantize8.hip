@@ -5,6 +5,12 @@
 namespace moe {
 namespace {
 
+__device__ __forceinline__ int live_rows(int64_t e, int R, const int32_t* counts) {
+  if (!counts) return R;
+  const int c = counts[e];
+  return c < R ? (c > 0 ? c : 0) : R;
+}
+
 template <typename ET> __device__ __forceinline__ void load8(const ET* p, float (&v)[8]);
 template <> __device__ __forceinline__ void load8<uint16_t>(const uint16_t* p, float (&v)[8]) { Vec16<uint16_t>::unpack(load_stream(reinterpret_cast<const uint4*>(p)), v); }
 template <> __device__ __forceinline__ void load8<float>(const float* p, float (&v)[8]) {
@@ -25,112 +31,108 @@ template <> __device__ __forceinline__ void load8<float>(const float* p, float (
 // BLOCKS: one exponent for the tile; else one for each row and column of it.  Rows past an expert's fill count as zero: the transposed form has
 // zeros there up to the end of its block; tiles that lie past it altogether are left alone.
 template <typename ET, bool BLOCKS>
-__global__ __launch_bounds__(256) void quantize8_kernel(const ET* __restrict__ src, const int32_t* __restrict__ counts, int64_t R, int64_t K,
+__global__ __launch_bounds__(256, 4) void quantize8_kernel(const ET* __restrict__ src, const int32_t* __restrict__ counts, int R, int K, int tiles_k,
                                                         uint8_t* __restrict__ q, uint8_t* __restrict__ scales, uint8_t* __restrict__ qt,
-                                                        uint8_t* __restrict__ scales_t, int64_t row8, int64_t row_sc, int64_t col8, int64_t col_sc) {
+                                                        uint8_t* __restrict__ scales_t, int row8, int row_sc, int col8, int col_sc) {
   __shared__ __attribute__((aligned(16))) uint8_t tile[kBlock8 * kBlock8];
-  __shared__ uint32_t tops[4][kBlock8];
-  const int64_t e = blockIdx.y, tiles_k = ceil_div(K, kBlock8), rb = blockIdx.x / tiles_k, kb = blockIdx.x % tiles_k;
-  int64_t rows = R;
-  if (counts) {
-    const int64_t c = counts[e];
-    rows = c < R ? (c > 0 ? c : 0) : R;
-  }
+  __shared__ uint32_t tops[16][kBlock8];
+  __shared__ uint8_t exponents[2][kBlock8];
+  const int64_t e = blockIdx.y;
+  const int rb = blockIdx.x / tiles_k, kb = blockIdx.x - rb * tiles_k;
+  const int rows = live_rows(e, R, counts);
   if (rb * kBlock8 >= rows) return;
   const int t = threadIdx.x, rg = t >> 4, cg = t & 15, wave = t >> 6;
-  const int64_t r0 = rb * kBlock8 + rg * 8, c0 = kb * kBlock8 + cg * 8;
+  const int r0 = rb * kBlock8 + rg * 8, c0 = kb * kBlock8 + cg * 8;
   float v[8][8];
+  if (r0 + 8 <= rows && c0 < K) {
+    const ET* at = src + (e * R + r0) * (int64_t)K + c0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 8; ++i) load8(at + (int64_t)i * K, v[i]);
+  } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
-    if (r0 + i < rows && c0 < K) load8(src + (e * R + r0 + i) * K + c0, v[i]);
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+      if (r0 + i < rows && c0 < K) load8(src + (e * R + r0 + i) * (int64_t)K + c0, v[i]);
+    }
   }
-  uint32_t row_scale[8], col_scale[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, magnitude_bits(v[i][j]));
-    row_scale[i] = max16(top);
-  }
+  // one row, or column, at a time: its largest magnitude, its exponent, its values (and for the tile's own exponent, that first)
+  uint32_t tile_scale = 0;
   if (BLOCKS) {
     uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, row_scale[i]);
-    top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = max(top, magnitude_bits(v[i][j]));
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
     if ((t & 63) == 0) tops[wave][0] = top;
     __syncthreads();
-    const uint32_t sc = scale_of_amax(max(max(tops[0][0], tops[1][0]), max(tops[2][0], tops[3][0])));
+    tile_scale = scale_of_amax(max(max(tops[0][0], tops[1][0]), max(tops[2][0], tops[3][0])));
+  }
+  if (q) {
+    uint8_t* to = q + (e * R + r0) * (int64_t)row8 + c0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) row_scale[i] = col_scale[i] = sc;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) row_scale[i] = scale_of_amax(row_scale[i]);
-    if (qt) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
+    for (int i = 0; i < 8; ++i) {
+      uint32_t sc = tile_scale;
+      if (!BLOCKS) {
         uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, magnitude_bits(v[i][j]));
-        top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-        if ((t & 63) < 16) tops[wave][cg * 8 + j] = top;
+        for (int j = 0; j < 8; ++j) top = max(top, magnitude_bits(v[i][j]));
+        sc = scale_of_amax(max16(top));
+        if (cg == 0) exponents[0][rg * 8 + i] = (uint8_t)sc;
       }
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int c = cg * 8 + j;
-        col_scale[j] = scale_of_amax(max(max(tops[0][c], tops[1][c]), max(tops[2][c], tops[3][c])));
-      }
-    }
-  }
-  const bool last_k = kb == tiles_k - 1, last_r = (rb + 1) * kBlock8 >= R;
-  if (q) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int64_t r = r0 + i;
-      if (r >= rows) break;
+      const float m = inverse_scale(sc);
       uint2 w;
-      w.x = pack8x4(v[i][0], v[i][1], v[i][2], v[i][3], row_scale[i]);
-      w.y = pack8x4(v[i][4], v[i][5], v[i][6], v[i][7], row_scale[i]);
-      *reinterpret_cast<uint2*>(q + (e * R + r) * row8 + c0) = w;
-    }
-    // exponents: of the thread's rows, or of the tile; the last tile of a row pads it
-    uint8_t* to = scales + (BLOCKS ? (e * ceil_div(R, kBlock8) + rb) : e * R + r0) * row_sc;
-    const int own = BLOCKS ? (t == 0) : (cg == 0 ? (int)(rows - r0 < 8 ? rows - r0 : 8) : 0);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (i >= own) break;
-      to[i * row_sc + kb] = (uint8_t)row_scale[i];
-      if (last_k) for (int64_t p = kb + 1; p < row_sc; ++p) to[i * row_sc + p] = (uint8_t)kScaleOne;
+      w.x = pack8x4(v[i][0], v[i][1], v[i][2], v[i][3], m);
+      w.y = pack8x4(v[i][4], v[i][5], v[i][6], v[i][7], m);
+      if (r0 + i < rows) *reinterpret_cast<uint2*>(to + (int64_t)i * row8) = w;
     }
   }
-  if (!qt) return;
-  {
-    uint8_t* to = scales_t + (BLOCKS ? (e * ceil_div(K, kBlock8) + kb) : e * K + c0) * col_sc;
-    const int own = BLOCKS ? (t == 0) : (rg == 0 && c0 < K ? 8 : 0);
+  if (qt && !BLOCKS) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      if (j >= own) break;
-      to[j * col_sc + rb] = (uint8_t)col_scale[j];
-      if (last_r) for (int64_t p = rb + 1; p < col_sc; ++p) to[j * col_sc + p] = (uint8_t)kScaleOne;
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = max(top, magnitude_bits(v[i][j]));
+      tops[rg][cg * 8 + j] = top;
+    }
+    __syncthreads();
+    if (t < kBlock8) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = max(top, tops[i][t]);
+      exponents[1][t] = (uint8_t)scale_of_amax(top);
     }
   }
+  if (!BLOCKS) __syncthreads();
+  if (qt) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    uint2 w;
-    w.x = pack8x4(v[0][j], v[1][j], v[2][j], v[3][j], col_scale[j]);
-    w.y = pack8x4(v[4][j], v[5][j], v[6][j], v[7][j], col_scale[j]);
-    *reinterpret_cast<uint2*>(tile + (cg * 8 + j) * kBlock8 + (((rg >> 1) ^ (cg & 7)) << 4) + (rg & 1) * 8) = w;
+    for (int j = 0; j < 8; ++j) {
+      const float m = inverse_scale(BLOCKS ? tile_scale : exponents[1][cg * 8 + j]);
+      uint2 w;
+      w.x = pack8x4(v[0][j], v[1][j], v[2][j], v[3][j], m);
+      w.y = pack8x4(v[4][j], v[5][j], v[6][j], v[7][j], m);
+      *reinterpret_cast<uint2*>(tile + (cg * 8 + j) * kBlock8 + (((rg >> 1) ^ (cg & 7)) << 4) + (rg & 1) * 8) = w;
+    }
   }
+  // exponents: the tile's from one thread, or row t's and column t - 128's from thread t; the last tile of a row of them pads it
+  const bool second = t >= kBlock8;
+  const int i = t & (kBlock8 - 1), at = second ? rb : kb, pitch = second ? col_sc : row_sc, line = (second ? kb : rb) * kBlock8 + i;
+  uint8_t* sc = second ? scales_t : scales;
+  if (sc && (BLOCKS ? i == 0 : line < (second ? K : rows))) {
+    sc += (BLOCKS ? e * (((second ? K : R) + kBlock8 - 1) / kBlock8) + line / kBlock8 : e * (second ? K : R) + line) * (int64_t)pitch + at;
+    sc[0] = (uint8_t)(BLOCKS ? tile_scale : exponents[second][i]);
+    if (at == (second ? (R + kBlock8 - 1) / kBlock8 : tiles_k) - 1)
+      for (int p = 1; p < pitch - at; ++p) sc[p] = (uint8_t)kScaleOne;
+  }
+  if (!qt) return;
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int c = i * 32 + (t >> 3), p = t & 7;
-    const int64_t col = kb * kBlock8 + c;
-    if (col < K) *reinterpret_cast<uint4*>(qt + (e * K + col) * col8 + rb * kBlock8 + p * 16) = *reinterpret_cast<const uint4*>(tile + c * kBlock8 + ((p ^ ((c >> 3) & 7)) << 4));
+  for (int s = 0; s < 4; ++s) {
+    const int c = s * 32 + (t >> 3), p = t & 7;
+    const int col = kb * kBlock8 + c;
+    if (col < K) *reinterpret_cast<uint4*>(qt + (e * K + col) * (int64_t)col8 + rb * kBlock8 + p * 16) = *reinterpret_cast<const uint4*>(tile + c * kBlock8 + ((p ^ ((c >> 3) & 7)) << 4));
   }
 }
 
@@ -175,8 +177,8 @@ hipError_t launch_quantize8(const void* src, int dtype, const int32_t* counts, i
                             uint8_t* scales, void* qt, uint8_t* scales_t, hipStream_t s) {
   const dim3 grid((unsigned)(ceil_div(K, kBlock8) * ceil_div(R, kBlock8)), (unsigned)E);
 #define MOE_QUANTIZE(ET, B)                                                                                                           \
-  quantize8_kernel<ET, B><<<grid, dim3(256), 0, s>>>((const ET*)src, counts, R, K, (uint8_t*)q, scales, (uint8_t*)qt, scales_t, row_bytes8(K), \
-                                                     row_scales8(K), row_bytes8(R), row_scales8(R))
+  quantize8_kernel<ET, B><<<grid, dim3(256), 0, s>>>((const ET*)src, counts, (int)R, (int)K, (int)ceil_div(K, kBlock8), (uint8_t*)q, scales, (uint8_t*)qt, scales_t, \
+                                                     (int)row_bytes8(K), (int)row_scales8(K), (int)row_bytes8(R), (int)row_scales8(R))
   if (dtype == MOE_F32) { if (blocks) MOE_QUANTIZE(float, true); else MOE_QUANTIZE(float, false); }
   else { if (blocks) MOE_QUANTIZE(uint16_t, true); else MOE_QUANTIZE(uint16_t, false); }
 #undef MOE_QUANTIZE
