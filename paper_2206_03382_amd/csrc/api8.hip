@@ -61,7 +61,7 @@ Layer8Workspace layer8_layout(int64_t T, int64_t M, int64_t H, int64_t E, int k,
 }
 
 struct FewWorkspace {
-  size_t logits, idx, loc, gate_w, counts, gate_ws, logit_parts, plan, hidden, partial, arrived, total;
+  size_t logits, idx, loc, gate_w, counts, plan, hidden, partial, arrived, total;
 };
 
 FewWorkspace few_layout(int64_t T, int64_t M, int64_t H, int64_t E, int k, int dtype) {
@@ -73,9 +73,6 @@ FewWorkspace few_layout(int64_t T, int64_t M, int64_t H, int64_t E, int k, int d
   w.loc = take((size_t)T * k * 4);
   w.gate_w = take((size_t)T * k * 4);
   w.counts = take((size_t)E * 4);
-  const int slices = few_gate_slices(T, M, E, k);
-  w.gate_ws = take(slices > 0 ? 0 : moe_gate_route_workspace_bytes(T, M, E, k, dtype));
-  w.logit_parts = take((size_t)slices * T * E * 8);
   w.plan = take((size_t)(E < T * k ? E : T * k) * kFewPlan * 4);
   w.hidden = take((size_t)T * k * H * esize(dtype));
   w.partial = take((size_t)T * k * M * 4);
@@ -247,13 +244,8 @@ int moe_layer_forward_few(const void* x, const void* Wg, const float* gate_bias,
   gate_w = gate_w ? gate_w : (float*)(base + w.gate_w);
   counts = counts ? counts : (int32_t*)(base + w.counts);
   logits = logits ? logits : (float*)(base + w.logits);
-  const int slices = few_gate_slices(T, M, E, k);
-  if (slices == 0)
-    if (int st = moe_gate_route(x, Wg, gate_bias, dtype, T, M, E, k, C, normalize, logits, idx, gate_w, loc, counts, nullptr, base + w.gate_ws,
-                                moe_gate_route_workspace_bytes(T, M, E, k, dtype), stream))
-      return st;
-  const FewTokens p = {x, Wg, W1, b1, W2, b2, gate_bias, s1, s2, idx, loc, counts, gate_w, logits, T, M, H, E, C, k, act, dtype, normalize, slices,
-                       (double*)(base + w.logit_parts), (int32_t*)(base + w.plan), base + w.hidden, (float*)(base + w.partial),
+  const FewTokens p = {x, Wg, W1, b1, W2, b2, gate_bias, s1, s2, idx, loc, counts, gate_w, logits, T, M, H, E, C, k, act, dtype, normalize, false, 0, 0,
+                       (int32_t*)(base + w.plan), base + w.hidden, (float*)(base + w.partial),
                        (int32_t*)(base + w.arrived), out};
   return status_of(launch_few_tokens(p, (hipStream_t)stream));
 }

@@ -103,11 +103,12 @@ struct FewTokens {
   const void *x, *Wg, *W1, *b1, *W2, *b2;
   const float* gate_bias;
   const uint8_t *s1, *s2;         // 8-bit weights [E, N, row_bytes8(K)] (blocks of 128 x 128), or null: [E, K, N] in dtype
-  int32_t *idx, *loc, *counts;    // the gate's decisions: outputs if slices > 0, else idx is given
+  int32_t *idx, *loc, *counts;    // the gate's decisions: outputs
   float *gate_w, *logits;
   int64_t T, M, H, E, C;
-  int k, act, dtype, normalize, slices;      // slices: few_gate_slices
-  double* logit_parts;            // [slices, T, E]
+  int k, act, dtype, normalize;
+  bool planned;                   // set by launch_few_tokens, as are the next two
+  int expert_bits, token_bits;
   int32_t* plan;                  // [min(E, T k), kFewPlan]
   void* hidden;                   // [T k, H]
   float* partial;                 // [T k, M]
@@ -115,7 +116,6 @@ struct FewTokens {
   void* out;
 };
 constexpr int kFewPlan = 2 + MOE_FEW_MAX_TOKENS;
-int few_gate_slices(int64_t T, int64_t M, int64_t E, int k);
 size_t few_arrivals_bytes(int64_t M);
 hipError_t launch_few_tokens(const FewTokens& p, hipStream_t s);
 

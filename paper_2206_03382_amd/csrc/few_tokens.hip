@@ -1,7 +1,7 @@
 // The experts' feed-forward layer and the combine for a few tokens:
 //   hidden[p, :] = act(x[t] * W1[e] + b1[e])    for every kept choice p = (t, j) with e = idx[t, j];
 //   out[t, :] = sum over its kept choices j of gate_w[t, j] * (hidden[p] * W2[e] + b2[e]).
-// Reading the chosen experts' weights once is all the time there is (HBM bound), so each product is cut into units of one expert and 64 columns, a block
+// Reading the chosen experts' weights once is all the time there is (HBM bound), so each product is cut into units of one expert and 64 or 32 columns, a block
 // each: eight waves share the sum over k, every one with loads of several steps in flight, and meet in LDS.  The expert's rows, 16 to a tile, go
 // through the matrix cores together, whose 16 rows cost the same whether they are filled or not.
 #include "block8.h"
@@ -10,49 +10,51 @@
 namespace moe {
 namespace {
 
-constexpr int kFewWaves = 8, kFewColumns = 64, kFewRows = MOE_FEW_MAX_TOKENS;
-constexpr int kFewGateLogits = 1024, kFewPairs = MOE_FEW_MAX_TOKENS * 128;      // k * E <= 16384 and k <= E: at most 128 choices
+constexpr int kFewWaves = 8, kFewRows = MOE_FEW_MAX_TOKENS;
+constexpr int kFewArrival = 32;                                     // columns to an arrival counter, at least
+constexpr int kFewExperts = 512;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 
-// An operand's rows in the form the matrix cores take them, and a step of the weights.  Lane l = 16 g + i has row i of the tokens; which k and columns it
+// An operand's rows in the form the matrix cores take them, and a step of the weights of 16 C columns.  Lane l = 16 g + i has row i of the tokens; which k and columns it
 // has of the weights is the weights' layout:
-//   bf16 [K, N]   step of 32 k: rows k = 8 g .. + 7, columns 4 i .. + 3 in eight 8-byte loads (128 bytes of a row to 16 lanes); column c of all lanes is a
-//                 fragment, put together from halves of two loads at a time;
-//   fp32 [K, N]   step of 16 k: rows 4 g .. + 3, columns 4 i .. + 3 in four 16-byte loads; a component of a load is a fragment as it is;
-//   8 bit [N, K]  step of 64 k: of columns 16 f + i, the k from 16 g, widened to bf16 with the block's exponent.  fp32 tokens enter as three bf16
-//                 pieces, which hold their 24 bits.
-// The result's lane (16 g + i) has row i and 4 values v of fragment f: column 16 g + 4 v + f, or 16 f + 4 g + v where fragments are 16 columns next to each other.
+//   bf16 [K, N]   step of 32 k: rows k = 8 g .. + 7, columns C i .. + C - 1 in eight loads (C = 4: 128 bytes of a row to 16 lanes); column c of all lanes is a fragment, put together
+//                 from halves of two loads at a time;
+//   fp32 [K, N]   step of 16 k: rows 4 g .. + 3, columns C i .. in four loads; a component of a load is a fragment as it is;
+//   8 bit [N, K]  step of 64 k: of columns 16 c + i, the k from 16 g, widened to bf16 with the block's exponent.  fp32 tokens enter as three bf16 pieces, which hold their 24 bits.
+// The result's lane (16 g + i) has row i and 4 values v of fragment c: column 4 C g + C v + c, or 16 c + 4 g + v where fragments are 16 columns next to each other (kApart).
 // at(): where a lane's first piece of step 0 is; columns past N repeat the last ones, rows that do not exist the first one (neither is stored).  load() and
 // load_rows() take the k that exist: all of them but in the last step (TAIL), where the others are zero.
-template <typename ET, bool W8> struct Few;
+template <typename ET, bool W8, int C> struct Few;
 
-template <> struct Few<uint16_t, false> {
+template <int C> struct Few<uint16_t, false, C> {
   static constexpr int kStep = 32;
   static constexpr bool kApart = false;
+  static __device__ __forceinline__ int step(int wave, int j) { return wave + j * kFewWaves; }
+  static constexpr int depth(int rt) { return rt == 4 ? 3 : 4; }
+  typedef __attribute__((ext_vector_type(C / 2))) uint32_t Piece;
   struct At { uint32_t n; };
-  static constexpr int depth(int rt) { return rt == 1 ? 5 : (rt == 2 ? 4 : 3); }
-  struct Weights { u32x2 w[8]; };
+  struct Weights { Piece w[8]; };
   struct Rows { u32x4 x; };
   static __device__ __forceinline__ At at(int64_t n0, int64_t N, int64_t, int i, int g) {
-    const int64_t n = n0 + 4 * i < N ? n0 + 4 * i : N - 4;
+    const int64_t n = n0 + C * i < N ? n0 + C * i : N - C;
     return {(uint32_t)((8 * g * N + n) * 2)};
   }
   static __device__ __forceinline__ int64_t step_bytes(int64_t N) { return kStep * N * 2; }
   template <bool TAIL> static __device__ __forceinline__ void load(Weights& o, const char* W, const At& at, const uint8_t*, int64_t N, int, int left, int g) {
     if (TAIL && 8 * g >= left) {
-      for (int r = 0; r < 8; ++r) o.w[r] = u32x2{0, 0};
+      for (int r = 0; r < 8; ++r) o.w[r] = Piece(0);
       return;
     }
 #pragma unroll
-    for (int r = 0; r < 8; ++r) o.w[r] = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(W + r * N * 2 + at.n));
+    for (int r = 0; r < 8; ++r) o.w[r] = __builtin_nontemporal_load(reinterpret_cast<const Piece*>(W + r * N * 2 + at.n));
   }
   template <bool TAIL> static __device__ __forceinline__ void load_rows(Rows& o, const uint16_t* row, int left, int g) {
     if (TAIL && 8 * g >= left) o.x = u32x4{0, 0, 0, 0};
     else o.x = *reinterpret_cast<const u32x4*>(row + 8 * g);
   }
-  template <int RT> static __device__ __forceinline__ void multiply(const Weights& w, const Rows (&x)[RT], f32x4 (&acc)[RT][4]) {
+  template <int RT> static __device__ __forceinline__ void multiply(const Weights& w, const Rows (&x)[RT], f32x4 (&acc)[RT][C]) {
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
+    for (int c = 0; c < C; ++c) {
       u32x4 b;
 #pragma unroll
       for (int r = 0; r < 4; ++r) b[r] = __builtin_amdgcn_perm(w.w[2 * r + 1][c >> 1], w.w[2 * r][c >> 1], c & 1 ? 0x07060302u : 0x05040100u);
@@ -63,58 +65,61 @@ template <> struct Few<uint16_t, false> {
   }
 };
 
-template <> struct Few<float, false> {
+template <int C> struct Few<float, false, C> {
   static constexpr int kStep = 16;
   static constexpr bool kApart = false;
+  static __device__ __forceinline__ int step(int wave, int j) { return wave + j * kFewWaves; }
+  static constexpr int depth(int rt) { return C == 4 ? (rt == 1 ? 5 : (rt == 2 ? 4 : 3)) : (rt == 4 ? 4 : 6); }
+  typedef __attribute__((ext_vector_type(C))) float Piece;
   struct At { uint32_t n; };
-  static constexpr int depth(int rt) { return rt == 1 ? 5 : (rt == 2 ? 4 : 3); }
-  struct Weights { f32x4 w[4]; };
+  struct Weights { Piece w[4]; };
   struct Rows { f32x4 x; };
   static __device__ __forceinline__ At at(int64_t n0, int64_t N, int64_t, int i, int g) {
-    const int64_t n = n0 + 4 * i < N ? n0 + 4 * i : N - 4;
+    const int64_t n = n0 + C * i < N ? n0 + C * i : N - C;
     return {(uint32_t)((4 * g * N + n) * 4)};
   }
   static __device__ __forceinline__ int64_t step_bytes(int64_t N) { return kStep * N * 4; }
   template <bool TAIL> static __device__ __forceinline__ void load(Weights& o, const char* W, const At& at, const uint8_t*, int64_t N, int, int left, int g) {
     if (TAIL && 4 * g >= left) {
-      for (int r = 0; r < 4; ++r) o.w[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int r = 0; r < 4; ++r) o.w[r] = Piece(0.f);
       return;
     }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) o.w[r] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(W + r * N * 4 + at.n));
+    for (int r = 0; r < 4; ++r) o.w[r] = __builtin_nontemporal_load(reinterpret_cast<const Piece*>(W + r * N * 4 + at.n));
   }
   template <bool TAIL> static __device__ __forceinline__ void load_rows(Rows& o, const float* row, int left, int g) {
     if (TAIL && 4 * g >= left) o.x = f32x4{0.f, 0.f, 0.f, 0.f};
     else o.x = *reinterpret_cast<const f32x4*>(row + 4 * g);
   }
-  template <int RT> static __device__ __forceinline__ void multiply(const Weights& w, const Rows (&x)[RT], f32x4 (&acc)[RT][4]) {
+  template <int RT> static __device__ __forceinline__ void multiply(const Weights& w, const Rows (&x)[RT], f32x4 (&acc)[RT][C]) {
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
+      for (int c = 0; c < C; ++c)
 #pragma unroll
         for (int t = 0; t < RT; ++t) acc[t][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(w.w[r][c], x[t].x[r], acc[t][c], 0, 0, 0);
   }
 };
 
-template <typename ET> struct Few<ET, true> {
+template <typename ET, int C> struct Few<ET, true, C> {
   static constexpr int kStep = 64, kPieces = sizeof(ET) == 4 ? 3 : 1, kWords = sizeof(ET) / 2;
   static constexpr bool kApart = true;
-  static constexpr int depth(int rt) { return rt == 1 ? 4 : (rt == 2 ? 3 : (sizeof(ET) == 4 ? 1 : 2)); }
-  struct Weights { u32x4 w[4]; uint32_t exponent; };
+  static __device__ __forceinline__ int step(int wave, int j) { return 2 * (wave + (j >> 1) * kFewWaves) + (j & 1); }      // two make a line of 128 bytes
+  static constexpr int depth(int rt) { return sizeof(ET) == 4 ? (rt == 1 ? (C == 4 ? 1 : 3) : (rt == 2 ? 2 : 1)) : (rt == 1 ? (C == 4 ? 3 : 4) : (rt == 2 ? 3 : 2)); }
+  struct At { uint32_t n[C]; };
+  struct Weights { u32x4 w[C]; uint32_t exponent; };
   struct Rows { u32x4 x[2][kWords]; };                              // k from 16 g + 8 q
-  struct At { uint32_t n[4]; };
   static __device__ __forceinline__ At at(int64_t n0, int64_t N, int64_t row8, int i, int g) {
     At a;
 #pragma unroll
-    for (int f = 0; f < 4; ++f) a.n[f] = (uint32_t)((n0 + 16 * f + i < N ? n0 + 16 * f + i : N - 1) * row8 + 16 * g);
+    for (int c = 0; c < C; ++c) a.n[c] = (uint32_t)((n0 + 16 * c + i < N ? n0 + 16 * c + i : N - 1) * row8 + 16 * g);
     return a;
   }
   static __device__ __forceinline__ int64_t step_bytes(int64_t) { return kStep; }
   // rows of 8-bit values are padded to whole blocks with zeros
   template <bool TAIL> static __device__ __forceinline__ void load(Weights& o, const char* W, const At& at, const uint8_t* sc, int64_t, int step, int, int) {
 #pragma unroll
-    for (int f = 0; f < 4; ++f) o.w[f] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(W + at.n[f]));
+    for (int c = 0; c < C; ++c) o.w[c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(W + at.n[c]));
     o.exponent = sc[step / 2];
   }
   template <bool TAIL> static __device__ __forceinline__ void load_rows(Rows& o, const ET* row, int left, int g) {
@@ -126,24 +131,24 @@ template <typename ET> struct Few<ET, true> {
         else o.x[q][d] = *reinterpret_cast<const u32x4*>((const char*)(row + 16 * g + 8 * q) + 16 * d);
       }
   }
-  template <int RT> static __device__ __forceinline__ void multiply(const Weights& w, const Rows (&x)[RT], f32x4 (&acc)[RT][4]) {
+  template <int RT> static __device__ __forceinline__ void multiply(const Weights& w, const Rows (&x)[RT], f32x4 (&acc)[RT][C]) {
     const uint32_t e = w.exponent;
     const float scale = e == kScaleNaN ? __uint_as_float(0x7fc00000u) : e == 0 ? __uint_as_float(0x00400000u) : __uint_as_float(e << 23);
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      bf16x8 b[4];
+      bf16x8 b[C];
 #pragma unroll
-      for (int f = 0; f < 4; ++f) {
-        const int lo = (int)w.w[f][2 * q], hi = (int)w.w[f][2 * q + 1];
+      for (int c = 0; c < C; ++c) {
+        const int lo = (int)w.w[c][2 * q], hi = (int)w.w[c][2 * q + 1];
         const bf16x2 b0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
         const bf16x2 b2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), b3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
-        b[f] = bf16x8{b0.x, b0.y, b1.x, b1.y, b2.x, b2.y, b3.x, b3.y};
+        b[c] = bf16x8{b0.x, b0.y, b1.x, b1.y, b2.x, b2.y, b3.x, b3.y};
       }
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
         if constexpr (kPieces == 1) {
 #pragma unroll
-          for (int f = 0; f < 4; ++f) acc[t][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[f], __builtin_bit_cast(bf16x8, x[t].x[q][0]), acc[t][f], 0, 0, 0);
+          for (int c = 0; c < C; ++c) acc[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[c], __builtin_bit_cast(bf16x8, x[t].x[q][0]), acc[t][c], 0, 0, 0);
         } else {
           bf16x8 a[3];
 #pragma unroll
@@ -158,52 +163,86 @@ template <typename ET> struct Few<ET, true> {
 #pragma unroll
           for (int d = 2; d >= 0; --d)
 #pragma unroll
-            for (int f = 0; f < 4; ++f) acc[t][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[f], a[d], acc[t][f], 0, 0, 0);
+            for (int c = 0; c < C; ++c) acc[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[c], a[d], acc[t][c], 0, 0, 0);
         }
       }
     }
   }
 };
 
-// One expert's rows times 64 columns of its weights, the sum over k shared by the block's waves; done(row, column, sum) for each result, by one thread.
-// rows[r]: where row r of the operand is; pitch: N, or the bytes of a row of 8-bit weights.
-template <typename ET, bool W8, int RT, typename F>
-__device__ __forceinline__ void few_product(const char* W, const uint8_t* sc, int64_t pitch, const ET* const* rows, int n_rows, int64_t K, int64_t N, int64_t n0,
-                                            float* sums, F&& done) {
-  typedef Few<ET, W8> L;
-  constexpr int D = L::depth(RT);                                   // steps in flight
+// A block's part of an expert's weights, and the first steps of each wave's share: their loads go out as soon as the expert is known, before its rows are.
+template <typename ET, bool W8, int C, int TILES> struct FewWeights {
+  typedef Few<ET, W8, C> L;
+  static constexpr int kFirst = L::depth(TILES) < 2 ? 1 : 2;
+  const char* W;
+  const uint8_t* sc;
+  int64_t pitch, step_bytes;                                        // pitch: N, or the bytes of a row of 8-bit weights
+  typename L::At at;
+  int full;                                                         // whole steps
+  typename L::Weights w[kFirst];
+
+  __device__ __forceinline__ void start(const void* weights, const uint8_t* scales, int64_t e, int64_t K, int64_t N, int64_t n0) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    pitch = W8 ? row_bytes8(K) : N;
+    W = (const char*)weights + (W8 ? e * N * pitch : e * K * N * (int64_t)sizeof(ET));
+    sc = W8 ? scales + (e * ceil_div(N, kBlock8) + n0 / kBlock8) * row_scales8(K) : nullptr;
+    step_bytes = L::step_bytes(pitch);
+    at = L::at(n0, N, pitch, lane & 15, lane >> 4);
+    full = (int)(K / L::kStep);
+#pragma unroll
+    for (int d = 0; d < kFirst; ++d) {
+      const int s = L::step(wave, d);
+      if (s < full) L::template load<false>(w[d], W + s * step_bytes, at, sc, pitch, s, 0, lane >> 4);
+    }
+  }
+};
+
+// One expert's rows times 16 C columns of its weights, the sum over k shared by the block's waves; done(row, column, sum) for each result, by one thread.
+// rows[r]: where row r of the operand is.
+template <typename ET, bool W8, int C, int TILES, int RT, typename F>
+__device__ __forceinline__ void few_product(const FewWeights<ET, W8, C, TILES>& o, const ET* const* rows, int n_rows, int64_t K, int64_t N, int64_t n0, float* sums, F&& done) {
+  typedef Few<ET, W8, C> L;
+  constexpr int D = L::depth(RT), kFirst = FewWeights<ET, W8, C, TILES>::kFirst, kColumns = 16 * C;        // D: steps in flight
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
   const ET* row[RT];
 #pragma unroll
   for (int t = 0; t < RT; ++t) row[t] = rows[16 * t + i < n_rows ? 16 * t + i : 0];
-  f32x4 acc[RT][4];
+  f32x4 acc[RT][C];
 #pragma unroll
   for (int t = 0; t < RT; ++t)
 #pragma unroll
-    for (int c = 0; c < 4; ++c) acc[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const typename L::At at = L::at(n0, N, pitch, i, g);
-  const int64_t step_bytes = L::step_bytes(pitch);
+    for (int c = 0; c < C; ++c) acc[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
   typename L::Weights w[D];
   typename L::Rows x[D][RT];
-  const int full = (int)(K / L::kStep);
-  auto fetch = [&](int s, int d) {
-    if (s >= full) return;
-    L::template load<false>(w[d], W + s * step_bytes, at, sc, pitch, s, 0, g);
+  const int full = o.full;
+  auto fetch_rows = [&](int s, int d) {
 #pragma unroll
     for (int t = 0; t < RT; ++t) L::template load_rows<false>(x[d][t], row[t] + s * L::kStep, 0, g);
   };
+  auto fetch = [&](int s, int d) {
+    if (s >= full) return;
+    L::template load<false>(w[d], o.W + s * o.step_bytes, o.at, o.sc, o.pitch, s, 0, g);
+    fetch_rows(s, d);
+  };
 #pragma unroll
-  for (int d = 0; d < D; ++d) fetch(wave + d * kFewWaves, d);
-  for (int s = wave; s < full; s += D * kFewWaves) {
+  for (int d = 0; d < D; ++d) {
+    const int s = L::step(wave, d);
+    if (d >= kFirst) fetch(s, d);
+    else if (s < full) {
+      w[d] = o.w[d];
+      fetch_rows(s, d);
+    }
+  }
+  for (int j = 0; L::step(wave, j) < full; j += D) {
 #pragma unroll
     for (int d = 0; d < D; ++d) {
-      if (s + d * kFewWaves >= full) break;
+      if (L::step(wave, j + d) >= full) break;
       L::template multiply<RT>(w[d], x[d], acc);
-      fetch(s + (d + D) * kFewWaves, d);
+      fetch(L::step(wave, j + d + D), d);
     }
   }
   if (const int left = (int)(K - (int64_t)full * L::kStep); left > 0 && wave == full % kFewWaves) {
-    L::template load<true>(w[0], W + full * step_bytes, at, sc, pitch, full, left, g);
+    L::template load<true>(w[0], o.W + full * o.step_bytes, o.at, o.sc, o.pitch, full, left, g);
 #pragma unroll
     for (int t = 0; t < RT; ++t) L::template load_rows<true>(x[0][t], row[t] + (int64_t)full * L::kStep, left, g);
     L::template multiply<RT>(w[0], x[0], acc);
@@ -216,71 +255,88 @@ __device__ __forceinline__ void few_product(const char* W, const uint8_t* sc, in
       __syncthreads();
     }
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
+    for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) sums[(wave * 16 + i) * (kFewColumns + 4) + (L::kApart ? 16 * c + 4 * g + v : 16 * g + 4 * v + c)] = acc[t][c][v];
+      for (int v = 0; v < 4; ++v) sums[(wave * 16 + i) * (kColumns + 4) + (L::kApart ? 16 * c + 4 * g + v : 4 * C * g + C * v + c)] = acc[t][c][v];
     __syncthreads();
-    for (int q = threadIdx.x; q < 16 * kFewColumns; q += 64 * kFewWaves) {
-      const int r = q / kFewColumns, c = q % kFewColumns;
+    for (int q = threadIdx.x; q < 16 * kColumns; q += 64 * kFewWaves) {
+      const int r = q / kColumns, c = q % kColumns;
       if (16 * t + r >= n_rows || n0 + c >= N) continue;
       float s = 0.f;
 #pragma unroll
-      for (int u = 0; u < kFewWaves; ++u) s += sums[(u * 16 + r) * (kFewColumns + 4) + c];
+      for (int u = 0; u < kFewWaves; ++u) s += sums[(u * 16 + r) * (kColumns + 4) + c];
       done(16 * t + r, n0 + c, s);
     }
   }
 }
 
-// Gate logits of few tokens and experts: part[s][t][e] = the sum over a slice of the model dim in fp64; whoever reads them adds the slices up in order, so the sum is
-// rounded once, like moe_gate_logits'.  A single block would wait for one load after the other (16 tokens x 8 experts, M = 2048: 12 us).
-constexpr int kGateStage = 8192;                                    // floats of the slice that a block holds at a time
-template <typename ET>
-__global__ __launch_bounds__(512) void few_logits_kernel(const ET* __restrict__ x, const ET* __restrict__ Wg, int T, int M, int E, int slice, int stage,
-                                                         int group_bits, double* __restrict__ part) {
-  __shared__ float tokens[kGateStage];                              // [T][stage] and then [stage][E]
-  float* weights = tokens + T * stage;
-  const int m_end = min(M, (int)(blockIdx.x + 1) * slice), pairs = T * E;
-  const int group = 1 << group_bits, sub = threadIdx.x & (group - 1);
-  constexpr int kTurns = 2;                                         // pairs of a thread: T * E <= 1024
-  double sum[kTurns] = {};
-  for (int m0 = blockIdx.x * slice; m0 < m_end; m0 += stage) {
-    const int n = min(stage, m_end - m0);
-    __syncthreads();
-    for (int q = threadIdx.x; q < T * n; q += 512) tokens[q / n * stage + q % n] = load_as_f32(x + (int64_t)(q / n) * M + m0 + q % n);
-    const ET* w = Wg + (int64_t)m0 * E;
-#pragma unroll 4
-    for (int q = threadIdx.x; q < n * E; q += 512) weights[q] = load_as_f32(w + q);
-    __syncthreads();
+// Gate logits of few tokens and experts, a block to TOKENS tokens and 8 experts: its threads take 8 of the model dim each at a time, all their loads go out together, and the
+// products are exact and summed in fp64, so a logit is rounded once, like moe_gate_logits'.  VECTOR: rows of Wg in pieces of 8 experts.
+constexpr int kLogitExperts = 8;
+template <typename ET, int TOKENS, bool VECTOR>
+__global__ __launch_bounds__(512) void few_logits_kernel(const ET* __restrict__ x, const ET* __restrict__ Wg, const float* __restrict__ gate_bias, int T, int M, int E,
+                                                         float* __restrict__ logits, int32_t* __restrict__ counts) {
+  constexpr int kSums = TOKENS * kLogitExperts, V = Vec16<ET>::N;
+  __shared__ double wave_sums[8][kSums];
+  const int e0 = blockIdx.x * kLogitExperts, t0 = blockIdx.y * TOKENS, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  double sum[kSums] = {};
+  for (int m = threadIdx.x * 8; m < M; m += 512 * 8) {
+    float a[TOKENS][8], b[8][kLogitExperts];
 #pragma unroll
-    for (int u = 0; u < kTurns; ++u) {
-      const int p = u * (512 >> group_bits) + (threadIdx.x >> group_bits);
-      if (p >= pairs) break;
-      const float* a = tokens + p / E * stage;
-      const float* b = weights + p % E;
-      for (int m = sub; m < n; m += group) sum[u] += (double)a[m] * (double)b[m * E];
+    for (int r = 0; r < 8; ++r) {
+      const ET* w = Wg + (int64_t)(m + r) * E + e0;
+#pragma unroll
+      for (int c = 0; c < kLogitExperts; c += V) {
+        if constexpr (VECTOR) {
+          float f[V];
+          Vec16<ET>::unpack(*reinterpret_cast<const uint4*>(w + c), f);
+#pragma unroll
+          for (int j = 0; j < V; ++j) b[r][c + j] = f[j];
+        } else {
+#pragma unroll
+          for (int j = 0; j < V; ++j) b[r][c + j] = load_as_f32(w + min(c + j, E - 1 - e0));
+        }
+      }
     }
-  }
 #pragma unroll
-  for (int u = 0; u < kTurns; ++u) {
-    const int p = u * (512 >> group_bits) + (threadIdx.x >> group_bits);
-    for (int d = 1; d < group; d <<= 1) sum[u] += __shfl_xor(sum[u], d);
-    if (p < pairs && sub == 0) part[(int64_t)blockIdx.x * pairs + p] = sum[u];
+    for (int i = 0; i < TOKENS; ++i)
+#pragma unroll
+      for (int c = 0; c < 8; c += V) {
+        float f[V];
+        Vec16<ET>::unpack(*reinterpret_cast<const uint4*>(x + (int64_t)min(t0 + i, T - 1) * M + m + c), f);
+#pragma unroll
+        for (int j = 0; j < V; ++j) a[i][c + j] = f[j];
+      }
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+#pragma unroll
+      for (int i = 0; i < TOKENS; ++i)
+#pragma unroll
+        for (int j = 0; j < kLogitExperts; ++j) sum[i * kLogitExperts + j] += (double)a[i][r] * (double)b[r][j];
   }
+  // a wave's lanes: each turn halves the sums that a lane goes on with, so lane l ends with the one whose index is l's low bits, reversed
+  int at = 0;
+#pragma unroll
+  for (int half = kSums / 2, d = 1; d < 64; d <<= 1, half >>= 1) {
+    const bool upper = lane & d;
+    if (half == 0) sum[0] += __shfl_xor(sum[0], d);
+#pragma unroll
+    for (int i = 0; i < half; ++i) {
+      const double give = upper ? sum[i] : sum[i + half], keep = upper ? sum[i + half] : sum[i];
+      sum[i] = keep + __shfl_xor(give, d);
+    }
+    at += upper ? half : 0;
+  }
+  if (lane < kSums) wave_sums[wave][at] = sum[0];
+  __syncthreads();
+  const int t = t0 + threadIdx.x / kLogitExperts, e = e0 + threadIdx.x % kLogitExperts;
+  if (threadIdx.x >= kSums || t >= T || e >= E) return;
+  if (t == 0) counts[e] = 0;                                        // what has arrivals is counted later
+  double s = gate_bias ? (double)gate_bias[e] : 0.0;
+#pragma unroll
+  for (int u = 0; u < 8; ++u) s += wave_sums[u][threadIdx.x];
+  logits[(int64_t)t * E + e] = (float)s;
 }
-
-// Columns of x that a slice has: a thread's share of the products should be short, and so should what every block adds up again.
-inline int few_gate_slice(int64_t M, int64_t T, int64_t E) {
-  int64_t slices = 16384 / (T * E);
-  slices = slices > 32 ? 32 : slices;
-  return (int)(ceil_div(ceil_div(M, slices), 8) * 8);
-}
-
-// What the first product's blocks work out of the gate: LDS that the sums take over later.
-struct FewGate {
-  uint32_t keys[kFewGateLogits];                                    // logits [T][E] as integers in the same order
-  int cnt[512];                                                     // arrivals per expert
-  int idx[kFewPairs];                                               // experts in the order of arrival: all first choices, all second ones, ...
-};
 
 __device__ __forceinline__ uint32_t ordered(float v) {              // -0 as +0
   const uint32_t u = __float_as_uint(v + 0.0f);
@@ -288,199 +344,306 @@ __device__ __forceinline__ uint32_t ordered(float v) {              // -0 as +0
 }
 __device__ __forceinline__ float unordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
 
-// Experts of every token from the logits' slices (p.slices > 0) or from idx as the gate's own kernels left it, arrivals per expert; in every block, since a
-// launch of its own would take longer.  A choice's rank is the number of experts with a larger logit, or an equal one and a lower index.
-__device__ __forceinline__ void few_choose(const FewTokens& p, FewGate& s) {
-  constexpr int threads = 64 * kFewWaves;
-  const int T = (int)p.T, E = (int)p.E, k = p.k;
-  for (int e = threadIdx.x; e < E; e += threads) s.cnt[e] = 0;
-  if (p.slices == 0) {
-    for (int o = threadIdx.x; o < T * k; o += threads) s.idx[o] = p.idx[o % T * k + o / T];
-    __syncthreads();
-  } else {
-    for (int q = threadIdx.x; q < T * E; q += threads) {
-      double v = 0.0;
+// Units of work of both products: an expert each, or, where there are fewer choices than experts, a choice each, of which the first one to arrive at its expert does the work.
+__host__ __device__ __forceinline__ int few_units(const FewTokens& p) { return (int)(p.E < p.T * p.k ? p.E : p.T * p.k); }
+
+// A token's logits as integers in the same order, and their ranks: the number of experts with a larger logit, or an equal one and a lower index.
+struct FewRanks {
+  uint32_t keys[kFewExperts];
+  int rank[kFewExperts];
+};
+__device__ __forceinline__ void few_rank(const FewTokens& p, int t, FewRanks& s) {
+  const int E = (int)p.E, group = 1 << p.expert_bits, sub = threadIdx.x & (group - 1), e = threadIdx.x >> p.expert_bits;     // threads to an expert, in one wave
+  if (threadIdx.x < E) s.keys[threadIdx.x] = ordered(p.logits[(int64_t)t * E + threadIdx.x]);
+  __syncthreads();
+  int rank = 0;
+  if (e < E) {
+    const uint32_t own = s.keys[e];
 #pragma unroll 8
-      for (int c = 0; c < p.slices; ++c) v += p.logit_parts[(int64_t)c * T * E + q];
-      if (p.gate_bias) v += (double)p.gate_bias[q % E];
-      s.keys[q] = ordered((float)v);
+    for (int o = sub; o < E; o += group) {
+      const uint32_t other = s.keys[o];
+      rank += other > own || (other == own && o < e) ? 1 : 0;
     }
-    __syncthreads();
-    for (int q = threadIdx.x; q < T * E; q += threads) {
-      const int t = q / E, e = q - t * E;
-      const uint32_t own = s.keys[q];
-      int rank = 0;
-#pragma unroll 8
-      for (int o = 0; o < E; ++o) {
-        const uint32_t other = s.keys[t * E + o];
-        rank += other > own || (other == own && o < e) ? 1 : 0;
-      }
-      if (rank < k) s.idx[rank * T + t] = e;
-    }
-    __syncthreads();
   }
-  for (int o = threadIdx.x; o < T * k; o += threads) atomicAdd(&s.cnt[s.idx[o]], 1);
+  for (int d = 1; d < group; d <<= 1) rank += __shfl_xor(rank, d);
+  if (e < E && sub == 0) s.rank[e] = rank;
   __syncthreads();
 }
 
-// The routing as the caller sees it, by one block.
-__device__ __forceinline__ void few_report(const FewTokens& p, const FewGate& s) {
-  constexpr int threads = 64 * kFewWaves;
-  const int T = (int)p.T, E = (int)p.E, k = p.k, lane = threadIdx.x & 63;
-  for (int e = threadIdx.x; e < E; e += threads) p.counts[e] = s.cnt[e];
-  for (int q = threadIdx.x; q < T * E; q += threads) p.logits[q] = unordered(s.keys[q]);
-  for (int o = threadIdx.x; o < T * k; o += threads) {
-    int before = 0;
-    for (int u = 0; u < o; ++u) before += s.idx[u] == s.idx[o] ? 1 : 0;
-    p.idx[o % T * k + o / T] = s.idx[o];
-    p.loc[o % T * k + o / T] = before;
-  }
-  for (int t = threadIdx.x >> 6; t < T; t += kFewWaves) {           // a wave to a token
-    const float top = unordered(s.keys[t * E + s.idx[t]]);
-    float all = 0.f, chosen = 0.f;
-    for (int e = lane; e < E; e += 64) all += expf(unordered(s.keys[t * E + e]) - top);
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) all += __shfl_xor(all, d);
-    for (int j = 0; j < k; ++j) chosen += expf(unordered(s.keys[t * E + s.idx[j * T + t]]) - top);
-    for (int j = lane; j < k; j += 64) p.gate_w[t * k + j] = expf(unordered(s.keys[t * E + s.idx[j * T + t]]) - top) / (p.normalize ? chosen : all);
-  }
-}
-
-// The a-th expert that has arrivals, or -1.
-__device__ __forceinline__ int active_expert(int a, const int* cnt, int E) {
-  const int lane = threadIdx.x & 63;
-  for (int e0 = 0; e0 < E; e0 += 64) {
-    unsigned long long m = __ballot(e0 + lane < E && cnt[e0 + lane] > 0);
-    const int n = __builtin_popcountll(m);
-    if (a < n) {
-      for (; a > 0; --a) m &= m - 1;
-      return e0 + __builtin_ctzll(m);
+// Tokens' choices and gate weights as the caller sees them: the b-th block has 8 tokens, a wave each, or, of more than 64 experts, one token.
+inline __host__ __device__ int few_token_blocks(const FewTokens& p) { return (int)(p.E <= 64 ? (p.T + kFewWaves - 1) / kFewWaves : p.T); }
+__device__ __forceinline__ void few_report(const FewTokens& p, int b, FewRanks& s) {
+  const int E = (int)p.E, k = p.k, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int t = b;
+  if (E <= 64) {
+    t = b * kFewWaves + wave;
+    if (t >= p.T) return;
+    const uint32_t own = lane < E ? ordered(p.logits[(int64_t)t * E + lane]) : 0;
+    int rank = 0;
+    for (int o = 0; o < E; ++o) {
+      const uint32_t other = (uint32_t)__builtin_amdgcn_readlane((int)own, o);
+      rank += other > own || (other == own && o < lane) ? 1 : 0;
     }
-    a -= n;
+    if (lane < E) s.keys[wave * 64 + lane] = own;
+    if (lane < E) s.rank[wave * 64 + lane] = rank;
+  } else {
+    few_rank(p, t, s);
+    if (wave > 0) return;
   }
-  return -1;
+  const uint32_t* keys = s.keys + (E <= 64 ? wave * 64 : 0);
+  const int* ranks = s.rank + (E <= 64 ? wave * 64 : 0);
+  uint32_t most = 0;
+  for (int e = lane; e < E; e += 64) most = max(most, keys[e]);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, d));
+  const float top = unordered(most);
+  float sum = 0.f;                                                  // over all experts, or the chosen ones
+  for (int e = lane; e < E; e += 64) sum += !p.normalize || ranks[e] < k ? expf(unordered(keys[e]) - top) : 0.f;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
+  for (int e = lane; e < E; e += 64) {
+    if (ranks[e] >= k) continue;
+    p.idx[(int64_t)t * k + ranks[e]] = e;
+    p.gate_w[(int64_t)t * k + ranks[e]] = expf(unordered(keys[e]) - top) / sum;
+  }
 }
 
-// Block x, y: 64 columns, the y-th expert that has arrivals.  The first product finds its expert's rows and leaves them for the second (p.plan: expert, number
-// of rows, 64 pairs).
-template <typename ET, bool W8, bool UP>
-__global__ __launch_bounds__(64 * kFewWaves) void few_kernel(const FewTokens p) {
-  constexpr int kSums = kFewWaves * 16 * (kFewColumns + 4);
+// The pairs (t, j) that expert e has, from the logits: a group of threads finds its rank for one token, and one wave the order of the arrivals: all first choices, all second ones ...
+__device__ __forceinline__ int few_own_rank(const FewTokens& p, int e) {
+  const int E = (int)p.E, group = 1 << p.token_bits, sub = threadIdx.x & (group - 1), t = threadIdx.x >> p.token_bits;
+  const float* row = p.logits + (int64_t)(t < p.T ? t : 0) * E;
+  const uint32_t own = ordered(row[e]);
+  int rank = 0;
+  for (int o0 = sub; o0 < E; o0 += 4 * group) {
+    float v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = row[o0 + i * group < E ? o0 + i * group : e];      // e itself counts for nothing
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t other = ordered(v[i]);
+      rank += other > own || (other == own && o0 + i * group < e) ? 1 : 0;
+    }
+  }
+  for (int d = 1; d < group; d <<= 1) rank += __shfl_xor(rank, d);
+  return rank;
+}
+// into pair_of; returns, in wave 0, how many there are, up to the capacity, if the first is the one given (any if negative), else 0
+__device__ __forceinline__ int few_own_pairs(const FewTokens& p, int e, int rank, int first, bool report, uint32_t* arrivals, int* pair_of) {
+  const int T = (int)p.T, lane = threadIdx.x & 63, t = threadIdx.x >> p.token_bits;
+  if (t < T && (threadIdx.x & ((1 << p.token_bits) - 1)) == 0) arrivals[t] = rank < p.k ? (uint32_t)(rank * T + t) : 0xffffffffu;
+  __syncthreads();
+  if (threadIdx.x >= 64) return 0;
+  const uint32_t key = lane < T ? arrivals[lane] : 0xffffffffu;
+  int before = 0;
+  for (int u = 0; u < T; ++u) before += (uint32_t)__builtin_amdgcn_readlane((int)key, u) < key ? 1 : 0;
+  const bool mine = key != 0xffffffffu;
+  if (first >= 0 && __ballot((int)key == first && before == 0) == 0) return 0;
+  const int q = lane * p.k + (int)(key / (uint32_t)T), n = __builtin_popcountll(__ballot(mine));
+  const int most = (int)(p.C < kFewRows ? p.C : kFewRows);
+  if (mine && before < most) pair_of[before] = q;
+  if (report && mine) p.loc[q] = before;
+  if (report && lane == 0 && n > 0) p.counts[e] = n;
+  return n < most ? n : most;
+}
+
+// The expert of choice o = j T + t.
+__device__ __forceinline__ int few_chosen(const FewTokens& p, int o, FewRanks& s, int* found) {
+  few_rank(p, o % (int)p.T, s);
+  if (threadIdx.x < p.E && s.rank[threadIdx.x] == o / (int)p.T) *found = threadIdx.x;
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(*found);
+}
+
+// plan: for the y-th blocks of the second product, or of both: their expert, its number of rows and its pairs.
+__device__ __forceinline__ void few_write_plan(int32_t* plan, int e, int n, const int* pair_of) {
+  const int lane = threadIdx.x & 63;
+  if (lane < n) plan[2 + lane] = pair_of[lane];
+  if (lane == 0) plan[0] = e;
+  if (lane == 0) plan[1] = n;
+}
+
+// The plan in a launch of its own: a block to a unit, then those that report the tokens' choices.
+__global__ __launch_bounds__(64 * kFewWaves) void few_plan_kernel(const FewTokens p) {
+  __shared__ FewRanks ranks;
+  __shared__ uint32_t arrivals[kFewRows];
+  __shared__ int pair_of[kFewRows], found;
+  const int units = few_units(p);
+  int e = blockIdx.x;
+  if (e >= units) {
+    few_report(p, e - units, ranks);
+    return;
+  }
+  if (e == 0)
+    for (int64_t s = threadIdx.x; s < ceil_div(p.M, kFewArrival); s += 64 * kFewWaves) p.arrived[s] = 0;
+  const bool direct = units == p.E;
+  if (!direct) e = few_chosen(p, blockIdx.x, ranks, &found);
+  const int n = few_own_pairs(p, e, few_own_rank(p, e), direct ? -1 : (int)blockIdx.x, true, arrivals, pair_of);
+  if (threadIdx.x < 64) few_write_plan(p.plan + (int64_t)blockIdx.x * kFewPlan, e, n, pair_of);
+}
+
+// Block x, y: 16 C columns of unit y's expert.
+// TILES: of 16 rows that an expert can have at most, 1 or 4; with 1 two blocks fit a CU.
+template <typename ET, bool W8, int C, int TILES, bool UP>
+__global__ __launch_bounds__(64 * kFewWaves, TILES == 1 ? 4 : 2) void few_kernel(const FewTokens p) {
+  constexpr int kColumns = 16 * C, kSums = kFewWaves * 16 * (kColumns + 4);
   union Lds {
-    FewGate gate;
+    FewRanks ranks;
+    uint32_t arrivals[kFewRows];
     float sums[kSums];
   };
   __shared__ Lds lds;
   __shared__ int pair_of[kFewRows], found[2];
   __shared__ const ET* rows[kFewRows];
   __shared__ int last;
-  const int64_t K = UP ? p.M : p.H, N = UP ? p.H : p.M, n0 = (int64_t)blockIdx.x * kFewColumns;
-  int32_t* plan = p.plan + (int64_t)blockIdx.y * kFewPlan;
+  const int64_t K = UP ? p.M : p.H, N = UP ? p.H : p.M, n0 = (int64_t)blockIdx.x * kColumns;
+  const int units = few_units(p);
   if constexpr (UP) {
-    if (blockIdx.y == 0) {                                          // the arrivals of the next launch's blocks start from zero
-      const int64_t at = (int64_t)blockIdx.x * (64 * kFewWaves) + threadIdx.x;
-      for (int64_t s = at; s < ceil_div(p.M, kFewColumns); s += (int64_t)gridDim.x * (64 * kFewWaves)) p.arrived[s] = 0;
+    // The tokens' choices: rows of blocks after the others, the last to start, so that it is theirs to share a CU (16 tokens x 8 experts of 2048 x 2048, 256 + 8 blocks: 41.1 us,
+    // and 45.8 with these among the others).
+    if (blockIdx.y >= units) {
+      const int b = (blockIdx.y - units) * gridDim.x + blockIdx.x;
+      if (b < few_token_blocks(p)) few_report(p, b, lds.ranks);
+      return;
     }
-    few_choose(p, lds.gate);
-    if (p.slices > 0 && blockIdx.x == 0 && blockIdx.y == 0) few_report(p, lds.gate);
-    const int e = active_expert(blockIdx.y, lds.gate.cnt, (int)p.E), lane = threadIdx.x & 63;
-    if (threadIdx.x < 64) {                                         // one wave goes through the arrivals
-      int n = 0;
-      const int most = (int)(p.C < kFewRows ? p.C : kFewRows);
-      for (int o0 = 0; e >= 0 && o0 < p.T * p.k; o0 += 64) {
-        const int o = o0 + lane;
-        const bool mine = o < p.T * p.k && lds.gate.idx[o] == e;
-        const unsigned long long m = __ballot(mine);
-        const int at = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
-        if (mine && at < most) pair_of[at] = (int)(o % p.T * p.k + o / p.T);
-        n += __builtin_popcountll(m);
-      }
-      n = n < most ? n : most;
-      if (blockIdx.x == 0) {
-        if (lane < n) plan[2 + lane] = pair_of[lane];
-        if (lane == 0) plan[0] = e;
-        if (lane == 0) plan[1] = n;
-      }
-      if (lane == 0) found[0] = e;
-      if (lane == 0) found[1] = n;
-    }
+    if (blockIdx.x == 0 && blockIdx.y == 0 && !p.planned)           // the arrivals of the next launch's blocks
+      for (int64_t s = threadIdx.x; s < ceil_div(p.M, kFewArrival); s += 64 * kFewWaves) p.arrived[s] = 0;
+  }
+  const bool direct = units == p.E;      // the weights' expert is known before its rows are
+  int32_t* plan = p.plan + (int64_t)blockIdx.y * kFewPlan;
+  FewWeights<ET, W8, C, TILES> weights;
+  const void* W = UP ? p.W1 : p.W2;
+  const uint8_t* sc = UP ? p.s1 : p.s2;
+  if (direct) weights.start(W, sc, blockIdx.y, K, N, n0);
+  const bool planned = !UP || p.planned;
+  int unit_e = blockIdx.y, v = 0;
+  if (planned) v = threadIdx.x < kFewPlan ? plan[threadIdx.x] : 0;
+  else {
+    if (!direct) unit_e = few_chosen(p, blockIdx.y, lds.ranks, found);
+    v = few_own_rank(p, unit_e);
+  }
+  if (planned) {
+    if (threadIdx.x < 2) found[threadIdx.x] = v;
+    else if (threadIdx.x < kFewPlan) pair_of[threadIdx.x - 2] = v;
   } else {
-    if (threadIdx.x < kFewPlan) {
-      const int v = plan[threadIdx.x];
-      if (threadIdx.x < 2) found[threadIdx.x] = v;
-      else pair_of[threadIdx.x - 2] = v;
+    const int n = few_own_pairs(p, unit_e, v, direct ? -1 : (int)blockIdx.y, blockIdx.x == 0, lds.arrivals, pair_of);
+    if (threadIdx.x < 64) {
+      if (blockIdx.x == 0) few_write_plan(plan, unit_e, n, pair_of);
+      if (threadIdx.x == 0) found[0] = unit_e;
+      if (threadIdx.x == 0) found[1] = n;
     }
   }
   __syncthreads();
-  const int e = found[0], n_rows = found[1];
+  const int e = __builtin_amdgcn_readfirstlane(found[0]), n_rows = __builtin_amdgcn_readfirstlane(found[1]);
+  if (!direct && n_rows > 0) weights.start(W, sc, e, K, N, n0);
   if (threadIdx.x < n_rows) {
     const int q = pair_of[threadIdx.x];
     rows[threadIdx.x] = UP ? (const ET*)p.x + (int64_t)(q / p.k) * K : (const ET*)p.hidden + (int64_t)q * K;
   }
   __syncthreads();
   if (n_rows > 0) {
-    const int64_t row8 = row_bytes8(K), pitch = W8 ? row8 : N;
-    const char* W = (const char*)(UP ? p.W1 : p.W2) + (W8 ? (int64_t)e * N * row8 : (int64_t)e * K * N * sizeof(ET));
-    const uint8_t* sc = W8 ? (UP ? p.s1 : p.s2) + ((int64_t)e * ceil_div(N, kBlock8) + n0 / kBlock8) * row_scales8(K) : nullptr;
     const ET* bias = (const ET*)(UP ? p.b1 : p.b2);
     auto done = [&](int r, int64_t n, float s) {
       if (bias) s += load_as_f32(bias + (int64_t)e * N + n);
       const int64_t q = pair_of[r];
       if (UP) store_from_f32((ET*)p.hidden + q * N + n, apply_act(s, p.act));
-      else p.partial[q * N + n] = s;
+      else if (p.k == 1) store_from_f32((ET*)p.out + q * N + n, p.gate_w[q] * s);
+      else __hip_atomic_store(p.partial + q * N + n, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     };
-    if (n_rows <= 16) few_product<ET, W8, 1>(W, sc, pitch, rows, n_rows, K, N, n0, lds.sums, done);
-    else if (n_rows <= 32) few_product<ET, W8, 2>(W, sc, pitch, rows, n_rows, K, N, n0, lds.sums, done);
-    else few_product<ET, W8, 4>(W, sc, pitch, rows, n_rows, K, N, n0, lds.sums, done);
+    if (TILES == 1 || n_rows <= 16) few_product<ET, W8, C, TILES, 1>(weights, rows, n_rows, K, N, n0, lds.sums, done);
+    else if (n_rows <= 32) few_product<ET, W8, C, TILES, 2>(weights, rows, n_rows, K, N, n0, lds.sums, done);
+    else few_product<ET, W8, C, TILES, 4>(weights, rows, n_rows, K, N, n0, lds.sums, done);
   }
   if (UP) return;
-  // The last block of these columns to arrive adds up every token's choices, in their order: the same sums whoever it is, and nobody waits.  One wave releases what
-  // the block has written: with a fence in every wave, 16 tokens x 8 experts of 2048 x 2048 took 50 us instead of 22.
+  if (p.k == 1) {                                                   // nothing to add up: what has no row here is zero
+    if (blockIdx.y > 0) return;
+    for (int64_t q = threadIdx.x; q < p.T * kColumns; q += 64 * kFewWaves) {
+      const int64_t t = q / kColumns, n = n0 + q % kColumns;
+      if (n < N && p.loc[t] >= p.C) store_from_f32((ET*)p.out + t * N + n, 0.f);
+    }
+    return;
+  }
+  // The last block of these columns to arrive adds up every token's choices, in their order: the same sums whoever it is, and nobody waits.  The stores of the partial
+  // sums go through the XCD's own L2, so when a wave has waited for its own they are where every XCD sees them, and counting needs no release, which would write
+  // back all of that L2: 64 tokens x 64 experts of 1024 x 4096 took 259 us with a release by one wave of each block instead of 227.
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  if (threadIdx.x == 0) last = __hip_atomic_fetch_add(p.arrived + blockIdx.x, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.y - 1;
+  if (threadIdx.x == 0) last = __hip_atomic_fetch_add(p.arrived + blockIdx.x, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.y - 1;
   __syncthreads();
   if (!last) return;
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-  for (int64_t q = threadIdx.x; q < p.T * kFewColumns; q += 64 * kFewWaves) {
-    const int64_t t = q / kFewColumns, n = n0 + q % kFewColumns;
+  for (int64_t q = threadIdx.x; q < p.T * kColumns; q += 64 * kFewWaves) {
+    const int64_t t = q / kColumns, n = n0 + q % kColumns;
     if (n >= N) continue;
     float s = 0.f;
-    for (int j = 0; j < p.k; ++j)
-      if (p.loc[t * p.k + j] < p.C) s += p.gate_w[t * p.k + j] * p.partial[(t * p.k + j) * N + n];
+    for (int j0 = 0; j0 < p.k; j0 += 8) {                           // their loads together; a choice without a row has no sums to read a value from
+      float w[8], v[8];
+      bool kept[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int64_t o = t * p.k + (j0 + j < p.k ? j0 + j : p.k - 1);
+        kept[j] = j0 + j < p.k && p.loc[o] < p.C;
+        w[j] = p.gate_w[o];
+        v[j] = p.partial[o * N + n];
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s += kept[j] ? w[j] * v[j] : 0.f;
+    }
     store_from_f32((ET*)p.out + t * N + n, s);
   }
 }
 
-template <typename ET> hipError_t launch_few_logits(const FewTokens& p, hipStream_t s) {
-  const int T = (int)p.T, E = (int)p.E, M = (int)p.M, slice = few_gate_slice(p.M, p.T, p.E);
-  int stage = kGateStage / (T + E), bits = 0;
-  if (stage > slice) stage = slice;
-  while (bits < 6 && (T * E << (bits + 1)) <= 512) ++bits;          // threads to a sum: as many as there are
-  few_logits_kernel<ET><<<dim3((unsigned)p.slices), dim3(512), 0, s>>>((const ET*)p.x, (const ET*)p.Wg, T, M, E, slice, stage, bits, p.logit_parts);
-  return hipGetLastError();
+template <typename ET, int TOKENS> void launch_few_logits(const FewTokens& p, hipStream_t s) {
+  const dim3 grid((unsigned)ceil_div(p.E, kLogitExperts), (unsigned)ceil_div(p.T, TOKENS)), block(512);
+  const bool vector = p.E % kLogitExperts == 0 && (reinterpret_cast<uintptr_t>(p.Wg) & 15) == 0;
+  if (vector) few_logits_kernel<ET, TOKENS, true><<<grid, block, 0, s>>>((const ET*)p.x, (const ET*)p.Wg, p.gate_bias, (int)p.T, (int)p.M, (int)p.E, p.logits, p.counts);
+  else few_logits_kernel<ET, TOKENS, false><<<grid, block, 0, s>>>((const ET*)p.x, (const ET*)p.Wg, p.gate_bias, (int)p.T, (int)p.M, (int)p.E, p.logits, p.counts);
+}
+
+template <typename ET, bool W8, int C, bool UP> void launch_few_units(const FewTokens& p, hipStream_t s) {
+  const int64_t columns = ceil_div(UP ? p.H : p.M, 16 * C), reports = UP && !p.planned ? ceil_div(few_token_blocks(p), columns) : 0;
+  const dim3 grid((unsigned)columns, (unsigned)(few_units(p) + reports)), block(64 * kFewWaves);
+  if (p.T <= 16) few_kernel<ET, W8, C, 1, UP><<<grid, block, 0, s>>>(p);
+  else few_kernel<ET, W8, C, 4, UP><<<grid, block, 0, s>>>(p);
+}
+
+// Blocks of 64 columns where there are enough of them for three quarters of their places (two to a CU with one tile of rows, one with four), else of 32: more blocks, and more
+// places taken, for more reads of the rows.  Rows of 32 columns of bf16 weights are half a line of 128 bytes: always 64.
+// A layer of 8-bit weights, us with 64 and with 32 columns (blocks of a product with 64): 1 token x 2 experts of 4096 x 4096 (128) 42.4, 37.3;
+// 16 x 8 of 2048 x 2048 (256) 37.2, 35.1; 16 x 32 of 1024 x 1024 (512) 49.1, 64.0; 64 x 16 of 4096 x 1024 (256 and 1024) 152.8, 171.7; 24 x 4 of 768 x 512 (32 and 48) 23.1, 21.3.
+template <typename ET, bool W8, bool UP> void launch_few_product(const FewTokens& p, hipStream_t s) {
+  const int64_t blocks = ceil_div(UP ? p.H : p.M, 64) * few_units(p);
+  if constexpr (!W8 && sizeof(ET) == 2) launch_few_units<ET, W8, 4, UP>(p, s);
+  else if (blocks >= (p.T <= 16 ? 384 : 192)) launch_few_units<ET, W8, 4, UP>(p, s);
+  else launch_few_units<ET, W8, 2, UP>(p, s);
 }
 
 template <typename ET, bool W8> hipError_t launch_few(const FewTokens& p, hipStream_t s) {
-  if (p.slices > 0)
-    if (hipError_t err = launch_few_logits<ET>(p, s)) return err;
-  const unsigned experts = (unsigned)(p.E < p.T * p.k ? p.E : p.T * p.k);
-  few_kernel<ET, W8, true><<<dim3((unsigned)ceil_div(p.H, kFewColumns), experts), dim3(64 * kFewWaves), 0, s>>>(p);
+  if (p.T == 1) launch_few_logits<ET, 1>(p, s);
+  else launch_few_logits<ET, 4>(p, s);
   if (hipError_t err = hipGetLastError()) return err;
-  few_kernel<ET, W8, false><<<dim3((unsigned)ceil_div(p.M, kFewColumns), experts), dim3(64 * kFewWaves), 0, s>>>(p);
+  if (p.planned) {
+    few_plan_kernel<<<dim3((unsigned)(few_units(p) + few_token_blocks(p))), dim3(64 * kFewWaves), 0, s>>>(p);
+    if (hipError_t err = hipGetLastError()) return err;
+  }
+  launch_few_product<ET, W8, true>(p, s);
+  if (hipError_t err = hipGetLastError()) return err;
+  launch_few_product<ET, W8, false>(p, s);
   return hipGetLastError();
 }
 
 }  // namespace
 
-// Slices of the model dim that the fused gate sums its logits in: 0 where the gate runs its own kernels.
-int few_gate_slices(int64_t T, int64_t M, int64_t E, int k) {
-  if (T * E > kFewGateLogits || E > 512) return 0;
-  return (int)ceil_div(M, few_gate_slice(M, T, E));
-}
+size_t few_arrivals_bytes(int64_t M) { return (size_t)ceil_div(M, kFewArrival) * 4; }
 
-size_t few_arrivals_bytes(int64_t M) { return (size_t)ceil_div(M, kFewColumns) * 4; }
-
-hipError_t launch_few_tokens(const FewTokens& p, hipStream_t s) {
+hipError_t launch_few_tokens(const FewTokens& given, hipStream_t s) {
+  FewTokens p = given;
+  // The plan by every block of the first product for itself, or, where they do not all run at once (two to a CU, or one of more than 16 tokens), in a launch of its own.
+  // us, first and then: 16 tokens x 8 experts of 2048 x 2048 (256 blocks) 41.1, 42.8; 1 x 8 of 128 of 4096 x 1024, 8 bits (128) 42.3, 44.1; 4 x 8 of 64 of 1024 x 4096 (512)
+  // 44.2, 46.3; 16 x 64 of 128 of 1024 x 1024, 8 bits (1024) 61.2, 58.5; 64 x 64 of 1024 x 4096 (4096) 264.7, 213.8.
+  p.planned = ceil_div(p.H, 64) * few_units(p) > (p.T <= 16 ? 512 : 256);
+  p.expert_bits = p.token_bits = 0;                                 // as many threads to an expert, and to a token, as there are
+  while (p.expert_bits < 6 && (p.E << (p.expert_bits + 1)) <= 64 * kFewWaves) ++p.expert_bits;
+  while (p.token_bits < 6 && (p.T << (p.token_bits + 1)) <= 64 * kFewWaves) ++p.token_bits;
   if (p.dtype == MOE_F32) return p.s1 ? launch_few<float, true>(p, s) : launch_few<float, false>(p, s);
   return p.s1 ? launch_few<uint16_t, true>(p, s) : launch_few<uint16_t, false>(p, s);
 }

@@ -134,7 +134,8 @@ def _p(t: Optional[torch.Tensor]):
 
 
 def _stream():
-    return torch.cuda.current_stream().cuda_stream
+    # torch.cuda.current_stream().cuda_stream without the Stream object, which takes as long to make as a kernel to launch
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def capacity(T: int, E: int, k: int, f: float) -> int:

@@ -53,7 +53,10 @@ def magnitudes(x, r, W1, b1, W2, b2, act, C):
 CASES = [(1, 8, 8, 1, 1, 1.0, 0, 0, False), (1, 256, 512, 4, 1, 1.0, 0, 0, True), (1, 264, 136, 9, 3, 2.0, 2, 1, False), (2, 512, 256, 8, 8, 8.0, 1, 1, True),
          (5, 256, 512, 4, 1, 0.5, 1, 0, True), (16, 520, 776, 8, 2, 2.0, 1, 1, False), (17, 256, 264, 40, 4, 10.0, 2, 1, True), (33, 128, 384, 2, 2, 1.0, 2, 1, False),
          (64, 384, 640, 3, 1, 3.0, 1, 0, True), (64, 136, 256, 64, 8, 1.0, 0, 1, False), (48, 1024, 512, 8, 2, 0.3, 1, 1, True), (9, 2048, 1024, 16, 2, 2.0, 1, 1, False),
-         (64, 264, 128, 130, 2, 1.0, 1, 1, True), (3, 4096, 256, 5, 2, 2.0, 2, 0, False), (64, 256, 2056, 1, 1, 1.0, 2, 1, False)]
+         (64, 264, 128, 130, 2, 1.0, 1, 1, True), (3, 4096, 256, 5, 2, 2.0, 2, 0, False), (64, 256, 2056, 1, 1, 1.0, 2, 1, False),
+         # many blocks: with as many units as experts and with fewer, of up to 16 tokens and of more; many experts
+         (16, 264, 1096, 40, 4, 2.0, 1, 1, True), (64, 128, 520, 64, 2, 0.5, 2, 0, False), (12, 64, 1160, 70, 3, 4.0, 1, 1, False), (20, 64, 1160, 70, 3, 1.0, 0, 1, True),
+         (2, 520, 128, 512, 3, 100.0, 1, 1, False), (1, 1032, 136, 512, 1, 1.0, 2, 0, True)]
 
 
 @pytest.mark.parametrize("kind", ["bf16", "fp32", "8bit", "8bit_fp32"])
