@@ -552,6 +552,11 @@ def _check_storage(code: int, *tensors: Optional[torch.Tensor]) -> None:
             raise ValueError("tensors must share the storage dtype")
 
 
+def _check_out(t: Optional[torch.Tensor], shape, dtype: torch.dtype) -> None:
+    if t is not None and (t.dtype != dtype or tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"out: expected {list(shape)} in {dtype}")
+
+
 def _check_int32(t: Optional[torch.Tensor], *shape: int) -> None:
     if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != shape):
         raise ValueError(f"counts and indices must be int32 {list(shape)}")
@@ -569,7 +574,15 @@ def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float, residu
     if out is None:
         out = dict(h=torch.empty_like(x) if residual is not None else x, y=torch.empty_like(x) if want_y else None,
                    y8=_alloc8((), T, M, False, x.device) if want_8 else None)
-    h, y, y8 = out["h"], out["y"], out["y8"]
+        h, y, y8 = out["h"], out["y"], out["y8"]
+    else:
+        h, y, y8 = out["h"], out["y"], out["y8"]
+        for t in (h, y):
+            _check_out(t, x.shape, x.dtype)
+        if y8 is not None:
+            _check8(y8, "y8")
+            if y8.blocks or y8.width != M or y8.q.shape[:-1] != x.shape[:-1]:
+                raise ValueError("y8 must have x's shape and one exponent per row and block")
     _check(lib().moe_rms_norm(_p(x), _p(residual), _p(weight), eps, code, T, M, _p(h) if residual is not None else None, _p(y),
                               _p(y8.q) if y8 is not None else None, _p(y8.s) if y8 is not None else None, _stream()), "moe_rms_norm")
     return out
@@ -589,6 +602,9 @@ def rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: Optional[torch.
     ws = torch.empty((nbytes,), dtype=torch.uint8, device=h.device)
     if out is None:
         out = dict(dx=torch.empty_like(h), dweight=torch.empty((M,), dtype=h.dtype, device=h.device))
+    else:
+        _check_out(out["dx"], h.shape, h.dtype)
+        _check_out(out["dweight"], (M,), h.dtype)
     _check(lib().moe_rms_norm_backward(_p(dy), _p(dh), _p(h), _p(weight), eps, code, T, M, _p(ws), nbytes, _p(out["dx"]),
                                        _p(out["dweight"]), _stream()), "moe_rms_norm_backward")
     return out
@@ -633,6 +649,8 @@ def matmul8(A: Block8, B: Block8, bias: Optional[torch.Tensor] = None, act: int 
     _check_int32(gather, E, C)
     if out is None:
         out = (torch.empty if counts is None else torch.zeros)((E, C, N), dtype=dtype, device=B.q.device)
+    else:
+        _check_out(out, (E, C, N), out.dtype)
     _check_storage(_dtype_code(out), bias)
     _check(lib().moe_matmul8(_p(A.q), _p(A.s), _p(B.q), _p(B.s), SCALE_BLOCKS if B.blocks else SCALE_ROWS, _p(bias), act, _dtype_code(out),
                              _p(counts), _p(k_counts), _p(gather), A.q.shape[0] if gather is not None else 0, E, C, A.width, N, _p(out),

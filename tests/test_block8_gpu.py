@@ -141,7 +141,8 @@ def assert_product(got, ref, mags, K, dtype, what="product"):
 
 
 MATMULS = [(1, 1, 8, 8), (1, 3, 128, 16), (2, 17, 136, 40), (1, 129, 640, 136), (3, 256, 512, 256), (1, 300, 1032, 520), (2, 520, 264, 264), (5, 64, 1288, 1000),
-           (1, 1024, 2048, 512), (9, 40, 384, 1152)]
+           (1, 1024, 2048, 512), (9, 40, 384, 1152),
+           (24, 453, 1040, 776), (1, 2100, 8328, 4104), (1, 200, 8328, 264)]          # the large tile, with more exponents than LDS holds at a time; the small one with them
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
@@ -196,7 +197,7 @@ def test_matmul8_many_experts(moe):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("E,C,K,N,ragged", [(1, 8, 8, 8, False), (3, 37, 136, 264, True), (2, 300, 520, 392, True), (4, 256, 256, 512, False), (1, 1, 128, 128, False)])
+@pytest.mark.parametrize("E,C,K,N,ragged", [(1, 8, 8, 8, False), (3, 37, 136, 264, True), (2, 300, 520, 392, True), (4, 256, 256, 512, False), (1, 1, 128, 128, False), (17, 453, 776, 1544, True)])
 def test_linear8_training_pass(moe, E, C, K, N, ragged, dtype):
     """y, dx and dW from the operands as the format holds them, and the gradients against differences of <y, dy> (bilinear in the stored operands, so that a difference
     is exact but for its own roundings)."""
@@ -244,7 +245,7 @@ def ffn8_reference(z, W1, b1, W2, b2, act, hidden):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("E,C,M,H,T,act,bias", [(2, 5, 64, 136, 9, 0, True), (3, 70, 264, 520, 100, 1, True), (4, 300, 256, 384, 700, 2, False), (1, 513, 512, 1024, 513, 1, True)])
+@pytest.mark.parametrize("E,C,M,H,T,act,bias", [(2, 5, 64, 136, 9, 0, True), (3, 70, 264, 520, 100, 1, True), (4, 300, 256, 384, 700, 2, False), (1, 513, 512, 1024, 513, 1, True), (24, 453, 1040, 776, 900, 1, True)])
 def test_expert_ffn8(moe, E, C, M, H, T, act, bias, dtype):
     rng = np.random.default_rng(C + H)
     X, x = operand(moe, rng, 1, T, M, False, spread=1)
@@ -362,3 +363,19 @@ def test_refusals(moe):
         moe.quantize8(torch.zeros((4, 12), device="cuda"))
     with pytest.raises(ValueError):
         moe.expert_ffn8(q, w, None, w, None, 0)                    # W2 must be [E,M,H]
+
+
+def test_refuses_outputs_of_other_shapes(moe):
+    x, w = torch.ones((4, 256), device="cuda"), torch.ones(256, device="cuda")
+    out = moe.rms_norm(x, w, 1e-6, residual=x, want_8=True)
+    wide = moe.rms_norm(torch.ones((4, 512), device="cuda"), None, 1e-6, want_8=True)
+    for key, bad in [("h", x[:2]), ("y", x.bfloat16()), ("y8", wide["y8"])]:
+        with pytest.raises(ValueError):
+            moe.rms_norm(x, w, 1e-6, residual=x, out={**out, key: bad})
+    grads = moe.rms_norm_backward(x, x, w, 1e-6)
+    for key, bad in [("dx", x[:2]), ("dweight", w[:8])]:
+        with pytest.raises(ValueError):
+            moe.rms_norm_backward(x, x, w, 1e-6, out={**grads, key: bad})
+    A, B_ = moe.quantize8(torch.ones((1, 8, 128), device="cuda"))[0], moe.quantize8(torch.ones((1, 16, 128), device="cuda"))[0]
+    with pytest.raises(ValueError):
+        moe.matmul8(A, B_, out=torch.empty((1, 8, 8), device="cuda"))
