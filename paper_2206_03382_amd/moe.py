@@ -540,9 +540,9 @@ def _alloc8(lead: Tuple[int, ...], R: int, K: int, blocks: bool, device) -> Bloc
 
 
 def _check8(m: Block8, what: str) -> None:
-    R, row = m.q.shape[-2:]
-    scales = (*m.q.shape[:-2], -(-R // 128) if m.blocks else R, -(-m.width // 512) * 4)
-    if m.q.dtype != torch.float8_e4m3fn or m.s.dtype != torch.uint8 or row != -(-m.width // 128) * 128 or tuple(m.s.shape) != scales:
+    *lead, R, row = m.q.shape
+    if m.s.shape != (*lead, -(-R // 128) if m.blocks else R, -(-m.width // 512) * 4) or row != -(-m.width // 128) * 128 \
+            or m.q.dtype != torch.float8_e4m3fn or m.s.dtype != torch.uint8:
         raise ValueError(f"{what}: not a matrix in the 8-bit block format")
 
 
@@ -553,7 +553,7 @@ def _check_storage(code: int, *tensors: Optional[torch.Tensor]) -> None:
 
 
 def _check_out(t: Optional[torch.Tensor], shape, dtype: torch.dtype) -> None:
-    if t is not None and (t.dtype != dtype or tuple(t.shape) != tuple(shape)):
+    if t is not None and (t.dtype != dtype or t.shape != shape):
         raise ValueError(f"out: expected {list(shape)} in {dtype}")
 
 
@@ -577,12 +577,12 @@ def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float, residu
         h, y, y8 = out["h"], out["y"], out["y8"]
     else:
         h, y, y8 = out["h"], out["y"], out["y8"]
-        for t in (h, y):
-            _check_out(t, x.shape, x.dtype)
+        _check_out(h, x.shape, x.dtype)
+        _check_out(y, x.shape, x.dtype)
         if y8 is not None:
-            _check8(y8, "y8")
-            if y8.blocks or y8.width != M or y8.q.shape[:-1] != x.shape[:-1]:
+            if y8.blocks or y8.width != M or y8.s.shape != (T, -(-M // 512) * 4) or y8.s.dtype != torch.uint8:
                 raise ValueError("y8 must have x's shape and one exponent per row and block")
+            _check_out(y8.q, (T, -(-M // 128) * 128), torch.float8_e4m3fn)
     _check(lib().moe_rms_norm(_p(x), _p(residual), _p(weight), eps, code, T, M, _p(h) if residual is not None else None, _p(y),
                               _p(y8.q) if y8 is not None else None, _p(y8.s) if y8 is not None else None, _stream()), "moe_rms_norm")
     return out
