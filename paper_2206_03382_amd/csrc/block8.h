@@ -107,7 +107,7 @@ struct FewTokens {
   float *gate_w, *logits;
   int64_t T, M, H, E, C;
   int k, act, dtype, normalize;
-  bool planned;                   // set by launch_few_tokens, as are the next two
+  bool planned, alone;            // set by launch_few_tokens, as are the next two
   int expert_bits, token_bits;
   int32_t* plan;                  // [min(E, T k), kFewPlan]
   void* hidden;                   // [T k, H]

@@ -4,6 +4,8 @@
 // Reading the chosen experts' weights once is all the time there is (HBM bound), so each product is cut into units of one expert and 64 or 32 columns, a block
 // each: eight waves share the sum over k, every one with loads of several steps in flight, and meet in LDS.  The expert's rows, 16 to a tile, go
 // through the matrix cores together, whose 16 rows cost the same whether they are filled or not.
+#include <type_traits>
+
 #include "block8.h"
 #include "ffn_device.h"
 
@@ -344,6 +346,76 @@ __device__ __forceinline__ uint32_t ordered(float v) {              // -0 as +0
 }
 __device__ __forceinline__ float unordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
 
+// The logits of very few tokens and experts, by every block of the first product for itself: pieces of 2 tokens and 4 experts, each to one or more waves.  fp64 as above.
+constexpr int kAloneTokens = 8, kAloneExperts = 64;
+// Tokens x experts x model dim up to here: a launch less.  us of a layer with the logits' own launch and without: 5 x 4 x 256 (fp32) 16.8, 13.8; 2 x 4 x 768 20.4, 16.7;
+// 1 x 8 x 1024 17.5, 17.2; 1 x 8 x 2048 23.8, 23.9; 4 x 8 x 1024 19.7, 21.8; 8 x 8 x 1024 20.6, 26.5.
+constexpr int64_t kAloneWork = 1 << 13;
+struct FewAlone {
+  double sums[kAloneTokens / 2 * kAloneExperts / 4][8];
+  float logits[kAloneTokens * kAloneExperts];
+};
+__device__ __forceinline__ void load4(const float* p, float (&v)[4]) { Vec16<float>::unpack(*reinterpret_cast<const uint4*>(p), v); }
+__device__ __forceinline__ void load4(const uint16_t* p, float (&v)[4]) {
+  const uint2 w = *reinterpret_cast<const uint2*>(p);
+  v[0] = __uint_as_float(w.x << 16); v[1] = __uint_as_float(w.x & 0xffff0000u);
+  v[2] = __uint_as_float(w.y << 16); v[3] = __uint_as_float(w.y & 0xffff0000u);
+}
+struct FewNone {};
+__device__ __forceinline__ const float* few_logits_of(const FewTokens&, const FewAlone& s) { return s.logits; }
+__device__ __forceinline__ const float* few_logits_of(const FewTokens& p, const FewNone&) { return p.logits; }
+template <typename ET> __device__ __forceinline__ void few_alone_logits(const FewTokens& p, FewAlone& s) {
+  const int T = (int)p.T, E = (int)p.E, M = (int)p.M, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int across = (E + 3) / 4, pieces = (T + 1) / 2 * across, parts = pieces >= kFewWaves ? 1 : kFewWaves / pieces;
+  const ET *x = (const ET*)p.x, *Wg = (const ET*)p.Wg;
+  const bool vector = E % 4 == 0 && (reinterpret_cast<uintptr_t>(Wg) & 15) == 0;
+  for (int piece = wave / parts; piece < pieces; piece += kFewWaves / parts) {
+    const int t0 = piece / across * 2, e0 = piece % across * 4, t1 = t0 + 1 < T ? t0 + 1 : t0;
+    double sum[8] = {};
+    for (int m = (wave % parts * 64 + lane) * 4; m < M; m += parts * 256) {
+      float a[2][4], b[4][4];
+      load4(x + (int64_t)t0 * M + m, a[0]);
+      load4(x + (int64_t)t1 * M + m, a[1]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const ET* w = Wg + (int64_t)(m + r) * E + e0;
+        if (vector) load4(w, b[r]);
+        else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) b[r][j] = load_as_f32(w + min(j, E - 1 - e0));
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) sum[4 * i + j] += (double)a[i][r] * (double)b[r][j];
+    }
+    int at = 0;
+#pragma unroll
+    for (int half = 4, d = 1; d < 64; d <<= 1, half >>= 1) {        // as in few_logits_kernel
+      const bool upper = lane & d;
+      if (half == 0) sum[0] += __shfl_xor(sum[0], d);
+#pragma unroll
+      for (int i = 0; i < half; ++i) {
+        const double give = upper ? sum[i] : sum[i + half], keep = upper ? sum[i + half] : sum[i];
+        sum[i] = keep + __shfl_xor(give, d);
+      }
+      at += upper ? half : 0;
+    }
+    if (lane < 8) s.sums[piece * parts + wave % parts][at] = sum[0];
+  }
+  __syncthreads();
+  if (threadIdx.x < T * E) {
+    const int t = threadIdx.x / E, e = threadIdx.x % E;
+    double sum = p.gate_bias ? (double)p.gate_bias[e] : 0.0;
+    for (int u = 0; u < parts; ++u) sum += s.sums[((t >> 1) * across + (e >> 2)) * parts + u][(t & 1) * 4 + (e & 3)];
+    s.logits[threadIdx.x] = (float)sum;
+  }
+  __syncthreads();
+}
+
 // Units of work of both products: an expert each, or, where there are fewer choices than experts, a choice each, of which the first one to arrive at its expert does the work.
 __host__ __device__ __forceinline__ int few_units(const FewTokens& p) { return (int)(p.E < p.T * p.k ? p.E : p.T * p.k); }
 
@@ -352,9 +424,9 @@ struct FewRanks {
   uint32_t keys[kFewExperts];
   int rank[kFewExperts];
 };
-__device__ __forceinline__ void few_rank(const FewTokens& p, int t, FewRanks& s) {
+__device__ __forceinline__ void few_rank(const FewTokens& p, const float* logits, int t, FewRanks& s) {
   const int E = (int)p.E, group = 1 << p.expert_bits, sub = threadIdx.x & (group - 1), e = threadIdx.x >> p.expert_bits;     // threads to an expert, in one wave
-  if (threadIdx.x < E) s.keys[threadIdx.x] = ordered(p.logits[(int64_t)t * E + threadIdx.x]);
+  if (threadIdx.x < E) s.keys[threadIdx.x] = ordered(logits[t * E + threadIdx.x]);
   __syncthreads();
   int rank = 0;
   if (e < E) {
@@ -372,13 +444,13 @@ __device__ __forceinline__ void few_rank(const FewTokens& p, int t, FewRanks& s)
 
 // Tokens' choices and gate weights as the caller sees them: the b-th block has 8 tokens, a wave each, or, of more than 64 experts, one token.
 inline __host__ __device__ int few_token_blocks(const FewTokens& p) { return (int)(p.E <= 64 ? (p.T + kFewWaves - 1) / kFewWaves : p.T); }
-__device__ __forceinline__ void few_report(const FewTokens& p, int b, FewRanks& s) {
+__device__ __forceinline__ void few_report(const FewTokens& p, const float* logits, int b, FewRanks& s) {
   const int E = (int)p.E, k = p.k, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int t = b;
   if (E <= 64) {
     t = b * kFewWaves + wave;
     if (t >= p.T) return;
-    const uint32_t own = lane < E ? ordered(p.logits[(int64_t)t * E + lane]) : 0;
+    const uint32_t own = lane < E ? ordered(logits[t * E + lane]) : 0;
     int rank = 0;
     for (int o = 0; o < E; ++o) {
       const uint32_t other = (uint32_t)__builtin_amdgcn_readlane((int)own, o);
@@ -387,7 +459,7 @@ __device__ __forceinline__ void few_report(const FewTokens& p, int b, FewRanks& 
     if (lane < E) s.keys[wave * 64 + lane] = own;
     if (lane < E) s.rank[wave * 64 + lane] = rank;
   } else {
-    few_rank(p, t, s);
+    few_rank(p, logits, t, s);
     if (wave > 0) return;
   }
   const uint32_t* keys = s.keys + (E <= 64 ? wave * 64 : 0);
@@ -409,9 +481,9 @@ __device__ __forceinline__ void few_report(const FewTokens& p, int b, FewRanks& 
 }
 
 // The pairs (t, j) that expert e has, from the logits: a group of threads finds its rank for one token, and one wave the order of the arrivals: all first choices, all second ones ...
-__device__ __forceinline__ int few_own_rank(const FewTokens& p, int e) {
+__device__ __forceinline__ int few_own_rank(const FewTokens& p, const float* logits, int e) {
   const int E = (int)p.E, group = 1 << p.token_bits, sub = threadIdx.x & (group - 1), t = threadIdx.x >> p.token_bits;
-  const float* row = p.logits + (int64_t)(t < p.T ? t : 0) * E;
+  const float* row = logits + (t < p.T ? t : 0) * E;
   const uint32_t own = ordered(row[e]);
   int rank = 0;
   for (int o0 = sub; o0 < E; o0 += 4 * group) {
@@ -447,8 +519,8 @@ __device__ __forceinline__ int few_own_pairs(const FewTokens& p, int e, int rank
 }
 
 // The expert of choice o = j T + t.
-__device__ __forceinline__ int few_chosen(const FewTokens& p, int o, FewRanks& s, int* found) {
-  few_rank(p, o % (int)p.T, s);
+__device__ __forceinline__ int few_chosen(const FewTokens& p, const float* logits, int o, FewRanks& s, int* found) {
+  few_rank(p, logits, o % (int)p.T, s);
   if (threadIdx.x < p.E && s.rank[threadIdx.x] == o / (int)p.T) *found = threadIdx.x;
   __syncthreads();
   return __builtin_amdgcn_readfirstlane(*found);
@@ -470,21 +542,24 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_plan_kernel(const FewToken
   const int units = few_units(p);
   int e = blockIdx.x;
   if (e >= units) {
-    few_report(p, e - units, ranks);
+    few_report(p, p.logits, e - units, ranks);
     return;
   }
   if (e == 0)
     for (int64_t s = threadIdx.x; s < ceil_div(p.M, kFewArrival); s += 64 * kFewWaves) p.arrived[s] = 0;
   const bool direct = units == p.E;
-  if (!direct) e = few_chosen(p, blockIdx.x, ranks, &found);
-  const int n = few_own_pairs(p, e, few_own_rank(p, e), direct ? -1 : (int)blockIdx.x, true, arrivals, pair_of);
+  if (!direct) e = few_chosen(p, p.logits, blockIdx.x, ranks, &found);
+  const int n = few_own_pairs(p, e, few_own_rank(p, p.logits, e), direct ? -1 : (int)blockIdx.x, true, arrivals, pair_of);
   if (threadIdx.x < 64) few_write_plan(p.plan + (int64_t)blockIdx.x * kFewPlan, e, n, pair_of);
 }
 
 // Block x, y: 16 C columns of unit y's expert.
-// TILES: of 16 rows that an expert can have at most, 1 or 4; with 1 two blocks fit a CU.
-template <typename ET, bool W8, int C, int TILES, bool UP>
-__global__ __launch_bounds__(64 * kFewWaves, TILES == 1 ? 4 : 2) void few_kernel(const FewTokens p) {
+// TILES: of 16 rows that an expert can have at most, 1 or 4; with 1 two blocks fit a CU (not beside the logits, which would spill).  STAGE: the first product, from the logits or the plan; with the logits worked out by each
+// block itself; the second product.
+constexpr int kFewUp = 0, kFewUpAlone = 1, kFewDown = 2;
+template <typename ET, bool W8, int C, int TILES, int STAGE>
+__global__ __launch_bounds__(64 * kFewWaves, TILES == 1 && STAGE != kFewUpAlone ? 4 : 2) void few_kernel(const FewTokens p) {
+  constexpr bool UP = STAGE != kFewDown, ALONE = STAGE == kFewUpAlone;
   constexpr int kColumns = 16 * C, kSums = kFewWaves * 16 * (kColumns + 4);
   union Lds {
     FewRanks ranks;
@@ -495,14 +570,27 @@ __global__ __launch_bounds__(64 * kFewWaves, TILES == 1 ? 4 : 2) void few_kernel
   __shared__ int pair_of[kFewRows], found[2];
   __shared__ const ET* rows[kFewRows];
   __shared__ int last;
+  __shared__ typename std::conditional<ALONE, FewAlone, FewNone>::type alone;
+  const float* logits = few_logits_of(p, alone);
   const int64_t K = UP ? p.M : p.H, N = UP ? p.H : p.M, n0 = (int64_t)blockIdx.x * kColumns;
   const int units = few_units(p);
+  if constexpr (ALONE) few_alone_logits<ET>(p, alone);
   if constexpr (UP) {
     // The tokens' choices: rows of blocks after the others, the last to start, so that it is theirs to share a CU (16 tokens x 8 experts of 2048 x 2048, 256 + 8 blocks: 41.1 us,
     // and 45.8 with these among the others).
     if (blockIdx.y >= units) {
       const int b = (blockIdx.y - units) * gridDim.x + blockIdx.x;
-      if (b < few_token_blocks(p)) few_report(p, b, lds.ranks);
+      if (b >= few_token_blocks(p)) return;
+      few_report(p, logits, b, lds.ranks);
+      if constexpr (ALONE) {                                        // one block has all tokens
+        __syncthreads();
+        for (int q = threadIdx.x; q < p.T * p.E; q += 64 * kFewWaves) p.logits[q] = logits[q];
+        if (threadIdx.x < p.E) {
+          int n = 0;
+          for (int t = 0; t < p.T; ++t) n += lds.ranks.rank[t * 64 + threadIdx.x] < p.k ? 1 : 0;
+          p.counts[threadIdx.x] = n;
+        }
+      }
       return;
     }
     if (blockIdx.x == 0 && blockIdx.y == 0 && !p.planned)           // the arrivals of the next launch's blocks
@@ -518,8 +606,8 @@ __global__ __launch_bounds__(64 * kFewWaves, TILES == 1 ? 4 : 2) void few_kernel
   int unit_e = blockIdx.y, v = 0;
   if (planned) v = threadIdx.x < kFewPlan ? plan[threadIdx.x] : 0;
   else {
-    if (!direct) unit_e = few_chosen(p, blockIdx.y, lds.ranks, found);
-    v = few_own_rank(p, unit_e);
+    if (!direct) unit_e = few_chosen(p, logits, blockIdx.y, lds.ranks, found);
+    v = few_own_rank(p, logits, unit_e);
   }
   if (planned) {
     if (threadIdx.x < 2) found[threadIdx.x] = v;
@@ -599,35 +687,39 @@ template <typename ET, int TOKENS> void launch_few_logits(const FewTokens& p, hi
   else few_logits_kernel<ET, TOKENS, false><<<grid, block, 0, s>>>((const ET*)p.x, (const ET*)p.Wg, p.gate_bias, (int)p.T, (int)p.M, (int)p.E, p.logits, p.counts);
 }
 
-template <typename ET, bool W8, int C, bool UP> void launch_few_units(const FewTokens& p, hipStream_t s) {
+template <typename ET, bool W8, int C, int STAGE> void launch_few_units(const FewTokens& p, hipStream_t s) {
+  constexpr bool UP = STAGE != kFewDown;
   const int64_t columns = ceil_div(UP ? p.H : p.M, 16 * C), reports = UP && !p.planned ? ceil_div(few_token_blocks(p), columns) : 0;
   const dim3 grid((unsigned)columns, (unsigned)(few_units(p) + reports)), block(64 * kFewWaves);
-  if (p.T <= 16) few_kernel<ET, W8, C, 1, UP><<<grid, block, 0, s>>>(p);
-  else few_kernel<ET, W8, C, 4, UP><<<grid, block, 0, s>>>(p);
+  if (STAGE == kFewUpAlone || p.T <= 16) few_kernel<ET, W8, C, 1, STAGE><<<grid, block, 0, s>>>(p);
+  else if constexpr (STAGE != kFewUpAlone) few_kernel<ET, W8, C, 4, STAGE><<<grid, block, 0, s>>>(p);
 }
 
 // Blocks of 64 columns where there are enough of them for three quarters of their places (two to a CU with one tile of rows, one with four), else of 32: more blocks, and more
 // places taken, for more reads of the rows.  Rows of 32 columns of bf16 weights are half a line of 128 bytes: always 64.
 // A layer of 8-bit weights, us with 64 and with 32 columns (blocks of a product with 64): 1 token x 2 experts of 4096 x 4096 (128) 42.4, 37.3;
 // 16 x 8 of 2048 x 2048 (256) 37.2, 35.1; 16 x 32 of 1024 x 1024 (512) 49.1, 64.0; 64 x 16 of 4096 x 1024 (256 and 1024) 152.8, 171.7; 24 x 4 of 768 x 512 (32 and 48) 23.1, 21.3.
-template <typename ET, bool W8, bool UP> void launch_few_product(const FewTokens& p, hipStream_t s) {
-  const int64_t blocks = ceil_div(UP ? p.H : p.M, 64) * few_units(p);
-  if constexpr (!W8 && sizeof(ET) == 2) launch_few_units<ET, W8, 4, UP>(p, s);
-  else if (blocks >= (p.T <= 16 ? 384 : 192)) launch_few_units<ET, W8, 4, UP>(p, s);
-  else launch_few_units<ET, W8, 2, UP>(p, s);
+template <typename ET, bool W8, int STAGE> void launch_few_product(const FewTokens& p, hipStream_t s) {
+  const int64_t blocks = ceil_div(STAGE != kFewDown ? p.H : p.M, 64) * few_units(p);
+  if constexpr (!W8 && sizeof(ET) == 2) launch_few_units<ET, W8, 4, STAGE>(p, s);
+  else if (blocks >= (p.T <= 16 ? 384 : 192)) launch_few_units<ET, W8, 4, STAGE>(p, s);
+  else launch_few_units<ET, W8, 2, STAGE>(p, s);
 }
 
 template <typename ET, bool W8> hipError_t launch_few(const FewTokens& p, hipStream_t s) {
-  if (p.T == 1) launch_few_logits<ET, 1>(p, s);
-  else launch_few_logits<ET, 4>(p, s);
-  if (hipError_t err = hipGetLastError()) return err;
-  if (p.planned) {
-    few_plan_kernel<<<dim3((unsigned)(few_units(p) + few_token_blocks(p))), dim3(64 * kFewWaves), 0, s>>>(p);
+  if (p.alone) launch_few_product<ET, W8, kFewUpAlone>(p, s);
+  else {
+    if (p.T == 1) launch_few_logits<ET, 1>(p, s);
+    else launch_few_logits<ET, 4>(p, s);
     if (hipError_t err = hipGetLastError()) return err;
+    if (p.planned) {
+      few_plan_kernel<<<dim3((unsigned)(few_units(p) + few_token_blocks(p))), dim3(64 * kFewWaves), 0, s>>>(p);
+      if (hipError_t err = hipGetLastError()) return err;
+    }
+    launch_few_product<ET, W8, kFewUp>(p, s);
   }
-  launch_few_product<ET, W8, true>(p, s);
   if (hipError_t err = hipGetLastError()) return err;
-  launch_few_product<ET, W8, false>(p, s);
+  launch_few_product<ET, W8, kFewDown>(p, s);
   return hipGetLastError();
 }
 
@@ -641,6 +733,7 @@ hipError_t launch_few_tokens(const FewTokens& given, hipStream_t s) {
   // us, first and then: 16 tokens x 8 experts of 2048 x 2048 (256 blocks) 41.1, 42.8; 1 x 8 of 128 of 4096 x 1024, 8 bits (128) 42.3, 44.1; 4 x 8 of 64 of 1024 x 4096 (512)
   // 44.2, 46.3; 16 x 64 of 128 of 1024 x 1024, 8 bits (1024) 61.2, 58.5; 64 x 64 of 1024 x 4096 (4096) 264.7, 213.8.
   p.planned = ceil_div(p.H, 64) * few_units(p) > (p.T <= 16 ? 512 : 256);
+  p.alone = !p.planned && p.T <= kAloneTokens && p.E <= kAloneExperts && p.T * p.E * p.M <= kAloneWork;
   p.expert_bits = p.token_bits = 0;                                 // as many threads to an expert, and to a token, as there are
   while (p.expert_bits < 6 && (p.E << (p.expert_bits + 1)) <= 64 * kFewWaves) ++p.expert_bits;
   while (p.token_bits < 6 && (p.T << (p.token_bits + 1)) <= 64 * kFewWaves) ++p.token_bits;
