@@ -267,10 +267,11 @@ bool large_covers(const Matmul8& p) {
 }
 
 hipError_t launch_large(const Matmul8& p, hipStream_t s) {
-  // Operands and results beyond the 256 MB of the last-level cache: stores that leave no line behind keep the operands there (128 experts x 2048 rows, 1024 x 4096 1480 -> 1340 us, 8 x
-  // 4096, 4096 x 2048 222 -> 203).  Below, whoever reads the results next finds them (and the product itself is 2 % faster).
+  // Stores that leave no line behind, where operands and results are 96 MB or more of the 256 MB that the last-level cache has: what the program reads before and after a product is in
+  // there too.  A training pass of 8 experts x 4096 rows, 2048 x 2048 (235 MB a product) 524 -> 482 us, x 2048 rows (134 MB) 284 -> 275, 64 x 512, 1024 x 1024 (168 MB) 272 -> 250,
+  // 8 x 1024, 2048 x 2048 (84 MB) 167 -> 169; a product of 128 x 2048, 1024 x 4096 1480 -> 1340.
   const int64_t row8 = row_bytes8(p.K), rows = p.counts && p.rows_hint && p.rows_hint < p.C ? p.rows_hint : p.C;
-  const bool stream = p.E * (rows * row8 + p.N * row8 + rows * p.N * (p.out ? 2 : 1)) > ((int64_t)256 << 20);
+  const bool stream = p.E * (rows * row8 + p.N * row8 + rows * p.N * (p.out ? 2 : 1)) >= ((int64_t)96 << 20);
   Args8 a = {p, row8, row_scales8(p.K), row_bytes8(p.N), row_scales8(p.N), (int)ceil_div(p.C, kBig), (int)ceil_div(p.N, kBig), 0, stream};
   const int64_t all = p.E * p.C, total = p.counts && p.rows_hint ? (p.E * p.rows_hint < all ? p.E * p.rows_hint : all) : all;
   const dim3 grid((unsigned)tile_grid(a.NT, live_row_tiles(p.E, p.C, total, kBig), true)), block(256);
