@@ -2,7 +2,8 @@
 //   h = x + residual;  y = h * r * w,  r = 1 / sqrt(mean(h^2) + eps);  the row's statistics and y from the fp32 sum, before h is rounded.
 //   backward, g = dy * w:  dx = r * (g - h * r^2 * mean(g * h)) + dh;  dw = sum over the rows of dy * h * r.
 // One pass: a row stays in the registers of 64, 256 or 1024 lanes between the reduction and its use.  HBM bound: every input is read once with
-// 16-byte loads and every output written once.
+// 16-byte loads and every output written once.  131072 x 4096 in bf16 with a residual, h and y: 737 us = 5.8 TB/s (a copy 5.2); 32768 x 4096 backward with the residual's gradient
+// 203 us = 5.3 TB/s; 16 x 4096 with the 8-bit output as well 4 us, a launch and a row's latency.
 #include "block8.h"
 
 namespace moe {
@@ -214,16 +215,23 @@ __global__ __launch_bounds__(1024) void weight_sum_kernel(const float* __restric
   }
 }
 
-// Lanes to a row of so many 16-byte pieces.  A wave alone needs no barrier and takes rows of up to four pieces a lane; few rows are spread over
-// more lanes, since there the time is a row's own latency.
-inline int lanes_of(int64_t pieces, int64_t T) {
-  if (pieces <= 64 || (pieces <= 256 && T >= 2048)) return 64;
+// Lanes to a row of so many 16-byte pieces.  A wave alone needs no barrier; more lanes have a shorter row, which is all the time that few rows take.
+// us with 64 and with 256 lanes, bf16 with a residual: widths of 512 (64 pieces) 16 rows 2.9, 3.0, 4096 4.7, 7.0, 65536 49, 72; 1024 16 rows 3.6, 3.0, 4096 7.7, 9.4, 65536 110, 107;
+// 2048 16 rows 4.9, 3.0, 4096 14.0, 15.8, 65536 221, 202.
+inline int forward_lanes(int64_t pieces, int64_t T) {
+  if (pieces <= 64 || (pieces <= 128 && T >= 2048)) return 64;
+  return pieces <= 1024 ? 256 : 1024;
+}
+// Backward, where rows of fewer lanes are in more slots, whose sums for dw are written and read again: widths of 512 4096 rows 19.7, 12.0, 16384 27.8, 34.9, 65536 54, 121;
+// 1024 4096 rows 26.6, 14.4, 16384 38, 41, 65536 92, 134; 2048 4096 rows 35, 21, 65536 190, 168.
+inline int backward_lanes(int64_t pieces, int64_t T) {
+  if (pieces <= 128 && T >= 16384) return 64;
   return pieces <= 1024 ? 256 : 1024;
 }
 constexpr int64_t kBackwardSlots = 1024;                            // of 256 lanes: four blocks to a unit
 
 inline int64_t backward_slots(int64_t pieces, int64_t T) {
-  const int lanes = lanes_of(pieces, T);
+  const int lanes = backward_lanes(pieces, T);
   const int64_t per_block = lanes < 256 ? 256 / lanes : 1;
   const int64_t most = kBackwardSlots * 256 / lanes;
   return ceil_div(T < most ? T : most, per_block) * per_block;
@@ -236,8 +244,7 @@ inline int64_t backward_slots(int64_t pieces, int64_t T) {
     const int64_t vpl = ceil_div(pieces, lanes);                       \
     if (lanes == 64) {                                                 \
       if (vpl <= 1) CALL(ET, 64, 1);                                   \
-      else if (vpl <= 2) CALL(ET, 64, 2);                              \
-      else CALL(ET, 64, 4);                                            \
+      else CALL(ET, 64, 2);                                            \
     } else if (lanes == 256) {                                         \
       if (vpl <= 1) CALL(ET, 256, 1);                                  \
       else if (vpl <= 2) CALL(ET, 256, 2);                             \
@@ -252,7 +259,7 @@ hipError_t launch_rms_norm(const void* x, const void* residual, const void* weig
                            void* y, void* q, uint8_t* scales, hipStream_t s) {
   const int n = dtype == MOE_F32 ? 4 : 8;
   const int64_t row8 = row_bytes8(M), pieces = ceil_div(q ? row8 : M, n);
-  const int lanes = lanes_of(pieces, T);
+  const int lanes = forward_lanes(pieces, T);
   const dim3 block(lanes < 256 ? 256 : lanes), grid((unsigned)ceil_div(T, block.x / lanes));
 #define MOE_NORM(ET, L, V)                                                                                                            \
   rms_norm_kernel<ET, L, V><<<grid, block, 0, s>>>((const ET*)x, (const ET*)residual, (const ET*)weight, eps, T, (int)M, (ET*)h, (ET*)y, \
@@ -271,7 +278,7 @@ size_t rms_norm_backward_workspace_bytes(int64_t T, int64_t M) {
 hipError_t launch_rms_norm_backward(const void* dy, const void* dh, const void* h, const void* weight, float eps, int dtype, int64_t T,
                                     int64_t M, float* ws, void* dx, void* dweight, hipStream_t s) {
   const int64_t pieces = M / (dtype == MOE_F32 ? 4 : 8);
-  const int lanes = lanes_of(pieces, T);
+  const int lanes = backward_lanes(pieces, T);
   const int64_t slots = backward_slots(pieces, T);
   const dim3 block(lanes < 256 ? 256 : lanes), grid((unsigned)(slots * lanes / block.x));
   float* partial = dweight ? ws : nullptr;

