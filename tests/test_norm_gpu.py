@@ -38,7 +38,7 @@ def assert_within(got, ref, bound, what):
     assert over.max() <= 0, f"{what}: {np.abs(got - ref).max():.3e} off, {over.max():.3e} beyond the bound"
 
 
-SHAPES = [(1, 8), (1, 4096), (3, 264), (5, 128), (7, 776), (16, 2048), (33, 520), (64, 1024), (300, 1000), (2, 16384), (3, 8200), (2100, 256), (2053, 2040), (2049, 4096), (17, 6144)]
+SHAPES = [(1, 8), (1, 4096), (3, 264), (5, 128), (7, 776), (16, 2048), (33, 520), (64, 1024), (300, 1000), (2, 16384), (3, 8200), (2100, 256), (2053, 2040), (2049, 4096), (17, 6144), (2100, 776)]
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
@@ -84,7 +84,7 @@ def assert_format(m, ref, slack):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("T,M", SHAPES + [(1500, 512), (5000, 264)])
+@pytest.mark.parametrize("T,M", SHAPES + [(1500, 512), (5000, 264), (16500, 776), (16400, 264)])
 def test_rms_norm_backward(moe, T, M, dtype):
     rng = np.random.default_rng(T * 5 + M)
     h, h64 = draw(rng, (T, M), dtype, 1.5)
