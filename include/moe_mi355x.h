@@ -384,6 +384,18 @@ int moe_matmul8(const void* A, const uint8_t* A_scales, const void* B, const uin
                 int dtype, const int32_t* counts, const int32_t* k_counts, const int32_t* gather, int64_t gather_rows, int64_t E, int64_t C,
                 int64_t K, int64_t N, void* out, void* out8, uint8_t* out8_scales, void* stream);
 
+/* A projection of the experts in 8 bits, trained: y[e] = q(x[e]) q(W[e]), and from dy its gradients dx[e] = q(dy[e]) q(W[e])^T, dW[e] = q(x[e]^T) q(dy[e]^T)^T, every operand
+ * quantised along the axis that its product sums over (W once, with an exponent for 128 x 128 values).
+ *   x, dx [E,C,K], W, dW [E,K,N], y, dy [E,C,N] in `dtype`; K and N multiples of 8; dx or dW may be NULL.
+ *   counts [E] int32 or NULL: only the first min(counts[e], C) rows of x and dy are read; the others of y and dx are zeros.
+ *   state: moe_expert_linear8_state_bytes (0: unsupported) bytes, 256-byte aligned, the same for both calls; its layout is private, and one state serves one call at a time.  The
+ *   backward may be called more than once. */
+size_t moe_expert_linear8_state_bytes(int64_t E, int64_t C, int64_t K, int64_t N);
+int moe_expert_linear8_train(const void* x, const void* W, int dtype, const int32_t* counts, int64_t E, int64_t C, int64_t K, int64_t N, void* y, void* state,
+                             size_t state_bytes, void* stream);
+int moe_expert_linear8_backward(const void* dy, int dtype, const int32_t* counts, int64_t E, int64_t C, int64_t K, int64_t N, void* state, size_t state_bytes,
+                                void* dx, void* dW, void* stream);
+
 /* moe_expert_ffn (or, with slot_src, moe_expert_ffn_gather) on 8-bit tokens and weights:
  *   Y[e] = act(Z[e] W1[e] + b1[e]) W2[e] + b2[e], the activations rounded once, to the 8-bit format (hidden8, hidden_scales: scratch).
  *   x8 / x_scales: Z [E,C,M], or with slot_src [E,C] the tokens [T,M]; W1 as [E,H,M], W2 as [E,M,H] (moe_quantize8's transposed form of [E,M,H] and

@@ -96,6 +96,39 @@ int layer_shape_status(int64_t T, int64_t M, int64_t H, int64_t E, int k, int dt
   return row_shape_status(H);
 }
 
+// A projection's training pass: what the forward keeps (x transposed, W as it is), and behind it what one call needs for itself (forward: x, W transposed; backward: dy in both forms).
+struct Linear8State {
+  size_t xt, xt_scales, W, W_scales, x, x_scales, Wt, Wt_scales, dy, dy_scales, dyt, dyt_scales, total;
+};
+
+Linear8State linear8_layout(int64_t E, int64_t C, int64_t K, int64_t N) {
+  Linear8State w;
+  size_t off = 0;
+  auto rows = [&](size_t& q, size_t& scales, int64_t R, int64_t width, bool blocks) {
+    q = off;
+    off = align_up(off + (size_t)E * R * row_bytes8(width), 256);
+    scales = off;
+    off = align_up(off + (size_t)E * (blocks ? ceil_div(R, kBlock8) : R) * row_scales8(width), 256);
+  };
+  rows(w.xt, w.xt_scales, K, C, false);
+  rows(w.W, w.W_scales, K, N, true);
+  const size_t kept = off;
+  rows(w.x, w.x_scales, C, K, false);
+  rows(w.Wt, w.Wt_scales, N, K, true);
+  w.total = off;
+  off = kept;
+  rows(w.dy, w.dy_scales, C, N, false);
+  rows(w.dyt, w.dyt_scales, N, C, false);
+  w.total = off > w.total ? off : w.total;
+  return w;
+}
+
+int linear8_status(int64_t E, int64_t C, int64_t K, int64_t N) {
+  for (int st : {matrix8_status(E, C, K), matrix8_status(E, K, N), matrix8_status(E, C, N), weights8_status(K, N), weights8_status(N, K), weights8_status(C, N)})
+    if (st) return st;
+  return MOE_OK;
+}
+
 // The two products of the experts' layer; the first one's rows are gathered from x8 if slot_src is given.
 hipError_t run_ffn8(const void* x8, const uint8_t* xs, const int32_t* slot_src, int64_t T, const void* W1, const uint8_t* s1, const void* b1,
                     const void* W2, const uint8_t* s2, const void* b2, int act, int dtype, const int32_t* counts, int64_t E, int64_t C,
@@ -182,6 +215,46 @@ int moe_expert_ffn8(const void* x8, const uint8_t* x_scales, const int32_t* slot
     return MOE_UNSUPPORTED;
   return status_of(run_ffn8(x8, x_scales, slot_src, T, W1, s1, b1, W2, s2, b2, act, dtype, counts, E, C, M, H, 0, hidden8, hidden_scales, Y,
                             (hipStream_t)stream));
+}
+
+size_t moe_expert_linear8_state_bytes(int64_t E, int64_t C, int64_t K, int64_t N) {
+  return linear8_status(E, C, K, N) == MOE_OK ? linear8_layout(E, C, K, N).total : 0;
+}
+
+int moe_expert_linear8_train(const void* x, const void* W, int dtype, const int32_t* counts, int64_t E, int64_t C, int64_t K, int64_t N, void* y, void* state,
+                             size_t state_bytes, void* stream) {
+  if (!x || !W || !y || !state || !dtype_ok(dtype)) return MOE_INVALID_ARG;
+  if (int st = linear8_status(E, C, K, N)) return st;
+  if (!all_aligned16({x, W, y}) || !aligned(state, 256)) return MOE_UNSUPPORTED;
+  const Linear8State w = linear8_layout(E, C, K, N);
+  if (state_bytes < w.total) return MOE_WORKSPACE_TOO_SMALL;
+  uint8_t* b = (uint8_t*)state;
+  const hipStream_t s = (hipStream_t)stream;
+  if (launch_quantize8(x, dtype, counts, E, C, K, false, b + w.x, b + w.x_scales, b + w.xt, b + w.xt_scales, s) != hipSuccess ||
+      launch_quantize8(W, dtype, nullptr, E, K, N, true, b + w.W, b + w.W_scales, b + w.Wt, b + w.Wt_scales, s) != hipSuccess ||
+      (counts && launch_zero_past(y, dtype, counts, E, C, N, s) != hipSuccess))
+    return MOE_HIP_ERROR;
+  const Matmul8 p = {b + w.x, b + w.x_scales, b + w.Wt, b + w.Wt_scales, 1, nullptr, MOE_ACT_NONE, counts, nullptr, nullptr, 0, E, C, K, N, 0, dtype, y, nullptr, nullptr};
+  return status_of(launch_matmul8(p, s));
+}
+
+int moe_expert_linear8_backward(const void* dy, int dtype, const int32_t* counts, int64_t E, int64_t C, int64_t K, int64_t N, void* state, size_t state_bytes,
+                                void* dx, void* dW, void* stream) {
+  if (!dy || !state || (!dx && !dW) || !dtype_ok(dtype)) return MOE_INVALID_ARG;
+  if (int st = linear8_status(E, C, K, N)) return st;
+  if (!all_aligned16({dy, dx, dW}) || !aligned(state, 256)) return MOE_UNSUPPORTED;
+  const Linear8State w = linear8_layout(E, C, K, N);
+  if (state_bytes < w.total) return MOE_WORKSPACE_TOO_SMALL;
+  uint8_t* b = (uint8_t*)state;
+  const hipStream_t s = (hipStream_t)stream;
+  if (launch_quantize8(dy, dtype, counts, E, C, N, false, dx ? b + w.dy : nullptr, dx ? b + w.dy_scales : nullptr, dW ? b + w.dyt : nullptr,
+                       dW ? b + w.dyt_scales : nullptr, s) != hipSuccess ||
+      (dx && counts && launch_zero_past(dx, dtype, counts, E, C, K, s) != hipSuccess))
+    return MOE_HIP_ERROR;
+  const Matmul8 px = {b + w.dy, b + w.dy_scales, b + w.W, b + w.W_scales, 1, nullptr, MOE_ACT_NONE, counts, nullptr, nullptr, 0, E, C, N, K, 0, dtype, dx, nullptr, nullptr};
+  if (dx && launch_matmul8(px, s) != hipSuccess) return MOE_HIP_ERROR;
+  const Matmul8 pw = {b + w.xt, b + w.xt_scales, b + w.dyt, b + w.dyt_scales, 0, nullptr, MOE_ACT_NONE, nullptr, counts, nullptr, 0, E, K, C, N, 0, dtype, dW, nullptr, nullptr};
+  return dW ? status_of(launch_matmul8(pw, s)) : MOE_OK;
 }
 
 size_t moe_layer8_workspace_bytes(int64_t T, int64_t M, int64_t H, int64_t E, int k, int64_t C, int dtype) {

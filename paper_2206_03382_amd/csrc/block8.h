@@ -78,6 +78,9 @@ hipError_t launch_quantize8(const void* src, int dtype, const int32_t* counts, i
 hipError_t launch_dequantize8(const void* q, const uint8_t* scales, bool blocks, int64_t E, int64_t R, int64_t K, int dtype, void* out,
                               hipStream_t s);
 
+// zeros in the rows of out [E, C, N] from counts[e] on
+hipError_t launch_zero_past(void* out, int dtype, const int32_t* counts, int64_t E, int64_t C, int64_t N, hipStream_t s);
+
 // out[e] (rows_e x N) = act(A[e] (rows_e x K) * B[e]^T + bias[e]), B [E, N, K]; A and B in the 8-bit format with blocks along K.
 struct Matmul8 {
   const void* A;

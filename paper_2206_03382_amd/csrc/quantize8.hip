@@ -172,7 +172,20 @@ __global__ __launch_bounds__(256) void dequantize8_kernel(const uint8_t* __restr
   }
 }
 
+// 16 bytes a lane and turn, behind an expert's last row
+__global__ __launch_bounds__(256) void zero_past_kernel(uint4* __restrict__ out, const int32_t* __restrict__ counts, int C, int64_t row_pieces) {
+  const int64_t e = blockIdx.y, end = C * row_pieces;
+  for (int64_t i = live_rows(e, C, counts) * row_pieces + (int64_t)blockIdx.x * 256 + threadIdx.x; i < end; i += (int64_t)gridDim.x * 256)
+    out[e * end + i] = make_uint4(0, 0, 0, 0);
+}
+
 }  // namespace
+
+hipError_t launch_zero_past(void* out, int dtype, const int32_t* counts, int64_t E, int64_t C, int64_t N, hipStream_t s) {
+  const int64_t row_pieces = N * (dtype == MOE_F32 ? 4 : 2) / 16, blocks = ceil_div(C * row_pieces, 4 * 256);
+  zero_past_kernel<<<dim3((unsigned)(blocks < 256 ? blocks : 256), (unsigned)E), dim3(256), 0, s>>>((uint4*)out, counts, (int)C, row_pieces);
+  return hipGetLastError();
+}
 
 hipError_t launch_quantize8(const void* src, int dtype, const int32_t* counts, int64_t E, int64_t R, int64_t K, bool blocks, void* q,
                             uint8_t* scales, void* qt, uint8_t* scales_t, hipStream_t s) {

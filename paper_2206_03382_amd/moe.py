@@ -76,6 +76,9 @@ SIGNATURES = {
     "moe_quantize8": (_i32, [_vp, _i32, _vp, _i64, _i64, _i64, _i32, _vp, _vp, _vp, _vp, _vp]),
     "moe_dequantize8": (_i32, [_vp, _vp, _i32, _i64, _i64, _i64, _i32, _vp, _vp]),
     "moe_matmul8": (_i32, [_vp, _vp, _vp, _vp, _i32, _vp, _i32, _i32, _vp, _vp, _vp, _i64, _i64, _i64, _i64, _i64, _vp, _vp, _vp, _vp]),
+    "moe_expert_linear8_state_bytes": (_sz, [_i64, _i64, _i64, _i64]),
+    "moe_expert_linear8_train": (_i32, [_vp, _vp, _i32, _vp, _i64, _i64, _i64, _i64, _vp, _vp, _sz, _vp]),
+    "moe_expert_linear8_backward": (_i32, [_vp, _i32, _vp, _i64, _i64, _i64, _i64, _vp, _sz, _vp, _vp, _vp]),
     "moe_expert_ffn8": (_i32, [_vp, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _vp, _i64, _i64, _i64, _i64, _vp, _vp, _vp, _vp]),
     "moe_layer8_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64, _i32, _i64, _i32]),
     "moe_layer_forward8": (_i32, [_vp] * 11 + [_i64, _i64, _i64, _i64, _i32, _dbl, _i32, _i32, _i32] + [_vp] * 7 + [_sz, _vp]),
@@ -658,19 +661,43 @@ def matmul8(A: Block8, B: Block8, bias: Optional[torch.Tensor] = None, act: int 
     return out
 
 
-def expert_linear8_train(x: torch.Tensor, W: torch.Tensor, counts: Optional[torch.Tensor] = None):
+class Linear8Kept(NamedTuple):
+    """What expert_linear8_backward needs of the forward."""
+    state: torch.Tensor
+    counts: Optional[torch.Tensor]
+    shape: Tuple[int, int, int, int]                           # E, C, K, N
+    dtype: torch.dtype
+
+
+def expert_linear8_train(x: torch.Tensor, W: torch.Tensor, counts: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Linear8Kept]:
     """One projection of the experts in 8 bits for a training step: y[e] = x[e] W[e] (x [E,C,K], W [E,K,N]), and what the backward needs of
-    them.  Every operand is quantised along the axis that its product sums over; W's blocks serve both directions."""
-    x8, xt8 = quantize8(x, rows=True, transposed=True, counts=counts)
-    W8, Wt8 = quantize8(W, blocks=True, rows=True, transposed=True)
-    return matmul8(x8, Wt8, dtype=x.dtype, counts=counts), (xt8, W8, counts)
+    them.  Every operand is quantised along the axis that its product sums over; W's blocks serve both directions.  Rows past an expert's count are zero."""
+    E, C, K = x.shape
+    N = W.shape[-1]
+    if W.shape != (E, K, N):
+        raise ValueError("x must be [E,C,K] and W [E,K,N]")
+    code = _dtype_code(x)
+    _check_storage(code, W)
+    _check_int32(counts, E)
+    nbytes = lib().moe_expert_linear8_state_bytes(E, C, K, N)
+    if nbytes == 0:
+        raise MoEError(UNSUPPORTED, "moe_expert_linear8_state_bytes")
+    dev = x.device
+    state, y = torch.empty((nbytes,), dtype=torch.uint8, device=dev), torch.empty((E, C, N), dtype=x.dtype, device=dev)
+    _check(lib().moe_expert_linear8_train(_p(x), _p(W), code, _p(counts), E, C, K, N, _p(y), _p(state), nbytes, _stream()), "moe_expert_linear8_train")
+    return y, Linear8Kept(state, counts, (E, C, K, N), x.dtype)
 
 
-def expert_linear8_backward(dy: torch.Tensor, kept) -> Tuple[torch.Tensor, torch.Tensor]:
+def expert_linear8_backward(dy: torch.Tensor, kept: Linear8Kept) -> Tuple[torch.Tensor, torch.Tensor]:
     """(dx, dW) of expert_linear8_train from dy [E,C,N] and what it kept."""
-    xt8, W8, counts = kept
-    dy8, dyt8 = quantize8(dy, rows=True, transposed=True, counts=counts)
-    return matmul8(dy8, W8, dtype=dy.dtype, counts=counts), matmul8(xt8, dyt8, dtype=dy.dtype, k_counts=counts)
+    E, C, K, N = kept.shape
+    if dy.shape != (E, C, N) or dy.dtype != kept.dtype:
+        raise ValueError("dy must have y's shape and type")
+    dev = dy.device
+    dx, dW = torch.empty((E, C, K), dtype=dy.dtype, device=dev), torch.empty((E, K, N), dtype=dy.dtype, device=dev)
+    _check(lib().moe_expert_linear8_backward(_p(dy), _dtype_code(dy), _p(kept.counts), E, C, K, N, _p(kept.state), kept.state.numel(), _p(dx), _p(dW),
+                                             _stream()), "moe_expert_linear8_backward")
+    return dx, dW
 
 
 def _check_ffn8(W1: Block8, b1, W2: Block8, b2, code: int) -> Tuple[int, int, int]:
@@ -699,10 +726,12 @@ def expert_ffn8(x8: Block8, W1: Block8, b1: Optional[torch.Tensor], W2: Block8, 
         raise ValueError("x8 must be [E,C,M], or [T,M] with slot_src [E,C]")
     _check_int32(counts, E)
     _check_int32(slot_src, E, C)
-    hidden = _alloc8((E,), C, H, False, dev)
+    row, sc = -(-H // 128) * 128, -(-H // 512) * 4             # moe_row_bytes8, moe_row_scales8
+    hidden = torch.empty((E * C * (row + sc),), dtype=torch.uint8, device=dev)
+    h = hidden.data_ptr()
     Y = torch.empty((E, C, M), dtype=dtype, device=dev)
     _check(lib().moe_expert_ffn8(_p(x8.q), _p(x8.s), _p(slot_src), x8.q.shape[0] if slot_src is not None else 0, _p(W1.q), _p(W1.s), _p(b1),
-                                 _p(W2.q), _p(W2.s), _p(b2), act, _dtype_code(Y), _p(counts), E, C, M, H, _p(hidden.q), _p(hidden.s), _p(Y),
+                                 _p(W2.q), _p(W2.s), _p(b2), act, _dtype_code(Y), _p(counts), E, C, M, H, h, h + E * C * row, _p(Y),
                                  _stream()), "moe_expert_ffn8")
     return Y
 

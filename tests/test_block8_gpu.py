@@ -379,3 +379,51 @@ def test_refuses_outputs_of_other_shapes(moe):
     A, B_ = moe.quantize8(torch.ones((1, 8, 128), device="cuda"))[0], moe.quantize8(torch.ones((1, 16, 128), device="cuda"))[0]
     with pytest.raises(ValueError):
         moe.matmul8(A, B_, out=torch.empty((1, 8, 8), device="cuda"))
+
+
+@pytest.mark.parametrize("counts", [None, [0, 5, 40, 900]])
+def test_linear8_is_its_pieces(moe, counts):
+    """The training pass is the quantisations and products that a caller could make one by one, bit for bit; either gradient alone is the same."""
+    E, C, K, N = 4, 300, 200, 328
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x, W, dy = (torch.randn(s, generator=g, device="cuda").bfloat16() for s in ((E, C, K), (E, K, N), (E, C, N)))
+    n = None if counts is None else torch.tensor(counts, dtype=torch.int32, device="cuda")
+    y, kept = moe.expert_linear8_train(x, W, counts=n)
+    dx, dW = moe.expert_linear8_backward(dy, kept)
+    x8, xt8 = moe.quantize8(x, transposed=True, counts=n)
+    W8, Wt8 = moe.quantize8(W, blocks=True, transposed=True)
+    dy8, dyt8 = moe.quantize8(dy, transposed=True, counts=n)
+    assert torch.equal(y, moe.matmul8(x8, Wt8, counts=n)) and torch.equal(dx, moe.matmul8(dy8, W8, counts=n)) and torch.equal(dW, moe.matmul8(xt8, dyt8, k_counts=n))
+    for alone in (0, 1):
+        out = [torch.full_like(dx, 7), torch.full_like(dW, 7)]
+        p = [o.data_ptr() if i == alone else None for i, o in enumerate(out)]
+        st = moe.lib().moe_expert_linear8_backward(dy.data_ptr(), moe.BF16, None if n is None else n.data_ptr(), E, C, K, N, kept.state.data_ptr(), kept.state.numel(), *p, moe._stream())
+        assert st == moe.OK and torch.equal(out[alone], (dx, dW)[alone]) and (out[1 - alone] == 7).all()
+    with pytest.raises(ValueError):
+        moe.expert_linear8_backward(dy[:, :8], kept)
+    with pytest.raises(ValueError):
+        moe.expert_linear8_train(x, W[:, :8])
+
+
+def test_linear8_in_hip_graph(moe):
+    E, C, K, N = 3, 130, 136, 264
+    x, W, dy = torch.randn((E, C, K), device="cuda"), torch.randn((E, K, N), device="cuda"), torch.randn((E, C, N), device="cuda")
+    counts = torch.tensor([130, 0, 17], dtype=torch.int32, device="cuda")
+
+    def step():
+        y, kept = moe.expert_linear8_train(x, W, counts=counts)
+        return (y, *moe.expert_linear8_backward(dy, kept))
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step()
+    for i in range(3):
+        x.normal_()
+        counts.copy_(torch.tensor([17 * i, 130, 129 - i], dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(captured, step()):
+            assert torch.equal(a, b)

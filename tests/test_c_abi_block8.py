@@ -50,6 +50,19 @@ def test_matrix_refusals(moe):
     assert mm(N=12) == mm(A=FAKE + 8) == mm(As=FAKE + 1) == mm(N=1 << 20, K=4096) == moe.UNSUPPORTED
 
 
+def test_linear8_refusals(moe):
+    L = moe.lib()
+    assert L.moe_expert_linear8_state_bytes(2, 8, 64, 64) >= 2 * (64 * 128 + 64 * 128 + 64 * 128 + 8 * 128)
+    assert L.moe_expert_linear8_state_bytes(2, 8, 60, 64) == L.moe_expert_linear8_state_bytes(2, 8, 64, 12) == L.moe_expert_linear8_state_bytes(0, 8, 64, 64) == 0
+    train = lambda x=FAKE, W=FAKE, dt=1, E=2, C=8, K=64, N=64, y=FAKE, st=FAKE, n=1 << 30: L.moe_expert_linear8_train(x, W, dt, None, E, C, K, N, y, st, n, None)   # noqa: E731
+    assert train(x=None) == train(W=None) == train(y=None) == train(st=None) == train(dt=7) == train(E=0) == train(C=0) == moe.INVALID_ARG
+    assert train(K=12) == train(N=20) == train(x=FAKE + 8) == train(st=FAKE + 16) == train(K=1 << 16, N=1 << 16) == moe.UNSUPPORTED
+    assert train(n=64) == moe.WORKSPACE_TOO_SMALL
+    back = lambda dy=FAKE, dt=1, K=64, st=FAKE, n=1 << 30, dx=FAKE, dW=FAKE: L.moe_expert_linear8_backward(dy, dt, None, 2, 8, K, 64, st, n, dx, dW, None)   # noqa: E731
+    assert back(dy=None) == back(st=None) == back(dx=None, dW=None) == back(dt=-1) == moe.INVALID_ARG
+    assert back(K=4) == back(dW=FAKE + 4) == moe.UNSUPPORTED and back(n=0) == moe.WORKSPACE_TOO_SMALL
+
+
 def test_layer_refusals(moe):
     L = moe.lib()
     ffn = lambda x=FAKE, act=0, M=64, H=64, slots=None, T=0, hid=FAKE: L.moe_expert_ffn8(x, FAKE, slots, T, FAKE, FAKE, None, FAKE, FAKE, None, act, 1, None, 2, 8, M, H, hid, FAKE, FAKE, None)   # noqa: E731
