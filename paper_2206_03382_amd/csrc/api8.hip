@@ -75,7 +75,7 @@ FewWorkspace few_layout(int64_t T, int64_t M, int64_t H, int64_t E, int k, int d
   w.counts = take((size_t)E * 4);
   w.plan = take((size_t)(E < T * k ? E : T * k) * kFewPlan * 4);
   w.hidden = take((size_t)T * k * H * esize(dtype));
-  w.partial = take((size_t)T * k * M * 4);
+  w.partial = take(few_partial_bytes(T, M, H, E, k));
   w.arrived = take(few_arrivals_bytes(M));
   w.total = off;
   return w;
@@ -317,7 +317,7 @@ int moe_layer_forward_few(const void* x, const void* Wg, const float* gate_bias,
   gate_w = gate_w ? gate_w : (float*)(base + w.gate_w);
   counts = counts ? counts : (int32_t*)(base + w.counts);
   logits = logits ? logits : (float*)(base + w.logits);
-  const FewTokens p = {x, Wg, W1, b1, W2, b2, gate_bias, s1, s2, idx, loc, counts, gate_w, logits, T, M, H, E, C, k, act, dtype, normalize, false, false, 0, 0,
+  const FewTokens p = {x, Wg, W1, b1, W2, b2, gate_bias, s1, s2, idx, loc, counts, gate_w, logits, T, M, H, E, C, k, act, dtype, normalize, false, false, 0, 0, 0, 0,
                        (int32_t*)(base + w.plan), base + w.hidden, (float*)(base + w.partial),
                        (int32_t*)(base + w.arrived), out};
   return status_of(launch_few_tokens(p, (hipStream_t)stream));

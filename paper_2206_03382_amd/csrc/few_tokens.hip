@@ -15,6 +15,7 @@ namespace {
 constexpr int kFewWaves = 8, kFewRows = MOE_FEW_MAX_TOKENS;
 constexpr int kFewArrival = 32;                                     // columns to an arrival counter, at least
 constexpr int kFewExperts = 512;
+constexpr int kFewPartBits = 3;                                     // at most 8 parts of a sum over k
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 
 // An operand's rows in the form the matrix cores take them, and a step of the weights of 16 C columns.  Lane l = 16 g + i has row i of the tokens; which k and columns it
@@ -180,21 +181,25 @@ template <typename ET, bool W8, int C, int TILES> struct FewWeights {
   const uint8_t* sc;
   int64_t pitch, step_bytes;                                        // pitch: N, or the bytes of a row of 8-bit weights
   typename L::At at;
-  int full;                                                         // whole steps
+  int first, last;                                                  // of the whole steps, this block's
+  bool end;                                                         // and what is left behind them
   typename L::Weights w[kFirst];
 
-  __device__ __forceinline__ void start(const void* weights, const uint8_t* scales, int64_t e, int64_t K, int64_t N, int64_t n0) {
+  __device__ __forceinline__ void start(const void* weights, const uint8_t* scales, int64_t e, int64_t K, int64_t N, int64_t n0, int part, int part_bits) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     pitch = W8 ? row_bytes8(K) : N;
     W = (const char*)weights + (W8 ? e * N * pitch : e * K * N * (int64_t)sizeof(ET));
     sc = W8 ? scales + (e * ceil_div(N, kBlock8) + n0 / kBlock8) * row_scales8(K) : nullptr;
     step_bytes = L::step_bytes(pitch);
     at = L::at(n0, N, pitch, lane & 15, lane >> 4);
-    full = (int)(K / L::kStep);
+    const int pairs = (int)(K / L::kStep + 1) / 2;                  // two steps of 8-bit weights are a line
+    first = (pairs * part >> part_bits) * 2;
+    end = part + 1 == 1 << part_bits;
+    last = end ? (int)(K / L::kStep) : (pairs * (part + 1) >> part_bits) * 2;
 #pragma unroll
     for (int d = 0; d < kFirst; ++d) {
-      const int s = L::step(wave, d);
-      if (s < full) L::template load<false>(w[d], W + s * step_bytes, at, sc, pitch, s, 0, lane >> 4);
+      const int s = first + L::step(wave, d);
+      if (s < last) L::template load<false>(w[d], W + s * step_bytes, at, sc, pitch, s, 0, lane >> 4);
     }
   }
 };
@@ -216,37 +221,37 @@ __device__ __forceinline__ void few_product(const FewWeights<ET, W8, C, TILES>& 
     for (int c = 0; c < C; ++c) acc[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
   typename L::Weights w[D];
   typename L::Rows x[D][RT];
-  const int full = o.full;
+  const int first = o.first, last = o.last;
   auto fetch_rows = [&](int s, int d) {
 #pragma unroll
     for (int t = 0; t < RT; ++t) L::template load_rows<false>(x[d][t], row[t] + s * L::kStep, 0, g);
   };
   auto fetch = [&](int s, int d) {
-    if (s >= full) return;
+    if (s >= last) return;
     L::template load<false>(w[d], o.W + s * o.step_bytes, o.at, o.sc, o.pitch, s, 0, g);
     fetch_rows(s, d);
   };
 #pragma unroll
   for (int d = 0; d < D; ++d) {
-    const int s = L::step(wave, d);
+    const int s = first + L::step(wave, d);
     if (d >= kFirst) fetch(s, d);
-    else if (s < full) {
+    else if (s < last) {
       w[d] = o.w[d];
       fetch_rows(s, d);
     }
   }
-  for (int j = 0; L::step(wave, j) < full; j += D) {
+  for (int j = 0; first + L::step(wave, j) < last; j += D) {
 #pragma unroll
     for (int d = 0; d < D; ++d) {
-      if (L::step(wave, j + d) >= full) break;
+      if (first + L::step(wave, j + d) >= last) break;
       L::template multiply<RT>(w[d], x[d], acc);
-      fetch(L::step(wave, j + d + D), d);
+      fetch(first + L::step(wave, j + d + D), d);
     }
   }
-  if (const int left = (int)(K - (int64_t)full * L::kStep); left > 0 && wave == full % kFewWaves) {
-    L::template load<true>(w[0], o.W + full * o.step_bytes, o.at, o.sc, o.pitch, full, left, g);
+  if (const int left = (int)(K - (int64_t)last * L::kStep); o.end && left > 0 && wave == last % kFewWaves) {
+    L::template load<true>(w[0], o.W + last * o.step_bytes, o.at, o.sc, o.pitch, last, left, g);
 #pragma unroll
-    for (int t = 0; t < RT; ++t) L::template load_rows<true>(x[0][t], row[t] + (int64_t)full * L::kStep, left, g);
+    for (int t = 0; t < RT; ++t) L::template load_rows<true>(x[0][t], row[t] + (int64_t)last * L::kStep, left, g);
     L::template multiply<RT>(w[0], x[0], acc);
   }
   // the waves' sums meet in LDS, 16 rows at a time: [wave][row][column], read back in the order of the waves
@@ -273,14 +278,21 @@ __device__ __forceinline__ void few_product(const FewWeights<ET, W8, C, TILES>& 
 }
 
 // Gate logits of few tokens and experts, a block to TOKENS tokens and 8 experts: its threads take 8 of the model dim each at a time, all their loads go out together, and the
-// products are exact and summed in fp64, so a logit is rounded once, like moe_gate_logits'.  VECTOR: rows of Wg in pieces of 8 experts.
+// products are exact and summed in fp64, so a logit is rounded once, like moe_gate_logits'.  VECTOR: rows of Wg in pieces of 8 experts, of which there is one at least, on 4 bytes.
 constexpr int kLogitExperts = 8;
+struct __attribute__((packed, aligned(4))) Words4 { uint32_t x, y, z, w; };
+__device__ __forceinline__ uint4 load16_any(const void* p) {
+  const Words4 v = *reinterpret_cast<const Words4*>(p);
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
 template <typename ET, int TOKENS, bool VECTOR>
 __global__ __launch_bounds__(512) void few_logits_kernel(const ET* __restrict__ x, const ET* __restrict__ Wg, const float* __restrict__ gate_bias, int T, int M, int E,
-                                                         float* __restrict__ logits, int32_t* __restrict__ counts) {
+                                                         float* __restrict__ logits, int32_t* __restrict__ counts, int32_t* __restrict__ arrived, int arrivals) {
   constexpr int kSums = TOKENS * kLogitExperts, V = Vec16<ET>::N;
   __shared__ double wave_sums[8][kSums];
-  const int e0 = blockIdx.x * kLogitExperts, t0 = blockIdx.y * TOKENS, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int e0 = VECTOR && (int)blockIdx.x * kLogitExperts > E - kLogitExperts ? E - kLogitExperts : blockIdx.x * kLogitExperts;      // the last ones may be in two blocks
+  const int t0 = blockIdx.y * TOKENS, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int i = (blockIdx.y * gridDim.x + blockIdx.x) * 512 + threadIdx.x; i < arrivals; i += gridDim.x * gridDim.y * 512) arrived[i] = 0;      // of the products' blocks
   double sum[kSums] = {};
   for (int m = threadIdx.x * 8; m < M; m += 512 * 8) {
     float a[TOKENS][8], b[8][kLogitExperts];
@@ -291,7 +303,7 @@ __global__ __launch_bounds__(512) void few_logits_kernel(const ET* __restrict__ 
       for (int c = 0; c < kLogitExperts; c += V) {
         if constexpr (VECTOR) {
           float f[V];
-          Vec16<ET>::unpack(*reinterpret_cast<const uint4*>(w + c), f);
+          Vec16<ET>::unpack(load16_any(w + c), f);
 #pragma unroll
           for (int j = 0; j < V; ++j) b[r][c + j] = f[j];
         } else {
@@ -545,21 +557,19 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_plan_kernel(const FewToken
     few_report(p, p.logits, e - units, ranks);
     return;
   }
-  if (e == 0)
-    for (int64_t s = threadIdx.x; s < ceil_div(p.M, kFewArrival); s += 64 * kFewWaves) p.arrived[s] = 0;
   const bool direct = units == p.E;
   if (!direct) e = few_chosen(p, p.logits, blockIdx.x, ranks, &found);
   const int n = few_own_pairs(p, e, few_own_rank(p, p.logits, e), direct ? -1 : (int)blockIdx.x, true, arrivals, pair_of);
   if (threadIdx.x < 64) few_write_plan(p.plan + (int64_t)blockIdx.x * kFewPlan, e, n, pair_of);
 }
 
-// Block x, y: 16 C columns of unit y's expert.
+// Block x, y, z: 16 C columns of unit y's expert, part z of the sum over k.
 // TILES: of 16 rows that an expert can have at most, 1 or 4; with 1 two blocks fit a CU (not beside the logits, which would spill).  STAGE: the first product, from the logits or the plan; with the logits worked out by each
 // block itself; the second product.
 constexpr int kFewUp = 0, kFewUpAlone = 1, kFewDown = 2;
 template <typename ET, bool W8, int C, int TILES, int STAGE>
 __global__ __launch_bounds__(64 * kFewWaves, TILES == 1 && STAGE != kFewUpAlone ? 4 : 2) void few_kernel(const FewTokens p) {
-  constexpr bool UP = STAGE != kFewDown, ALONE = STAGE == kFewUpAlone;
+  constexpr bool UP = STAGE != kFewDown, ALONE = STAGE == kFewUpAlone, SPLIT = TILES == 1 && !ALONE;
   constexpr int kColumns = 16 * C, kSums = kFewWaves * 16 * (kColumns + 4);
   union Lds {
     FewRanks ranks;
@@ -573,14 +583,15 @@ __global__ __launch_bounds__(64 * kFewWaves, TILES == 1 && STAGE != kFewUpAlone 
   __shared__ typename std::conditional<ALONE, FewAlone, FewNone>::type alone;
   const float* logits = few_logits_of(p, alone);
   const int64_t K = UP ? p.M : p.H, N = UP ? p.H : p.M, n0 = (int64_t)blockIdx.x * kColumns;
-  const int units = few_units(p);
+  const int units = few_units(p), part_bits = SPLIT ? (UP ? p.up_bits : p.down_bits) : 0, parts = 1 << part_bits;
+  const int unit = blockIdx.y, part = SPLIT ? blockIdx.z : 0;
   if constexpr (ALONE) few_alone_logits<ET>(p, alone);
   if constexpr (UP) {
     // The tokens' choices: rows of blocks after the others, the last to start, so that it is theirs to share a CU (16 tokens x 8 experts of 2048 x 2048, 256 + 8 blocks: 41.1 us,
     // and 45.8 with these among the others).
-    if (blockIdx.y >= units) {
-      const int b = (blockIdx.y - units) * gridDim.x + blockIdx.x;
-      if (b >= few_token_blocks(p)) return;
+    if (unit >= units) {
+      const int b = (unit - units) * gridDim.x + blockIdx.x;
+      if (b >= few_token_blocks(p) || part > 0) return;
       few_report(p, logits, b, lds.ranks);
       if constexpr (ALONE) {                                        // one block has all tokens
         __syncthreads();
@@ -593,56 +604,57 @@ __global__ __launch_bounds__(64 * kFewWaves, TILES == 1 && STAGE != kFewUpAlone 
       }
       return;
     }
-    if (blockIdx.x == 0 && blockIdx.y == 0 && !p.planned)           // the arrivals of the next launch's blocks
+    if (ALONE && blockIdx.x == 0 && blockIdx.y == 0)                // the arrivals of the next launch's blocks
       for (int64_t s = threadIdx.x; s < ceil_div(p.M, kFewArrival); s += 64 * kFewWaves) p.arrived[s] = 0;
   }
   const bool direct = units == p.E;      // the weights' expert is known before its rows are
-  int32_t* plan = p.plan + (int64_t)blockIdx.y * kFewPlan;
+  int32_t* plan = p.plan + (int64_t)unit * kFewPlan;
   FewWeights<ET, W8, C, TILES> weights;
   const void* W = UP ? p.W1 : p.W2;
   const uint8_t* sc = UP ? p.s1 : p.s2;
-  if (direct) weights.start(W, sc, blockIdx.y, K, N, n0);
+  if (direct) weights.start(W, sc, unit, K, N, n0, part, part_bits);
   const bool planned = !UP || p.planned;
-  int unit_e = blockIdx.y, v = 0;
+  int unit_e = unit, v = 0;
   if (planned) v = threadIdx.x < kFewPlan ? plan[threadIdx.x] : 0;
   else {
-    if (!direct) unit_e = few_chosen(p, logits, blockIdx.y, lds.ranks, found);
+    if (!direct) unit_e = few_chosen(p, logits, unit, lds.ranks, found);
     v = few_own_rank(p, logits, unit_e);
   }
   if (planned) {
     if (threadIdx.x < 2) found[threadIdx.x] = v;
     else if (threadIdx.x < kFewPlan) pair_of[threadIdx.x - 2] = v;
   } else {
-    const int n = few_own_pairs(p, unit_e, v, direct ? -1 : (int)blockIdx.y, blockIdx.x == 0, lds.arrivals, pair_of);
+    const int n = few_own_pairs(p, unit_e, v, direct ? -1 : unit, blockIdx.x == 0 && part == 0, lds.arrivals, pair_of);
     if (threadIdx.x < 64) {
-      if (blockIdx.x == 0) few_write_plan(plan, unit_e, n, pair_of);
+      if (blockIdx.x == 0 && part == 0) few_write_plan(plan, unit_e, n, pair_of);
       if (threadIdx.x == 0) found[0] = unit_e;
       if (threadIdx.x == 0) found[1] = n;
     }
   }
   __syncthreads();
   const int e = __builtin_amdgcn_readfirstlane(found[0]), n_rows = __builtin_amdgcn_readfirstlane(found[1]);
-  if (!direct && n_rows > 0) weights.start(W, sc, e, K, N, n0);
+  if (!direct && n_rows > 0) weights.start(W, sc, e, K, N, n0, part, part_bits);
   if (threadIdx.x < n_rows) {
     const int q = pair_of[threadIdx.x];
     rows[threadIdx.x] = UP ? (const ET*)p.x + (int64_t)(q / p.k) * K : (const ET*)p.hidden + (int64_t)q * K;
   }
   __syncthreads();
+  const ET* bias = (const ET*)(UP ? p.b1 : p.b2);
+  const int64_t pairs = p.T * p.k;
   if (n_rows > 0) {
-    const ET* bias = (const ET*)(UP ? p.b1 : p.b2);
     auto done = [&](int r, int64_t n, float s) {
-      if (bias) s += load_as_f32(bias + (int64_t)e * N + n);
+      if (bias && part == 0) s += load_as_f32(bias + (int64_t)e * N + n);
       const int64_t q = pair_of[r];
-      if (UP) store_from_f32((ET*)p.hidden + q * N + n, apply_act(s, p.act));
-      else if (p.k == 1) store_from_f32((ET*)p.out + q * N + n, p.gate_w[q] * s);
-      else __hip_atomic_store(p.partial + q * N + n, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (UP && parts == 1) store_from_f32((ET*)p.hidden + q * N + n, apply_act(s, p.act));
+      else if (!UP && p.k == 1 && parts == 1) store_from_f32((ET*)p.out + q * N + n, p.gate_w[q] * s);
+      else __hip_atomic_store(p.partial + (part * pairs + q) * N + n, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     };
     if (TILES == 1 || n_rows <= 16) few_product<ET, W8, C, TILES, 1>(weights, rows, n_rows, K, N, n0, lds.sums, done);
     else if (n_rows <= 32) few_product<ET, W8, C, TILES, 2>(weights, rows, n_rows, K, N, n0, lds.sums, done);
     else few_product<ET, W8, C, TILES, 4>(weights, rows, n_rows, K, N, n0, lds.sums, done);
   }
-  if (UP) return;
-  if (p.k == 1) {                                                   // nothing to add up: what has no row here is zero
+  if (UP && parts == 1) return;
+  if (!UP && p.k == 1 && parts == 1) {                              // nothing to add up: what has no row here is zero
     if (blockIdx.y > 0) return;
     for (int64_t q = threadIdx.x; q < p.T * kColumns; q += 64 * kFewWaves) {
       const int64_t t = q / kColumns, n = n0 + q % kColumns;
@@ -650,28 +662,44 @@ __global__ __launch_bounds__(64 * kFewWaves, TILES == 1 && STAGE != kFewUpAlone 
     }
     return;
   }
-  // The last block of these columns to arrive adds up every token's choices, in their order: the same sums whoever it is, and nobody waits.  The partial sums are stored and loaded
+  // The last block of these columns to arrive (first product: with this unit) adds up what there is for them, in the order of choices and parts: the same sums whoever it is, and nobody waits.  The partial sums are stored and loaded
   // past what each XCD caches for itself (agent scope), so that a wave which has waited for its stores has them where every XCD sees them, and the last block, whose loads go out after
   // its count has come back, finds them there.  Counting needs no release then, which would write back all of an L2, and reading no acquire, which would drop it: 64 tokens x 64 experts of
   // 1024 x 4096 took 259 us with a release by one wave of each block instead of 227; 1 x 2 of 8, 4096 x 4096 in 8 bits 41.6 with an acquire instead of 35.3.
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  if (threadIdx.x == 0) last = __hip_atomic_fetch_add(p.arrived + blockIdx.x, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.y - 1;
+  int32_t* arrived = UP ? p.arrived + ceil_div(p.M, kFewArrival) + (int64_t)unit * gridDim.x : p.arrived;
+  if (threadIdx.x == 0) last = __hip_atomic_fetch_add(arrived + blockIdx.x, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (UP ? parts : units * parts) - 1;
   __syncthreads();
   if (!last) return;
+  if constexpr (UP) {
+    for (int q0 = threadIdx.x; q0 < n_rows * kColumns; q0 += 64 * kFewWaves) {
+      const int64_t q = pair_of[q0 / kColumns], n = n0 + q0 % kColumns;
+      if (n >= N) continue;
+      float v[1 << kFewPartBits];
+#pragma unroll
+      for (int u = 0; u < 1 << kFewPartBits; ++u) v[u] = __hip_atomic_load(p.partial + ((u < parts ? u : 0) * pairs + q) * N + n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      float s = 0.f;
+#pragma unroll
+      for (int u = 0; u < 1 << kFewPartBits; ++u) s += u < parts ? v[u] : 0.f;
+      store_from_f32((ET*)p.hidden + q * N + n, apply_act(s, p.act));
+    }
+    return;
+  }
   for (int64_t q = threadIdx.x; q < p.T * kColumns; q += 64 * kFewWaves) {
     const int64_t t = q / kColumns, n = n0 + q % kColumns;
     if (n >= N) continue;
     float s = 0.f;
-    for (int j0 = 0; j0 < p.k; j0 += 8) {                           // their loads together; a choice without a row has no sums to read a value from
+    for (int j0 = 0; j0 < p.k * parts; j0 += 8) {                   // their loads together; a choice without a row has no sums to read a value from
       float w[8], v[8];
       bool kept[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int64_t o = t * p.k + (j0 + j < p.k ? j0 + j : p.k - 1);
-        kept[j] = j0 + j < p.k && p.loc[o] < p.C;
+        const int at = j0 + j < p.k * parts ? j0 + j : 0, choice = at >> part_bits;
+        const int64_t o = t * p.k + choice;
+        kept[j] = j0 + j < p.k * parts && p.loc[o] < p.C;
         w[j] = p.gate_w[o];
-        v[j] = __hip_atomic_load(p.partial + o * N + n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        v[j] = __hip_atomic_load(p.partial + ((at & (parts - 1)) * pairs + o) * N + n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) s += kept[j] ? w[j] * v[j] : 0.f;
@@ -680,17 +708,30 @@ __global__ __launch_bounds__(64 * kFewWaves, TILES == 1 && STAGE != kFewUpAlone 
   }
 }
 
-template <typename ET, int TOKENS> void launch_few_logits(const FewTokens& p, hipStream_t s) {
-  const dim3 grid((unsigned)ceil_div(p.E, kLogitExperts), (unsigned)ceil_div(p.T, TOKENS)), block(512);
-  const bool vector = p.E % kLogitExperts == 0 && (reinterpret_cast<uintptr_t>(p.Wg) & 15) == 0;
-  if (vector) few_logits_kernel<ET, TOKENS, true><<<grid, block, 0, s>>>((const ET*)p.x, (const ET*)p.Wg, p.gate_bias, (int)p.T, (int)p.M, (int)p.E, p.logits, p.counts);
-  else few_logits_kernel<ET, TOKENS, false><<<grid, block, 0, s>>>((const ET*)p.x, (const ET*)p.Wg, p.gate_bias, (int)p.T, (int)p.M, (int)p.E, p.logits, p.counts);
+// Parts of the sum over k, 2^bits, for up to as many blocks as there are CUs: one takes 25 GB/s or so from memory whatever its waves ask for.  Parts of 512 k at least, or 2048 of 8-bit
+// weights.  us without and with: 1 token x 2 experts of 2048 x 2048 in bf16 (64 blocks) 29.0, 24.7; 1 x 4 of 4096 x 1024 (64 and 256) 36.5, 31.0; 4 x 8 of 64 of 1024 x 4096 (512 and 128)
+// 43.4, 37.9; 16 x 4 of 2048 x 4096 (256 and 128) 52.1, 47.2; parts of 256 k, 16 x 8 of 512 x 512 20.1, 22.3; of 1024, 1 x 2 of 2048 x 2048 in 8 bits 21.2, 22.0.  More than 16 tokens: 40 x 2
+// of 1024 x 1024 27.6, 30.4.
+inline int few_part_bits(int64_t T, int64_t blocks, int64_t K, bool w8) {
+  int bits = 0;
+  while (T <= 16 && bits < kFewPartBits && blocks << (bits + 1) <= 256 && K >> (bits + 1) >= (w8 ? 2048 : 512)) ++bits;
+  return bits;
 }
 
-template <typename ET, bool W8, int C, int STAGE> void launch_few_units(const FewTokens& p, hipStream_t s) {
+template <typename ET, int TOKENS> void launch_few_logits(const FewTokens& p, hipStream_t s) {
+  const dim3 grid((unsigned)ceil_div(p.E, kLogitExperts), (unsigned)ceil_div(p.T, TOKENS)), block(512);
+  const int arrivals = (int)(few_arrivals_bytes(p.M) / 4);
+  const bool vector = p.E >= kLogitExperts && (sizeof(ET) == 4 || p.E % 2 == 0) && (reinterpret_cast<uintptr_t>(p.Wg) & 3) == 0;
+  if (vector) few_logits_kernel<ET, TOKENS, true><<<grid, block, 0, s>>>((const ET*)p.x, (const ET*)p.Wg, p.gate_bias, (int)p.T, (int)p.M, (int)p.E, p.logits, p.counts, p.arrived, arrivals);
+  else few_logits_kernel<ET, TOKENS, false><<<grid, block, 0, s>>>((const ET*)p.x, (const ET*)p.Wg, p.gate_bias, (int)p.T, (int)p.M, (int)p.E, p.logits, p.counts, p.arrived, arrivals);
+}
+
+template <typename ET, bool W8, int C, int STAGE> void launch_few_units(FewTokens p, hipStream_t s) {
   constexpr bool UP = STAGE != kFewDown;
   const int64_t columns = ceil_div(UP ? p.H : p.M, 16 * C), reports = UP && !p.planned ? ceil_div(few_token_blocks(p), columns) : 0;
-  const dim3 grid((unsigned)columns, (unsigned)(few_units(p) + reports)), block(64 * kFewWaves);
+  const int bits = STAGE == kFewUpAlone ? 0 : few_part_bits(p.T, columns * few_units(p), UP ? p.M : p.H, W8);
+  (UP ? p.up_bits : p.down_bits) = bits;
+  const dim3 grid((unsigned)columns, (unsigned)(few_units(p) + reports), 1u << bits), block(64 * kFewWaves);
   if (STAGE == kFewUpAlone || p.T <= 16) few_kernel<ET, W8, C, 1, STAGE><<<grid, block, 0, s>>>(p);
   else if constexpr (STAGE != kFewUpAlone) few_kernel<ET, W8, C, 4, STAGE><<<grid, block, 0, s>>>(p);
 }
@@ -725,7 +766,15 @@ template <typename ET, bool W8> hipError_t launch_few(const FewTokens& p, hipStr
 
 }  // namespace
 
-size_t few_arrivals_bytes(int64_t M) { return (size_t)ceil_div(M, kFewArrival) * 4; }
+// counters of arrivals: for columns of the second product, and for blocks of the first one where they share a sum, which are 128 at most
+size_t few_arrivals_bytes(int64_t M) { return (size_t)(ceil_div(M, kFewArrival) + 128) * 4; }
+
+// sums that blocks leave for each other
+size_t few_partial_bytes(int64_t T, int64_t M, int64_t H, int64_t E, int k) {
+  const int64_t units = E < T * k ? E : T * k;
+  const int64_t up = H << few_part_bits(T, ceil_div(H, 64) * units, M, false), down = M << few_part_bits(T, ceil_div(M, 64) * units, H, false);      // the most that either kind of weights takes
+  return (size_t)T * k * (up > down ? up : down) * 4;
+}
 
 hipError_t launch_few_tokens(const FewTokens& given, hipStream_t s) {
   FewTokens p = given;

@@ -58,7 +58,9 @@ CASES = [(1, 8, 8, 1, 1, 1.0, 0, 0, False), (1, 256, 512, 4, 1, 1.0, 0, 0, True)
          (16, 264, 1096, 40, 4, 2.0, 1, 1, True), (64, 128, 520, 64, 2, 0.5, 2, 0, False), (12, 64, 1160, 70, 3, 4.0, 1, 1, False), (20, 64, 1160, 70, 3, 1.0, 0, 1, True),
          (2, 520, 128, 512, 3, 100.0, 1, 1, False), (1, 1032, 136, 512, 1, 1.0, 2, 0, True),
          # little enough for every block to work out the logits: odd tokens and experts, more pieces than waves
-         (7, 136, 264, 7, 3, 1.0, 1, 1, True), (8, 16, 72, 64, 2, 2.0, 2, 0, False), (3, 256, 128, 9, 9, 9.0, 1, 1, False), (8, 128, 136, 8, 2, 0.4, 0, 1, True)]
+         (7, 136, 264, 7, 3, 1.0, 1, 1, True), (8, 16, 72, 64, 2, 2.0, 2, 0, False), (3, 256, 128, 9, 9, 9.0, 1, 1, False), (8, 128, 136, 8, 2, 0.4, 0, 1, True),
+         # few blocks and long sums: parts of them to a block; the second with dropped choices, the third with one choice, the last ones in more parts
+         (1, 1544, 1032, 4, 2, 2.0, 1, 1, True), (9, 1032, 520, 2, 2, 0.5, 2, 1, True), (3, 1096, 2056, 3, 1, 0.4, 1, 0, True), (1, 8200, 264, 8, 1, 1.0, 2, 0, False), (2, 4104, 4160, 1, 1, 1.0, 0, 0, True)]
 
 
 @pytest.mark.parametrize("kind", ["bf16", "fp32", "8bit", "8bit_fp32"])
