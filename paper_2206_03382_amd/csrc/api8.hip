@@ -230,9 +230,8 @@ int moe_expert_linear8_train(const void* x, const void* W, int dtype, const int3
   if (state_bytes < w.total) return MOE_WORKSPACE_TOO_SMALL;
   uint8_t* b = (uint8_t*)state;
   const hipStream_t s = (hipStream_t)stream;
-  if (launch_quantize8(x, dtype, counts, E, C, K, false, b + w.x, b + w.x_scales, b + w.xt, b + w.xt_scales, s) != hipSuccess ||
-      launch_quantize8(W, dtype, nullptr, E, K, N, true, b + w.W, b + w.W_scales, b + w.Wt, b + w.Wt_scales, s) != hipSuccess ||
-      (counts && launch_zero_past(y, dtype, counts, E, C, N, s) != hipSuccess))
+  if (launch_quantize8(x, dtype, counts, E, C, K, false, b + w.x, b + w.x_scales, b + w.xt, b + w.xt_scales, s, counts ? y : nullptr, N) != hipSuccess ||
+      launch_quantize8(W, dtype, nullptr, E, K, N, true, b + w.W, b + w.W_scales, b + w.Wt, b + w.Wt_scales, s) != hipSuccess)
     return MOE_HIP_ERROR;
   const Matmul8 p = {b + w.x, b + w.x_scales, b + w.Wt, b + w.Wt_scales, 1, nullptr, MOE_ACT_NONE, counts, nullptr, nullptr, 0, E, C, K, N, 0, dtype, y, nullptr, nullptr};
   return status_of(launch_matmul8(p, s));
@@ -248,8 +247,7 @@ int moe_expert_linear8_backward(const void* dy, int dtype, const int32_t* counts
   uint8_t* b = (uint8_t*)state;
   const hipStream_t s = (hipStream_t)stream;
   if (launch_quantize8(dy, dtype, counts, E, C, N, false, dx ? b + w.dy : nullptr, dx ? b + w.dy_scales : nullptr, dW ? b + w.dyt : nullptr,
-                       dW ? b + w.dyt_scales : nullptr, s) != hipSuccess ||
-      (dx && counts && launch_zero_past(dx, dtype, counts, E, C, K, s) != hipSuccess))
+                       dW ? b + w.dyt_scales : nullptr, s, counts ? dx : nullptr, K) != hipSuccess)
     return MOE_HIP_ERROR;
   const Matmul8 px = {b + w.dy, b + w.dy_scales, b + w.W, b + w.W_scales, 1, nullptr, MOE_ACT_NONE, counts, nullptr, nullptr, 0, E, C, N, K, 0, dtype, dx, nullptr, nullptr};
   if (dx && launch_matmul8(px, s) != hipSuccess) return MOE_HIP_ERROR;
