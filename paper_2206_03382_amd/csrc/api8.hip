@@ -61,7 +61,7 @@ Layer8Workspace layer8_layout(int64_t T, int64_t M, int64_t H, int64_t E, int k,
 }
 
 struct FewWorkspace {
-  size_t logits, idx, loc, gate_w, counts, plan, hidden, partial, arrived, total;
+  size_t logits, idx, loc, gate_w, counts, logit_parts, plan, hidden, partial, arrived, total;
 };
 
 FewWorkspace few_layout(int64_t T, int64_t M, int64_t H, int64_t E, int k, int dtype) {
@@ -73,6 +73,7 @@ FewWorkspace few_layout(int64_t T, int64_t M, int64_t H, int64_t E, int k, int d
   w.loc = take((size_t)T * k * 4);
   w.gate_w = take((size_t)T * k * 4);
   w.counts = take((size_t)E * 4);
+  w.logit_parts = take(few_logit_bytes(T, M, E));
   w.plan = take((size_t)(E < T * k ? E : T * k) * kFewPlan * 4);
   w.hidden = take((size_t)T * k * H * esize(dtype));
   w.partial = take(few_partial_bytes(T, M, H, E, k));
@@ -315,8 +316,8 @@ int moe_layer_forward_few(const void* x, const void* Wg, const float* gate_bias,
   gate_w = gate_w ? gate_w : (float*)(base + w.gate_w);
   counts = counts ? counts : (int32_t*)(base + w.counts);
   logits = logits ? logits : (float*)(base + w.logits);
-  const FewTokens p = {x, Wg, W1, b1, W2, b2, gate_bias, s1, s2, idx, loc, counts, gate_w, logits, T, M, H, E, C, k, act, dtype, normalize, false, false, 0, 0, 0, 0,
-                       (int32_t*)(base + w.plan), base + w.hidden, (float*)(base + w.partial),
+  const FewTokens p = {x, Wg, W1, b1, W2, b2, gate_bias, s1, s2, idx, loc, counts, gate_w, logits, T, M, H, E, C, k, act, dtype, normalize, false, false, 0, 0, 0, 0, 0,
+                       (double*)(base + w.logit_parts), (int32_t*)(base + w.plan), base + w.hidden, (float*)(base + w.partial),
                        (int32_t*)(base + w.arrived), out};
   return status_of(launch_few_tokens(p, (hipStream_t)stream));
 }

@@ -109,7 +109,8 @@ struct FewTokens {
   int64_t T, M, H, E, C;
   int k, act, dtype, normalize;
   bool planned, alone;            // set by launch_few_tokens, as are the next two
-  int expert_bits, token_bits, up_bits, down_bits;
+  int expert_bits, token_bits, slice_bits, up_bits, down_bits;
+  double* logit_parts;            // few_logit_bytes: [slices, T, E]
   int32_t* plan;                  // [min(E, T k), kFewPlan]
   void* hidden;                   // [T k, H]
   float* partial;                 // few_partial_bytes: [parts, T k, H or M]
@@ -118,6 +119,7 @@ struct FewTokens {
 };
 constexpr int kFewPlan = 2 + MOE_FEW_MAX_TOKENS;
 size_t few_arrivals_bytes(int64_t M);
+size_t few_logit_bytes(int64_t T, int64_t M, int64_t E);
 size_t few_partial_bytes(int64_t T, int64_t M, int64_t H, int64_t E, int k);
 hipError_t launch_few_tokens(const FewTokens& p, hipStream_t s);
 

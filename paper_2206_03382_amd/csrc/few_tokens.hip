@@ -279,24 +279,28 @@ __device__ __forceinline__ void few_product(const FewWeights<ET, W8, C, TILES>& 
   }
 }
 
-// Gate logits of few tokens and experts, a block to TOKENS tokens and 8 experts: its threads take 8 of the model dim each at a time, all their loads go out together, and the
-// products are exact and summed in fp64, so a logit is rounded once, like moe_gate_logits'.  VECTOR: rows of Wg in pieces of 8 experts, of which there is one at least, on 4 bytes.
-constexpr int kLogitExperts = 8;
+// Gate logits of few tokens and experts, a block to TOKENS tokens, 8 experts and a slice of the model dim: its threads take 8 of it each at a time, all their loads go out together,
+// and the products are exact and summed in fp64.  part[slice][t][e], or the logit itself of a single slice; whoever reads them adds up the slices, so a logit is rounded once, like moe_gate_logits'.  VECTOR: rows of Wg in
+// pieces of 8 experts, of which there is one at least, on 4 bytes.
+constexpr int kLogitExperts = 8, kLogitThreads = 256, kLogitSliceBits = 2;      // twice the threads where there are no slices
 struct __attribute__((packed, aligned(4))) Words4 { uint32_t x, y, z, w; };
 __device__ __forceinline__ uint4 load16_any(const void* p) {
   const Words4 v = *reinterpret_cast<const Words4*>(p);
   return make_uint4(v.x, v.y, v.z, v.w);
 }
 template <typename ET, int TOKENS, bool VECTOR>
-__global__ __launch_bounds__(512) void few_logits_kernel(const ET* __restrict__ x, const ET* __restrict__ Wg, const float* __restrict__ gate_bias, int T, int M, int E,
-                                                         float* __restrict__ logits, int32_t* __restrict__ counts, int32_t* __restrict__ arrived, int arrivals) {
+__global__ __launch_bounds__(2 * kLogitThreads) void few_logits_kernel(const ET* __restrict__ x, const ET* __restrict__ Wg, const float* __restrict__ gate_bias, int T, int M, int E, int slice,
+                                                                   double* __restrict__ part, float* __restrict__ logits,
+                                                                   int32_t* __restrict__ counts, int32_t* __restrict__ arrived, int arrivals) {
   constexpr int kSums = TOKENS * kLogitExperts, V = Vec16<ET>::N;
-  __shared__ double wave_sums[8][kSums];
+  __shared__ double wave_sums[2 * kLogitThreads / 64][kSums];
   const int e0 = VECTOR && (int)blockIdx.x * kLogitExperts > E - kLogitExperts ? E - kLogitExperts : blockIdx.x * kLogitExperts;      // the last ones may be in two blocks
   const int t0 = blockIdx.y * TOKENS, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int i = (blockIdx.y * gridDim.x + blockIdx.x) * 512 + threadIdx.x; i < arrivals; i += gridDim.x * gridDim.y * 512) arrived[i] = 0;      // of the products' blocks
+  if (blockIdx.z == 0)                                              // of the products' blocks
+    for (int i = (blockIdx.y * gridDim.x + blockIdx.x) * blockDim.x + threadIdx.x; i < arrivals; i += gridDim.x * gridDim.y * blockDim.x) arrived[i] = 0;
   double sum[kSums] = {};
-  for (int m = threadIdx.x * 8; m < M; m += 512 * 8) {
+  const int end = min(M, (int)(blockIdx.z + 1) * slice);
+  for (int m = blockIdx.z * slice + threadIdx.x * 8; m < end; m += blockDim.x * 8) {
     float a[TOKENS][8], b[8][kLogitExperts];
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
@@ -347,12 +351,33 @@ __global__ __launch_bounds__(512) void few_logits_kernel(const ET* __restrict__ 
   __syncthreads();
   const int t = t0 + threadIdx.x / kLogitExperts, e = e0 + threadIdx.x % kLogitExperts;
   if (threadIdx.x >= kSums || t >= T || e >= E) return;
-  if (t == 0) counts[e] = 0;                                        // what has arrivals is counted later
-  double s = gate_bias ? (double)gate_bias[e] : 0.0;
-#pragma unroll
-  for (int u = 0; u < 8; ++u) s += wave_sums[u][threadIdx.x];
-  logits[(int64_t)t * E + e] = (float)s;
+  if (t == 0 && blockIdx.z == 0) counts[e] = 0;                     // what has arrivals is counted later
+  double s = 0.0;
+  for (int u = 0; u < (int)blockDim.x / 64; ++u) s += wave_sums[u][threadIdx.x];
+  if (gridDim.z == 1) logits[(int64_t)t * E + e] = (float)(s + (gate_bias ? (double)gate_bias[e] : 0.0));
+  else part[((int64_t)blockIdx.z * T + t) * E + e] = s;
 }
+
+// A logit of expert e, from its slices if there are several.
+struct FewSlices {
+  const double* part;
+  const float *bias, *logits;
+  int all, E, bits;
+  __device__ __forceinline__ explicit FewSlices(const FewTokens& p)
+      : part(p.logit_parts), bias(p.gate_bias), logits(p.logits), all((int)(p.T * p.E)), E((int)p.E), bits(p.slice_bits) {}
+  template <int N> __device__ __forceinline__ float sum(int at, int e) const {
+    double v[N], s = bias ? (double)bias[e] : 0.0;
+#pragma unroll
+    for (int u = 0; u < N; ++u) v[u] = part[u * all + at];
+#pragma unroll
+    for (int u = 0; u < N; ++u) s += v[u];
+    return (float)s;
+  }
+  __device__ __forceinline__ float operator()(int t, int e) const {
+    const int at = t * E + e;
+    return bits == 0 ? logits[at] : bits == 1 ? sum<2>(at, e) : sum<4>(at, e);
+  }
+};
 
 __device__ __forceinline__ uint32_t ordered(float v) {              // -0 as +0
   const uint32_t u = __float_as_uint(v + 0.0f);
@@ -376,8 +401,17 @@ __device__ __forceinline__ void load4(const uint16_t* p, float (&v)[4]) {
   v[2] = __uint_as_float(w.y << 16); v[3] = __uint_as_float(w.y & 0xffff0000u);
 }
 struct FewNone {};
-__device__ __forceinline__ const float* few_logits_of(const FewTokens&, const FewAlone& s) { return s.logits; }
-__device__ __forceinline__ const float* few_logits_of(const FewTokens& p, const FewNone&) { return p.logits; }
+struct FewWorkedOut {
+  const float* logits;
+  int E;
+  __device__ __forceinline__ float operator()(int t, int e) const { return logits[t * E + e]; }
+};
+// in LDS, or in one piece (more than 16 tokens: few_slice_bits), or in slices
+template <int TILES> __device__ __forceinline__ FewWorkedOut few_logits_of(const FewTokens& p, const FewAlone& s) { return {s.logits, (int)p.E}; }
+template <int TILES> __device__ __forceinline__ typename std::conditional<TILES == 1, FewSlices, FewWorkedOut>::type few_logits_of(const FewTokens& p, const FewNone&) {
+  if constexpr (TILES == 1) return FewSlices(p);
+  else return {p.logits, (int)p.E};
+}
 template <typename ET> __device__ __forceinline__ void few_alone_logits(const FewTokens& p, FewAlone& s) {
   const int T = (int)p.T, E = (int)p.E, M = (int)p.M, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int across = (E + 3) / 4, pieces = (T + 1) / 2 * across, parts = pieces >= kFewWaves ? 1 : kFewWaves / pieces;
@@ -438,9 +472,9 @@ struct FewRanks {
   uint32_t keys[kFewExperts];
   int rank[kFewExperts];
 };
-__device__ __forceinline__ void few_rank(const FewTokens& p, const float* logits, int t, FewRanks& s) {
+template <typename L> __device__ __forceinline__ void few_rank(const FewTokens& p, const L& logits, int t, FewRanks& s) {
   const int E = (int)p.E, group = 1 << p.expert_bits, sub = threadIdx.x & (group - 1), e = threadIdx.x >> p.expert_bits;     // threads to an expert, in one wave
-  if (threadIdx.x < E) s.keys[threadIdx.x] = ordered(logits[t * E + threadIdx.x]);
+  if (threadIdx.x < E) s.keys[threadIdx.x] = ordered(logits(t, threadIdx.x));
   __syncthreads();
   int rank = 0;
   if (e < E) {
@@ -456,15 +490,15 @@ __device__ __forceinline__ void few_rank(const FewTokens& p, const float* logits
   __syncthreads();
 }
 
-// Tokens' choices and gate weights as the caller sees them: the b-th block has 8 tokens, a wave each, or, of more than 64 experts, one token.
+// Tokens' logits, choices and gate weights as the caller sees them: the b-th block has 8 tokens, a wave each, or, of more than 64 experts, one token.
 inline __host__ __device__ int few_token_blocks(const FewTokens& p) { return (int)(p.E <= 64 ? (p.T + kFewWaves - 1) / kFewWaves : p.T); }
-__device__ __forceinline__ void few_report(const FewTokens& p, const float* logits, int b, FewRanks& s) {
+template <typename L> __device__ __forceinline__ void few_report(const FewTokens& p, const L& logits, int b, FewRanks& s) {
   const int E = (int)p.E, k = p.k, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int t = b;
   if (E <= 64) {
     t = b * kFewWaves + wave;
     if (t >= p.T) return;
-    const uint32_t own = lane < E ? ordered(logits[t * E + lane]) : 0;
+    const uint32_t own = lane < E ? ordered(logits(t, lane)) : 0;
     int rank = 0;
     for (int o = 0; o < E; ++o) {
       const uint32_t other = (uint32_t)__builtin_amdgcn_readlane((int)own, o);
@@ -479,7 +513,10 @@ __device__ __forceinline__ void few_report(const FewTokens& p, const float* logi
   const uint32_t* keys = s.keys + (E <= 64 ? wave * 64 : 0);
   const int* ranks = s.rank + (E <= 64 ? wave * 64 : 0);
   uint32_t most = 0;
-  for (int e = lane; e < E; e += 64) most = max(most, keys[e]);
+  for (int e = lane; e < E; e += 64) {
+    most = max(most, keys[e]);
+    if (p.alone || p.slice_bits > 0) p.logits[(int64_t)t * E + e] = unordered(keys[e]);
+  }
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, d));
   const float top = unordered(most);
@@ -495,15 +532,14 @@ __device__ __forceinline__ void few_report(const FewTokens& p, const float* logi
 }
 
 // The pairs (t, j) that expert e has, from the logits: a group of threads finds its rank for one token, and one wave the order of the arrivals: all first choices, all second ones ...
-__device__ __forceinline__ int few_own_rank(const FewTokens& p, const float* logits, int e) {
-  const int E = (int)p.E, group = 1 << p.token_bits, sub = threadIdx.x & (group - 1), t = threadIdx.x >> p.token_bits;
-  const float* row = logits + (t < p.T ? t : 0) * E;
-  const uint32_t own = ordered(row[e]);
+template <typename L> __device__ __forceinline__ int few_own_rank(const FewTokens& p, const L& logits, int e) {
+  const int E = (int)p.E, group = 1 << p.token_bits, sub = threadIdx.x & (group - 1), t = (int)(threadIdx.x >> p.token_bits), row = t < p.T ? t : 0;
+  const uint32_t own = ordered(logits(row, e));
   int rank = 0;
   for (int o0 = sub; o0 < E; o0 += 4 * group) {
     float v[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = row[o0 + i * group < E ? o0 + i * group : e];      // e itself counts for nothing
+    for (int i = 0; i < 4; ++i) v[i] = logits(row, o0 + i * group < E ? o0 + i * group : e);      // e itself counts for nothing
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t other = ordered(v[i]);
@@ -533,7 +569,7 @@ __device__ __forceinline__ int few_own_pairs(const FewTokens& p, int e, int rank
 }
 
 // The expert of choice o = j T + t.
-__device__ __forceinline__ int few_chosen(const FewTokens& p, const float* logits, int o, FewRanks& s, int* found) {
+template <typename L> __device__ __forceinline__ int few_chosen(const FewTokens& p, const L& logits, int o, FewRanks& s, int* found) {
   few_rank(p, logits, o % (int)p.T, s);
   if (threadIdx.x < p.E && s.rank[threadIdx.x] == o / (int)p.T) *found = threadIdx.x;
   __syncthreads();
@@ -553,15 +589,16 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_plan_kernel(const FewToken
   __shared__ FewRanks ranks;
   __shared__ uint32_t arrivals[kFewRows];
   __shared__ int pair_of[kFewRows], found;
+  const FewSlices logits(p);
   const int units = few_units(p);
   int e = blockIdx.x;
   if (e >= units) {
-    few_report(p, p.logits, e - units, ranks);
+    few_report(p, logits, e - units, ranks);
     return;
   }
   const bool direct = units == p.E;
-  if (!direct) e = few_chosen(p, p.logits, blockIdx.x, ranks, &found);
-  const int n = few_own_pairs(p, e, few_own_rank(p, p.logits, e), direct ? -1 : (int)blockIdx.x, true, arrivals, pair_of);
+  if (!direct) e = few_chosen(p, logits, blockIdx.x, ranks, &found);
+  const int n = few_own_pairs(p, e, few_own_rank(p, logits, e), direct ? -1 : (int)blockIdx.x, true, arrivals, pair_of);
   if (threadIdx.x < 64) few_write_plan(p.plan + (int64_t)blockIdx.x * kFewPlan, e, n, pair_of);
 }
 
@@ -583,7 +620,7 @@ __global__ __launch_bounds__(64 * kFewWaves, TILES == 1 && STAGE != kFewUpAlone 
   __shared__ const ET* rows[kFewRows];
   __shared__ int last;
   __shared__ typename std::conditional<ALONE, FewAlone, FewNone>::type alone;
-  const float* logits = few_logits_of(p, alone);
+  const auto logits = few_logits_of<TILES>(p, alone);
   const int64_t K = UP ? p.M : p.H, N = UP ? p.H : p.M, n0 = (int64_t)blockIdx.x * kColumns;
   const int units = few_units(p), part_bits = SPLIT ? (UP ? p.up_bits : p.down_bits) : 0, parts = 1 << part_bits;
   const int unit = blockIdx.y, part = SPLIT ? blockIdx.z : 0;
@@ -597,7 +634,6 @@ __global__ __launch_bounds__(64 * kFewWaves, TILES == 1 && STAGE != kFewUpAlone 
       few_report(p, logits, b, lds.ranks);
       if constexpr (ALONE) {                                        // one block has all tokens
         __syncthreads();
-        for (int q = threadIdx.x; q < p.T * p.E; q += 64 * kFewWaves) p.logits[q] = logits[q];
         if (threadIdx.x < p.E) {
           int n = 0;
           for (int t = 0; t < p.T; ++t) n += lds.ranks.rank[t * 64 + threadIdx.x] < p.k ? 1 : 0;
@@ -720,12 +756,22 @@ inline int few_part_bits(int64_t T, int64_t blocks, int64_t K, bool w8) {
   return bits;
 }
 
+// Slices of the model dim, 2^bits: one turn of a block's threads each, up to four; more than 16 tokens make blocks enough.  A block's reads of Wg bring whole lines for 16 bytes of each: 1 token, 8 of 128 experts of 4096 x 1024
+// 39.7 us without, 37.5 with them, 8 of 256 of 8192 x 1024 72.6, 65.0; 2 of 8 of 2048 x 2048 in two slices 24.2, 25.0.
+inline int few_slice_bits(int64_t T, int64_t M) {
+  int bits = 0;
+  while (T <= 16 && bits < kLogitSliceBits && M > kLogitThreads * 8 << bits) ++bits;
+  return bits;
+}
+
 template <typename ET, int TOKENS> void launch_few_logits(const FewTokens& p, hipStream_t s) {
-  const dim3 grid((unsigned)ceil_div(p.E, kLogitExperts), (unsigned)ceil_div(p.T, TOKENS)), block(512);
-  const int arrivals = (int)(few_arrivals_bytes(p.M) / 4);
+  const int slices = 1 << p.slice_bits, slice = (int)(ceil_div(ceil_div(p.M, slices), 8) * 8), arrivals = (int)(few_arrivals_bytes(p.M) / 4);
+  const dim3 grid((unsigned)ceil_div(p.E, kLogitExperts), (unsigned)ceil_div(p.T, TOKENS), (unsigned)slices), block(p.T > 16 ? 2 * kLogitThreads : kLogitThreads);
   const bool vector = p.E >= kLogitExperts && (sizeof(ET) == 4 || p.E % 2 == 0) && (reinterpret_cast<uintptr_t>(p.Wg) & 3) == 0;
-  if (vector) few_logits_kernel<ET, TOKENS, true><<<grid, block, 0, s>>>((const ET*)p.x, (const ET*)p.Wg, p.gate_bias, (int)p.T, (int)p.M, (int)p.E, p.logits, p.counts, p.arrived, arrivals);
-  else few_logits_kernel<ET, TOKENS, false><<<grid, block, 0, s>>>((const ET*)p.x, (const ET*)p.Wg, p.gate_bias, (int)p.T, (int)p.M, (int)p.E, p.logits, p.counts, p.arrived, arrivals);
+#define MOE_FEW_LOGITS(V) few_logits_kernel<ET, TOKENS, V><<<grid, block, 0, s>>>((const ET*)p.x, (const ET*)p.Wg, p.gate_bias, (int)p.T, (int)p.M, (int)p.E, slice, p.logit_parts, p.logits, p.counts, p.arrived, arrivals)
+  if (vector) MOE_FEW_LOGITS(true);
+  else MOE_FEW_LOGITS(false);
+#undef MOE_FEW_LOGITS
 }
 
 template <typename ET, bool W8, int C, int STAGE> void launch_few_units(FewTokens p, hipStream_t s) {
@@ -771,6 +817,8 @@ template <typename ET, bool W8> hipError_t launch_few(const FewTokens& p, hipStr
 // counters of arrivals: for columns of the second product, and for blocks of the first one where they share a sum, which are 128 at most
 size_t few_arrivals_bytes(int64_t M) { return (size_t)(ceil_div(M, kFewArrival) + 128) * 4; }
 
+size_t few_logit_bytes(int64_t T, int64_t M, int64_t E) { return (size_t)T * E * 8 << few_slice_bits(T, M); }
+
 // sums that blocks leave for each other
 size_t few_partial_bytes(int64_t T, int64_t M, int64_t H, int64_t E, int k) {
   const int64_t units = E < T * k ? E : T * k;
@@ -785,6 +833,7 @@ hipError_t launch_few_tokens(const FewTokens& given, hipStream_t s) {
   // 44.2, 46.3; 16 x 64 of 128 of 1024 x 1024, 8 bits (1024) 61.2, 58.5; 64 x 64 of 1024 x 4096 (4096) 264.7, 213.8.
   p.planned = ceil_div(p.H, 64) * few_units(p) > (p.T <= 16 ? 512 : 256);
   p.alone = !p.planned && p.T <= kAloneTokens && p.E <= kAloneExperts && p.T * p.E * p.M <= kAloneWork;
+  p.slice_bits = few_slice_bits(p.T, p.M);
   p.expert_bits = p.token_bits = 0;                                 // as many threads to an expert, and to a token, as there are
   while (p.expert_bits < 6 && (p.E << (p.expert_bits + 1)) <= 64 * kFewWaves) ++p.expert_bits;
   while (p.token_bits < 6 && (p.T << (p.token_bits + 1)) <= 64 * kFewWaves) ++p.token_bits;
