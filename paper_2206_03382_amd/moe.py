@@ -568,24 +568,29 @@ def _check_int32(t: Optional[torch.Tensor], *shape: int) -> None:
 def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float, residual: Optional[torch.Tensor] = None, want_y: bool = True,
              want_8: bool = False, out: Optional[Dict] = None) -> Dict:
     """h = x + residual (x itself without one), y = RMS norm of h times weight, y8 = the same in 8 bits; `out`: an earlier result of the same
-    shapes to write into."""
+    shapes to write into.  Without a residual nothing is written for h: the result names x and, under "spare", that x and the memory that a later call
+    with a residual writes instead of it (None: the call allocates)."""
     T, M = x.shape
     code = _dtype_code(x)
     if (residual is not None and residual.shape != x.shape) or (weight is not None and weight.numel() != M):
         raise ValueError("residual must have x's shape and weight its width")
     _check_storage(code, residual, weight)
     if out is None:
-        out = dict(h=torch.empty_like(x) if residual is not None else x, y=torch.empty_like(x) if want_y else None,
-                   y8=_alloc8((), T, M, False, x.device) if want_8 else None)
-        h, y, y8 = out["h"], out["y"], out["y8"]
+        out = dict(h=None, y=torch.empty_like(x) if want_y else None, y8=_alloc8((), T, M, False, x.device) if want_8 else None)
+    h, y, y8 = out["h"], out["y"], out["y8"]
+    if "spare" in out and h is out["spare"][0]:
+        h = out["spare"][1]
+    _check_out(h, x.shape, x.dtype)
+    _check_out(y, x.shape, x.dtype)
+    if y8 is not None:
+        if y8.blocks or y8.width != M or y8.s.shape != (T, -(-M // 512) * 4) or y8.s.dtype != torch.uint8:
+            raise ValueError("y8 must have x's shape and one exponent per row and block")
+        _check_out(y8.q, (T, -(-M // 128) * 128), torch.float8_e4m3fn)
+    if residual is None:
+        out["h"], out["spare"] = x, (x, h)
     else:
-        h, y, y8 = out["h"], out["y"], out["y8"]
-        _check_out(h, x.shape, x.dtype)
-        _check_out(y, x.shape, x.dtype)
-        if y8 is not None:
-            if y8.blocks or y8.width != M or y8.s.shape != (T, -(-M // 512) * 4) or y8.s.dtype != torch.uint8:
-                raise ValueError("y8 must have x's shape and one exponent per row and block")
-            _check_out(y8.q, (T, -(-M // 128) * 128), torch.float8_e4m3fn)
+        out["h"] = h = torch.empty_like(x) if h is None else h
+        out.pop("spare", None)
     _check(lib().moe_rms_norm(_p(x), _p(residual), _p(weight), eps, code, T, M, _p(h) if residual is not None else None, _p(y),
                               _p(y8.q) if y8 is not None else None, _p(y8.s) if y8 is not None else None, _stream()), "moe_rms_norm")
     return out
@@ -812,8 +817,8 @@ class NormMoELayer8:
                       int(act), code, _p(self.out), _p(r.get("idx")), _p(r.get("loc")), _p(r.get("gate_w")), _p(r.get("counts")),
                       _p(r.get("logits")), _p(self.ws), nbytes)
 
-    def forward(self, x: torch.Tensor, residual: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
-        """(out, h): h is the residual of the next block."""
+    def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor]) -> Tuple[torch.Tensor, torch.Tensor]:
+        """(out, h): h is the residual of the next block; without one here (a model's first block) it is x itself."""
         if x.shape != self.normed["h"].shape:
             raise ValueError(f"x must be {tuple(self.normed['h'].shape)}")
         n = rms_norm(x, self.norm_weight, self.eps, residual=residual, out=self.normed)

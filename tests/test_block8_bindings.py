@@ -1,0 +1,81 @@
+"""What the bindings of the norm, the 8-bit matrices and the few-token layer hand to the library and give back, with the library replaced by one that records its
+calls: no GPU needed, and a call with wrong sizes reads nothing."""
+import pytest
+import torch
+
+from paper_2206_03382_amd import moe
+
+
+class Recorder:
+    """The library: every entry point succeeds, every size is 4096, and the last call of each is kept."""
+
+    def __init__(self):
+        self.calls = {}
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls[name] = args
+            return b"recorded" if name == "moe_status_string" else 4096 if name.endswith("_bytes") else 8 if name == "moe_capacity" else moe.OK
+        return call
+
+
+@pytest.fixture()
+def library(monkeypatch):
+    r = Recorder()
+    monkeypatch.setattr(moe, "lib", lambda: r)
+    monkeypatch.setattr(moe, "_p", lambda t: None if t is None else t.data_ptr())
+    monkeypatch.setattr(moe, "_stream", lambda: 0)
+    return r
+
+
+# ---- rms_norm's results, used again as `out` ------------------------------------------------------------------------
+
+def test_rms_norm_without_a_residual_gives_this_call_s_x(library):
+    a, b = torch.ones((4, 64)), torch.full((4, 64), 2.0)
+    first = moe.rms_norm(a, None, 1e-6)
+    assert first["h"] is a
+    again = moe.rms_norm(b, None, 1e-6, out=first)
+    assert again["h"] is b and library.calls["moe_rms_norm"][7] is None
+
+
+def test_rms_norm_with_a_residual_never_writes_into_an_earlier_x(library):
+    a, b, res = torch.ones((4, 64)), torch.full((4, 64), 2.0), torch.zeros((4, 64))
+    out = moe.rms_norm(a, None, 1e-6)
+    got = moe.rms_norm(b, None, 1e-6, residual=res, out=out)
+    to = library.calls["moe_rms_norm"][7]
+    assert to == got["h"].data_ptr() and to not in (a.data_ptr(), b.data_ptr(), res.data_ptr())
+    # from then on the same memory, calls without a residual in between or not
+    moe.rms_norm(a, None, 1e-6, out=got)
+    assert got["h"] is a
+    last = moe.rms_norm(a, None, 1e-6, residual=res, out=got)
+    assert library.calls["moe_rms_norm"][7] == to == last["h"].data_ptr()
+
+
+def test_rms_norm_writes_h_where_the_caller_says(library):
+    x, res, y = torch.ones((4, 64)), torch.zeros((4, 64)), torch.empty((4, 64))
+    mine = torch.empty((4, 64))
+    moe.rms_norm(x, None, 1e-6, residual=res, out={**moe.rms_norm(x, None, 1e-6), "h": mine})
+    assert library.calls["moe_rms_norm"][7] == mine.data_ptr()
+    plain = moe.rms_norm(x, None, 1e-6)
+    with pytest.raises(ValueError):
+        moe.rms_norm(x, None, 1e-6, residual=res, out={**plain, "y": y[:2]})
+    assert plain["h"] is x                                          # a refused call changes nothing
+    out = dict(h=res, y=y, y8=None)                                # the sum replaces the residual
+    got = moe.rms_norm(x, None, 1e-6, residual=res, out=out)
+    assert library.calls["moe_rms_norm"][7] == res.data_ptr() and got["h"] is res and got["y"] is y
+
+
+def test_norm_layer_without_a_residual(library):
+    """The first block of a model: h is x, and the next forward, with a residual, has its own h again."""
+    bf = torch.bfloat16
+    W1, W2 = moe._alloc8((4,), 128, 64, True, "cpu"), moe._alloc8((4,), 64, 128, True, "cpu")
+    for T in (8, 100):
+        layer = moe.NormMoELayer8(None, 1e-6, torch.zeros((64, 4), dtype=bf), None, W1, None, W2, None, T, 2, 1.0, 1, 0)
+        x, res = torch.ones((T, 64), dtype=bf), torch.zeros((T, 64), dtype=bf)
+        out, h = layer.forward(x, None)
+        assert h is x and out is layer.out
+        _, h = layer.forward(x, res)
+        own = library.calls["moe_rms_norm"][7]
+        assert h.data_ptr() == own and own not in (x.data_ptr(), res.data_ptr())
+        _, h = layer.forward(x, None)
+        assert h is x
