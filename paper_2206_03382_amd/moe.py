@@ -542,7 +542,9 @@ def _alloc8(lead: Tuple[int, ...], R: int, K: int, blocks: bool, device) -> Bloc
     return Block8(q, torch.empty((*lead, -(-R // 128) if blocks else R, sc), dtype=torch.uint8, device=device), K, blocks)
 
 
-def _check8(m: Block8, what: str) -> None:
+def _check8(m: Block8, what: str, dims: Optional[int] = None) -> None:
+    if dims is not None and m.q.dim() != dims:
+        raise ValueError(f"{what}: expected {'E matrices' if dims == 3 else 'one matrix'} in the 8-bit block format, not values of {m.q.dim()} dimensions")
     *lead, R, row = m.q.shape
     if m.s.shape != (*lead, -(-R // 128) if m.blocks else R, -(-m.width // 512) * 4) or row != -(-m.width // 128) * 128 \
             or m.q.dtype != torch.float8_e4m3fn or m.s.dtype != torch.uint8:
@@ -646,11 +648,11 @@ def matmul8(A: Block8, B: Block8, bias: Optional[torch.Tensor] = None, act: int 
             out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """out[e] = act(A[e] B[e]^T + bias[e]): A [E,C,K] (rows gathered from [rows,K] with gather [E,C]), B [E,N,K].  Rows past an expert's count are
     zero, or what `out` holds."""
-    _check8(A, "A")
-    _check8(B, "B")
+    _check8(A, "A", 3 if gather is None else 2)
+    _check8(B, "B", 3)
     E, N = B.q.shape[:2]
     C = gather.shape[1] if gather is not None else A.q.shape[1]
-    if A.blocks or A.width != B.width or (gather is None and A.q.shape[0] != E) or (gather is not None and (A.q.dim() != 2 or gather.shape[0] != E)):
+    if A.blocks or A.width != B.width or (gather is None and A.q.shape[0] != E):
         raise ValueError("A must have one exponent per row and block, and A, B and gather must agree in shape")
     _check_int32(counts, E)
     _check_int32(k_counts, E)
@@ -706,8 +708,8 @@ def expert_linear8_backward(dy: torch.Tensor, kept: Linear8Kept) -> Tuple[torch.
 
 
 def _check_ffn8(W1: Block8, b1, W2: Block8, b2, code: int) -> Tuple[int, int, int]:
-    _check8(W1, "W1")
-    _check8(W2, "W2")
+    _check8(W1, "W1", 3)
+    _check8(W2, "W2", 3)
     E, H, M = W1.q.shape[0], W1.q.shape[1], W1.width
     if not W1.blocks or not W2.blocks or W2.q.shape[:2] != (E, M) or W2.width != H:
         raise ValueError("W1 must be [E,H,M] and W2 [E,M,H] with one exponent for 128 x 128 values")
@@ -722,12 +724,12 @@ def expert_ffn8(x8: Block8, W1: Block8, b1: Optional[torch.Tensor], W2: Block8, 
                 slot_src: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The experts' layer on 8-bit tokens and weights (quantize8's transposed forms of W1 [E,M,H] and W2 [E,H,M], blocks=True): x8 [E,C,M], or
     the tokens [T,M] with slot_src [E,C]."""
-    _check8(x8, "x8")
+    _check8(x8, "x8", 3 if slot_src is None else 2)
     dev = x8.q.device
     code = F32 if dtype == torch.float32 else BF16
     E, M, H = _check_ffn8(W1, b1, W2, b2, code)
     C = slot_src.shape[1] if slot_src is not None else x8.q.shape[1]
-    if x8.blocks or x8.width != M or (slot_src is None and x8.q.shape[0] != E) or (slot_src is not None and (x8.q.dim() != 2 or slot_src.shape[0] != E)):
+    if x8.blocks or x8.width != M or (slot_src is None and x8.q.shape[0] != E):
         raise ValueError("x8 must be [E,C,M], or [T,M] with slot_src [E,C]")
     _check_int32(counts, E)
     _check_int32(slot_src, E, C)

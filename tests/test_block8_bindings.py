@@ -79,3 +79,37 @@ def test_norm_layer_without_a_residual(library):
         assert h.data_ptr() == own and own not in (x.data_ptr(), res.data_ptr())
         _, h = layer.forward(x, None)
         assert h is x
+
+
+# ---- shapes of 8-bit matrices: a product reads what they say ------------------------------------------------------------
+
+def matrix8(*shape, blocks=False):
+    *lead, R, K = shape
+    return moe._alloc8(tuple(lead), R, K, blocks, "cpu")
+
+
+def test_matmul8_refuses_plain_matrices(library):
+    """Two [256, 512] operands pass for 256 experts of [512, 512] if rows are taken for experts."""
+    plain, stack = matrix8(256, 512), matrix8(2, 16, 128)
+    four = moe.Block8(stack.q[None], stack.s[None], 128, False)
+    rows = torch.zeros((2, 16), dtype=torch.int32)
+    for A, B, gather in [(plain, plain, None), (plain, matrix8(256, 512, blocks=True), None), (stack, matrix8(16, 128), None), (four, four, None), (stack, four, None),
+                         (four, stack, None), (stack, stack, rows), (four, stack, rows), (matrix8(2, 128), matrix8(2, 128), rows)]:
+        with pytest.raises(ValueError):
+            moe.matmul8(A, B, gather=gather)
+    assert "moe_matmul8" not in library.calls
+    assert moe.matmul8(stack, stack).shape == (2, 16, 16) and moe.matmul8(matrix8(9, 128), stack, gather=rows).shape == (2, 16, 16)
+    assert library.calls["moe_matmul8"][12:16] == (2, 16, 128, 16)
+
+
+def test_expert_ffn8_refuses_plain_matrices(library):
+    W1, W2 = matrix8(4, 256, 128, blocks=True), matrix8(4, 128, 256, blocks=True)
+    slots = torch.zeros((4, 16), dtype=torch.int32)
+    for x8, a, b, s in [(matrix8(4, 128), W1, W2, None), (matrix8(1, 9, 128), W1, W2, slots), (matrix8(1, 4, 16, 128), W1, W2, None),
+                        (matrix8(4, 16, 128), matrix8(128, 128, blocks=True), matrix8(128, 128, blocks=True), None)]:
+        with pytest.raises(ValueError):
+            moe.expert_ffn8(x8, a, None, b, None, moe.ACT_RELU, slot_src=s)
+    with pytest.raises(ValueError):
+        moe.FewTokenLayer(torch.zeros((128, 128), dtype=torch.bfloat16), None, matrix8(128, 128, blocks=True), None, matrix8(128, 128, blocks=True), None, 4, 1, 1.0, 0, 0)
+    assert not any(name.startswith(("moe_expert", "moe_layer")) for name in library.calls)
+    assert moe.expert_ffn8(matrix8(4, 16, 128), W1, None, W2, None, moe.ACT_RELU).shape == (4, 16, 128)
