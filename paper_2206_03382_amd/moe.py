@@ -661,6 +661,8 @@ def matmul8(A: Block8, B: Block8, bias: Optional[torch.Tensor] = None, act: int 
         out = (torch.empty if counts is None else torch.zeros)((E, C, N), dtype=dtype, device=B.q.device)
     else:
         _check_out(out, (E, C, N), out.dtype)
+    if bias is not None and tuple(bias.shape) != (E, N):
+        raise ValueError("bias must be [E,N]")
     _check_storage(_dtype_code(out), bias)
     _check(lib().moe_matmul8(_p(A.q), _p(A.s), _p(B.q), _p(B.s), SCALE_BLOCKS if B.blocks else SCALE_ROWS, _p(bias), act, _dtype_code(out),
                              _p(counts), _p(k_counts), _p(gather), A.q.shape[0] if gather is not None else 0, E, C, A.width, N, _p(out),

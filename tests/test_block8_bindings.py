@@ -113,3 +113,12 @@ def test_expert_ffn8_refuses_plain_matrices(library):
         moe.FewTokenLayer(torch.zeros((128, 128), dtype=torch.bfloat16), None, matrix8(128, 128, blocks=True), None, matrix8(128, 128, blocks=True), None, 4, 1, 1.0, 0, 0)
     assert not any(name.startswith(("moe_expert", "moe_layer")) for name in library.calls)
     assert moe.expert_ffn8(matrix8(4, 16, 128), W1, None, W2, None, moe.ACT_RELU).shape == (4, 16, 128)
+
+
+def test_matmul8_checks_the_bias(library):
+    A, B = matrix8(2, 16, 128), matrix8(2, 24, 128)
+    for bad in (torch.zeros(24, dtype=torch.bfloat16), torch.zeros((2, 16), dtype=torch.bfloat16), torch.zeros((1, 24), dtype=torch.bfloat16), torch.zeros((2, 24))):
+        with pytest.raises(ValueError):
+            moe.matmul8(A, B, bias=bad)
+    assert "moe_matmul8" not in library.calls
+    moe.matmul8(A, B, bias=torch.zeros((2, 24), dtype=torch.bfloat16))
