@@ -709,15 +709,19 @@ def expert_linear8_backward(dy: torch.Tensor, kept: Linear8Kept) -> Tuple[torch.
     return dx, dW
 
 
+def _check_biases(E: int, M: int, H: int, b1, b2, code: int) -> None:
+    if (b1 is not None and tuple(b1.shape) != (E, H)) or (b2 is not None and tuple(b2.shape) != (E, M)):
+        raise ValueError("b1 must be [E,H] and b2 [E,M]")
+    _check_storage(code, b1, b2)
+
+
 def _check_ffn8(W1: Block8, b1, W2: Block8, b2, code: int) -> Tuple[int, int, int]:
     _check8(W1, "W1", 3)
     _check8(W2, "W2", 3)
     E, H, M = W1.q.shape[0], W1.q.shape[1], W1.width
     if not W1.blocks or not W2.blocks or W2.q.shape[:2] != (E, M) or W2.width != H:
         raise ValueError("W1 must be [E,H,M] and W2 [E,M,H] with one exponent for 128 x 128 values")
-    if (b1 is not None and tuple(b1.shape) != (E, H)) or (b2 is not None and tuple(b2.shape) != (E, M)):
-        raise ValueError("b1 must be [E,H] and b2 [E,M]")
-    _check_storage(code, b1, b2)
+    _check_biases(E, M, H, b1, b2, code)
     return E, M, H
 
 
@@ -765,7 +769,8 @@ class FewTokenLayer:
             w1, s1, w2, s2 = W1.q, W1.s, W2.q, W2.s
         else:
             self.E, self.M, self.H = W1.shape
-            _check_storage(code, W1, b1, W2, b2)
+            _check_storage(code, W1, W2)
+            _check_biases(self.E, self.M, self.H, b1, b2, code)
             w1, s1, w2, s2 = W1, None, W2, None
         if tuple(Wg.shape) != (self.M, self.E) or (s1 is None and tuple(W2.shape) != (self.E, self.H, self.M)):
             raise ValueError("Wg must be [M,E], W1 [E,M,H] and W2 [E,H,M]")

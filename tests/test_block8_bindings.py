@@ -122,3 +122,19 @@ def test_matmul8_checks_the_bias(library):
             moe.matmul8(A, B, bias=bad)
     assert "moe_matmul8" not in library.calls
     moe.matmul8(A, B, bias=torch.zeros((2, 24), dtype=torch.bfloat16))
+
+
+def few_layer(gate_bias=None, b1=None, b2=None, w8=False):
+    bf = torch.bfloat16
+    W1, W2 = (matrix8(4, 128, 64, blocks=True), matrix8(4, 64, 128, blocks=True)) if w8 else (torch.zeros((4, 64, 128), dtype=bf), torch.zeros((4, 128, 64), dtype=bf))
+    return moe.FewTokenLayer(torch.zeros((64, 4), dtype=bf), gate_bias, W1, b1, W2, b2, 8, 2, 1.0, 1, 0)
+
+
+@pytest.mark.parametrize("w8", [False, True])
+def test_few_token_layer_checks_the_experts_biases(library, w8):
+    bf = dict(dtype=torch.bfloat16)
+    for b1, b2 in [(torch.zeros(128, **bf), None), (torch.zeros((4, 64), **bf), None), (torch.zeros((4, 128)), None), (None, torch.zeros(64, **bf)),
+                   (None, torch.zeros((4, 128), **bf)), (None, torch.zeros((1, 64), **bf))]:
+        with pytest.raises(ValueError):
+            few_layer(None, b1, b2, w8)
+    few_layer(None, torch.zeros((4, 128), **bf), torch.zeros((4, 64), **bf), w8)
