@@ -715,6 +715,13 @@ def _check_biases(E: int, M: int, H: int, b1, b2, code: int) -> None:
     _check_storage(code, b1, b2)
 
 
+def _check_gate(Wg: torch.Tensor, gate_bias: Optional[torch.Tensor], M: int, E: int) -> None:
+    if tuple(Wg.shape) != (M, E):
+        raise ValueError("Wg must be [M,E]")
+    if gate_bias is not None and (gate_bias.dtype != torch.float32 or gate_bias.numel() != E):
+        raise ValueError("gate_bias must be [E] in float32")
+
+
 def _check_ffn8(W1: Block8, b1, W2: Block8, b2, code: int) -> Tuple[int, int, int]:
     _check8(W1, "W1", 3)
     _check8(W2, "W2", 3)
@@ -772,8 +779,9 @@ class FewTokenLayer:
             _check_storage(code, W1, W2)
             _check_biases(self.E, self.M, self.H, b1, b2, code)
             w1, s1, w2, s2 = W1, None, W2, None
-        if tuple(Wg.shape) != (self.M, self.E) or (s1 is None and tuple(W2.shape) != (self.E, self.H, self.M)):
-            raise ValueError("Wg must be [M,E], W1 [E,M,H] and W2 [E,H,M]")
+        _check_gate(Wg, gate_bias, self.M, self.E)
+        if s1 is None and tuple(W2.shape) != (self.E, self.H, self.M):
+            raise ValueError("W1 must be [E,M,H] and W2 [E,H,M]")
         dev = Wg.device
         nbytes = int(lib().moe_layer_few_workspace_bytes(T, self.M, self.H, self.E, k, code))
         if nbytes == 0:
@@ -803,8 +811,7 @@ class NormMoELayer8:
         self.few = FewTokenLayer(Wg, gate_bias, W1, b1, W2, b2, T, k, f, normalize, act, keep_routing) if T <= FEW_MAX_TOKENS else None
         code = _dtype_code(Wg)
         E, M, H = _check_ffn8(W1, b1, W2, b2, code)
-        if tuple(Wg.shape) != (M, E):
-            raise ValueError("Wg must be [M,E]")
+        _check_gate(Wg, gate_bias, M, E)
         dev = Wg.device
         self.normed = dict(h=torch.empty((T, M), dtype=Wg.dtype, device=dev), y=torch.empty((T, M), dtype=Wg.dtype, device=dev),
                            y8=None if self.few else _alloc8((), T, M, False, dev))

@@ -138,3 +138,17 @@ def test_few_token_layer_checks_the_experts_biases(library, w8):
         with pytest.raises(ValueError):
             few_layer(None, b1, b2, w8)
     few_layer(None, torch.zeros((4, 128), **bf), torch.zeros((4, 64), **bf), w8)
+
+
+def test_layers_check_the_gate_bias(library):
+    bf = torch.bfloat16
+    W1, W2 = matrix8(4, 128, 64, blocks=True), matrix8(4, 64, 128, blocks=True)
+
+    def norm_layer(bias, T):
+        return moe.NormMoELayer8(None, 1e-6, torch.zeros((64, 4), dtype=bf), bias, W1, None, W2, None, T, 2, 1.0, 1, 0)
+    for bad in (torch.zeros(4, dtype=bf), torch.zeros(3), torch.zeros(4, dtype=torch.float64), torch.zeros((4, 4))):
+        for make in (few_layer, lambda b: norm_layer(b, 8), lambda b: norm_layer(b, 100)):
+            with pytest.raises(ValueError):
+                make(bad)
+    for make in (few_layer, lambda b: norm_layer(b, 8), lambda b: norm_layer(b, 100)):
+        make(torch.zeros(4))
