@@ -623,6 +623,8 @@ def rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: Optional[torch.
 def quantize8(src: torch.Tensor, blocks: bool = False, rows: bool = True, transposed: bool = False,
               counts: Optional[torch.Tensor] = None) -> Tuple[Optional[Block8], Optional[Block8]]:
     """(src [E,R,K] or [R,K] in 8 bits, its transpose in 8 bits): what is asked for, from one read."""
+    if src.dim() not in (2, 3):
+        raise ValueError("src must be [E,R,K] or [R,K]")
     lead, (R, K) = tuple(src.shape[:-2]), src.shape[-2:]
     E = lead[0] if lead else 1
     _check_int32(counts, E)
@@ -635,7 +637,8 @@ def quantize8(src: torch.Tensor, blocks: bool = False, rows: bool = True, transp
 
 
 def dequantize8(m: Block8, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
-    _check8(m, "m")
+    """Back to values [E,R,K] or [R,K]."""
+    _check8(m, "m", 2 if m.q.dim() == 2 else 3)
     lead, R = tuple(m.q.shape[:-2]), m.q.shape[-2]
     out = torch.empty((*lead, R, m.width), dtype=dtype, device=m.q.device)
     _check(lib().moe_dequantize8(_p(m.q), _p(m.s), SCALE_BLOCKS if m.blocks else SCALE_ROWS, lead[0] if lead else 1, R, m.width,

@@ -152,3 +152,15 @@ def test_layers_check_the_gate_bias(library):
                 make(bad)
     for make in (few_layer, lambda b: norm_layer(b, 8), lambda b: norm_layer(b, 100)):
         make(torch.zeros(4))
+
+
+def test_more_leading_dimensions_are_refused(library):
+    """The library takes one leading dimension; of more, all but the first matrices were left unwritten."""
+    with pytest.raises(ValueError):
+        moe.quantize8(torch.zeros((2, 3, 16, 128)))
+    with pytest.raises(ValueError):
+        moe.dequantize8(matrix8(2, 3, 16, 128))
+    assert not library.calls
+    for shape in ((16, 128), (2, 16, 128)):
+        q, _ = moe.quantize8(torch.zeros(shape))
+        assert tuple(moe.dequantize8(q).shape) == shape
