@@ -567,10 +567,10 @@ def _check_int32(t: Optional[torch.Tensor], *shape: int) -> None:
         raise ValueError(f"counts and indices must be int32 {list(shape)}")
 
 
-def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float, residual: Optional[torch.Tensor] = None, want_y: bool = True,
-             want_8: bool = False, out: Optional[Dict] = None) -> Dict:
-    """h = x + residual (x itself without one), y = RMS norm of h times weight, y8 = the same in 8 bits; `out`: an earlier result of the same
-    shapes to write into.  Without a residual nothing is written for h: the result names x and, under "spare", that x and the memory that a later call
+def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float, residual: Optional[torch.Tensor] = None, want_y: Optional[bool] = None,
+             want_8: Optional[bool] = None, out: Optional[Dict] = None) -> Dict:
+    """h = x + residual (x itself without one), y = RMS norm of h times weight (unless want_y is False), y8 = the same in 8 bits (if want_8 is True).
+    `out`: an earlier result of the same shapes to write into, all that it has memory for.  Without a residual nothing is written for h: the result names x and, under "spare", that x and the memory that a later call
     with a residual writes instead of it (None: the call allocates)."""
     T, M = x.shape
     code = _dtype_code(x)
@@ -578,10 +578,12 @@ def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float, residu
         raise ValueError("residual must have x's shape and weight its width")
     _check_storage(code, residual, weight)
     if out is None:
-        out = dict(h=None, y=torch.empty_like(x) if want_y else None, y8=_alloc8((), T, M, False, x.device) if want_8 else None)
+        out = dict(h=None, y=torch.empty_like(x) if want_y is None or want_y else None, y8=_alloc8((), T, M, False, x.device) if want_8 else None)
     h, y, y8 = out["h"], out["y"], out["y8"]
     if "spare" in out and h is out["spare"][0]:
         h = out["spare"][1]
+    if (want_y and y is None) or (want_8 and y8 is None):
+        raise ValueError("out has no memory for what is wanted")
     _check_out(h, x.shape, x.dtype)
     _check_out(y, x.shape, x.dtype)
     if y8 is not None:

@@ -164,3 +164,20 @@ def test_more_leading_dimensions_are_refused(library):
     for shape in ((16, 128), (2, 16, 128)):
         q, _ = moe.quantize8(torch.zeros(shape))
         assert tuple(moe.dequantize8(q).shape) == shape
+
+
+def test_rms_norm_refuses_outputs_that_out_has_no_memory_for(library):
+    x = torch.ones((4, 128))
+    only_8, only_y = moe.rms_norm(x, None, 1e-6, want_y=False, want_8=True), moe.rms_norm(x, None, 1e-6)
+    for kept, asked in [(only_8, dict(want_y=True)), (only_y, dict(want_8=True)), (only_8, dict(want_y=True, want_8=True))]:
+        library.calls.clear()
+        with pytest.raises(ValueError):
+            moe.rms_norm(x, None, 1e-6, out=kept, **asked)
+        assert not library.calls
+    for kept, y, y8 in [(only_8, False, True), (only_y, True, False)]:          # without a word: what `out` has
+        got = moe.rms_norm(x, None, 1e-6, out=kept)
+        assert (got["y"] is not None, got["y8"] is not None) == (y, y8)
+        moe.rms_norm(x, None, 1e-6, out=kept, want_y=y, want_8=y8)
+    both = moe.rms_norm(x, None, 1e-6, want_8=True)
+    moe.rms_norm(x, None, 1e-6, want_y=False, out=both)                         # all of them are this call's
+    assert library.calls["moe_rms_norm"][8] == both["y"].data_ptr()
