@@ -683,7 +683,7 @@ __global__ __launch_bounds__(64 * kFewWaves, TILES == 1 && STAGE != kFewUpAlone 
     auto done = [&](int r, int64_t n, float s) {
       if (bias && part == 0) s += load_as_f32(bias + (int64_t)e * N + n);
       const int64_t q = pair_of[r];
-      if (UP && parts == 1) store_from_f32((ET*)p.hidden + q * N + n, apply_act(s, p.act));
+      if (UP && parts == 1) store_from_f32((ET*)p.hidden + q * N + n, act_full(s, p.act));
       else if (!UP && p.k == 1 && parts == 1) store_from_f32((ET*)p.out + q * N + n, p.gate_w[q] * s);
       else __hip_atomic_store(p.partial + (part * pairs + q) * N + n, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     };
@@ -720,7 +720,7 @@ __global__ __launch_bounds__(64 * kFewWaves, TILES == 1 && STAGE != kFewUpAlone 
       float s = 0.f;
 #pragma unroll
       for (int u = 0; u < 1 << kFewPartBits; ++u) s += u < parts ? v[u] : 0.f;
-      store_from_f32((ET*)p.hidden + q * N + n, apply_act(s, p.act));
+      store_from_f32((ET*)p.hidden + q * N + n, act_full(s, p.act));
     }
     return;
   }

@@ -181,7 +181,7 @@ __global__ __launch_bounds__(256, 2) void matmul8_kernel(const Args8 a) {
         f32x4 v = acc[i][j];
         if (p.act >= 0)
 #pragma unroll
-          for (int c = 0; c < 4; ++c) v[c] = apply_act(v[c], p.act);
+          for (int c = 0; c < 4; ++c) v[c] = act_full(v[c], p.act);
         if (r >= live || n >= N) continue;                          // N is a multiple of 8
         if (p.dtype == MOE_F32) *reinterpret_cast<f32x4*>((float*)p.out + at) = v;
         else *reinterpret_cast<uint2*>((uint16_t*)p.out + at) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
@@ -201,7 +201,7 @@ __global__ __launch_bounds__(256, 2) void matmul8_kernel(const Args8 a) {
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         float v = acc[i][j][c];
-        if constexpr (EXACT) v = p.act >= 0 ? apply_act(v, p.act) : v;
+        if constexpr (EXACT) v = p.act >= 0 ? act_full(v, p.act) : v;
         else v = act8<ACT>(v);
         if (n0 + wn * 64 + j * 16 + 4 * g >= N) v = 0.f;
         acc[i][j][c] = v;
