@@ -387,7 +387,9 @@ int moe_matmul8(const void* A, const uint8_t* A_scales, const void* B, const uin
 /* A projection of the experts in 8 bits, trained: y[e] = q(x[e]) q(W[e]), and from dy its gradients dx[e] = q(dy[e]) q(W[e])^T, dW[e] = q(x[e]^T) q(dy[e]^T)^T, every operand
  * quantised along the axis that its product sums over (W once, with an exponent for 128 x 128 values).
  *   x, dx [E,C,K], W, dW [E,K,N], y, dy [E,C,N] in `dtype`; K and N multiples of 8; dx or dW may be NULL.
- *   counts [E] int32 or NULL: only the first min(counts[e], C) rows of x and dy are read; the others of y and dx are zeros.
+ *   counts [E] int32 or NULL: only the first min(counts[e], C) rows of x and dy are read; the others of y and dx are zeros.  The
+ *   forward keeps them in the state, and the backward goes by those: its own `counts` only says that there are any, and has to be NULL if and only if
+ *   the forward's was.
  *   state: moe_expert_linear8_state_bytes (0: unsupported) bytes, 256-byte aligned, the same for both calls; its layout is private, and one state serves one call at a time.  The
  *   backward may be called more than once. */
 size_t moe_expert_linear8_state_bytes(int64_t E, int64_t C, int64_t K, int64_t N);

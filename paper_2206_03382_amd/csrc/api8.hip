@@ -97,9 +97,10 @@ int layer_shape_status(int64_t T, int64_t M, int64_t H, int64_t E, int k, int dt
   return row_shape_status(H);
 }
 
-// A projection's training pass: what the forward keeps (x transposed, W as it is), and behind it what one call needs for itself (forward: x, W transposed; backward: dy in both forms).
+// A projection's training pass: what the forward keeps (x transposed, W as it is), behind it what one call needs for itself (forward: x, W transposed; backward: dy in both
+// forms), and at the end the fills that the forward saw.
 struct Linear8State {
-  size_t xt, xt_scales, W, W_scales, x, x_scales, Wt, Wt_scales, dy, dy_scales, dyt, dyt_scales, total;
+  size_t xt, xt_scales, W, W_scales, x, x_scales, Wt, Wt_scales, dy, dy_scales, dyt, dyt_scales, fills, total;
 };
 
 Linear8State linear8_layout(int64_t E, int64_t C, int64_t K, int64_t N) {
@@ -116,11 +117,12 @@ Linear8State linear8_layout(int64_t E, int64_t C, int64_t K, int64_t N) {
   const size_t kept = off;
   rows(w.x, w.x_scales, C, K, false);
   rows(w.Wt, w.Wt_scales, N, K, true);
-  w.total = off;
+  w.fills = off;
   off = kept;
   rows(w.dy, w.dy_scales, C, N, false);
   rows(w.dyt, w.dyt_scales, N, C, false);
-  w.total = off > w.total ? off : w.total;
+  w.fills = off > w.fills ? off : w.fills;
+  w.total = w.fills + (size_t)E * 4;
   return w;
 }
 
@@ -231,7 +233,8 @@ int moe_expert_linear8_train(const void* x, const void* W, int dtype, const int3
   if (state_bytes < w.total) return MOE_WORKSPACE_TOO_SMALL;
   uint8_t* b = (uint8_t*)state;
   const hipStream_t s = (hipStream_t)stream;
-  if (launch_quantize8(x, dtype, counts, E, C, K, false, b + w.x, b + w.x_scales, b + w.xt, b + w.xt_scales, s, counts ? y : nullptr, N) != hipSuccess ||
+  if (launch_quantize8(x, dtype, counts, E, C, K, false, b + w.x, b + w.x_scales, b + w.xt, b + w.xt_scales, s, counts ? (int32_t*)(b + w.fills) : nullptr,
+                       counts ? y : nullptr, N) != hipSuccess ||
       launch_quantize8(W, dtype, nullptr, E, K, N, true, b + w.W, b + w.W_scales, b + w.Wt, b + w.Wt_scales, s) != hipSuccess)
     return MOE_HIP_ERROR;
   const Matmul8 p = {b + w.x, b + w.x_scales, b + w.Wt, b + w.Wt_scales, 1, nullptr, MOE_ACT_NONE, counts, nullptr, nullptr, 0, E, C, K, N, 0, dtype, y, nullptr, nullptr};
@@ -247,8 +250,11 @@ int moe_expert_linear8_backward(const void* dy, int dtype, const int32_t* counts
   if (state_bytes < w.total) return MOE_WORKSPACE_TOO_SMALL;
   uint8_t* b = (uint8_t*)state;
   const hipStream_t s = (hipStream_t)stream;
+  // The forward's fills, not what the caller's counts hold by now: of the transposed x only their blocks were written.  (Without counts the products need no loads of them: 1 % of 8 experts
+  // x 4096 rows, 2048 x 2048.)
+  if (counts) counts = (const int32_t*)(b + w.fills);
   if (launch_quantize8(dy, dtype, counts, E, C, N, false, dx ? b + w.dy : nullptr, dx ? b + w.dy_scales : nullptr, dW ? b + w.dyt : nullptr,
-                       dW ? b + w.dyt_scales : nullptr, s, counts ? dx : nullptr, K) != hipSuccess)
+                       dW ? b + w.dyt_scales : nullptr, s, nullptr, counts ? dx : nullptr, K) != hipSuccess)
     return MOE_HIP_ERROR;
   const Matmul8 px = {b + w.dy, b + w.dy_scales, b + w.W, b + w.W_scales, 1, nullptr, MOE_ACT_NONE, counts, nullptr, nullptr, 0, E, C, N, K, 0, dtype, dx, nullptr, nullptr};
   if (dx && launch_matmul8(px, s) != hipSuccess) return MOE_HIP_ERROR;

@@ -77,9 +77,10 @@ hipError_t launch_rms_norm(const void* x, const void* residual, const void* weig
 size_t rms_norm_backward_workspace_bytes(int64_t T, int64_t M);
 hipError_t launch_rms_norm_backward(const void* dy, const void* dh, const void* h, const void* weight, float eps, int dtype, int64_t T,
                                     int64_t M, float* ws, void* dx, void* dweight, hipStream_t s);
+// fills [E]: gets min(counts[e], R), not below 0.  zeros [E, R, zero_width] in dtype: rows past the counts get zeros.
 hipError_t launch_quantize8(const void* src, int dtype, const int32_t* counts, int64_t E, int64_t R, int64_t K, bool blocks, void* q,
-                            uint8_t* scales, void* qt, uint8_t* scales_t, hipStream_t s, void* zeros = nullptr, int64_t zero_width = 0);   // zeros [E, R, zero_width] in dtype: rows past
-                                                                                                                                   // the counts get zeros
+                            uint8_t* scales, void* qt, uint8_t* scales_t, hipStream_t s, int32_t* fills = nullptr, void* zeros = nullptr,
+                            int64_t zero_width = 0);
 hipError_t launch_dequantize8(const void* q, const uint8_t* scales, bool blocks, int64_t E, int64_t R, int64_t K, int dtype, void* out,
                               hipStream_t s);
 

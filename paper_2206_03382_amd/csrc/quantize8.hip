@@ -30,17 +30,19 @@ template <> __device__ __forceinline__ void load8<float>(const float* p, float (
 // 8-byte pieces of both forms.  The transposed form goes through LDS (16 KB, 8-byte pieces, the pair of piece p of column c at p/2 ^ c/8 % 8: lanes of a
 // wave write to different banks) and out in rows of 128 bytes.
 // BLOCKS: one exponent for the tile; else one for each row and column of it.  Rows past an expert's fill count as zero: the transposed form has
-// zeros there up to the end of its block; tiles that lie past it altogether are left alone.  zeros: a matrix of R rows of zero_pieces 16 bytes for each expert that gets zeros in those rows.
+// zeros there up to the end of its block; tiles that lie past it altogether are left alone.  fills: gets the experts' live rows.  zeros: a matrix of R rows of zero_pieces 16 bytes for each expert that gets zeros in those rows.
 template <typename ET, bool BLOCKS>
 __global__ __launch_bounds__(256, 4) void quantize8_kernel(const ET* __restrict__ src, const int32_t* __restrict__ counts, int R, int K, int tiles_k,
                                                         uint8_t* __restrict__ q, uint8_t* __restrict__ scales, uint8_t* __restrict__ qt,
-                                                        uint8_t* __restrict__ scales_t, int row8, int row_sc, int col8, int col_sc, uint4* __restrict__ zeros, int zero_pieces) {
+                                                        uint8_t* __restrict__ scales_t, int row8, int row_sc, int col8, int col_sc, int32_t* __restrict__ fills,
+                                                        uint4* __restrict__ zeros, int zero_pieces) {
   __shared__ __attribute__((aligned(16))) uint8_t tile[kBlock8 * kBlock8];
   __shared__ uint32_t tops[16][kBlock8];
   __shared__ uint8_t exponents[2][kBlock8];
   const int64_t e = blockIdx.y;
   const int rb = blockIdx.x / tiles_k, kb = blockIdx.x - rb * tiles_k;
   const int rows = live_rows(e, R, counts);
+  if (fills && blockIdx.x == 0 && threadIdx.x == 0) fills[e] = rows;
   if (zeros) {                                                      // the same rows of another matrix, those that do not exist: shared by the tiles of a row of them
     const int first = max(rows, rb * kBlock8), last = min(R, (rb + 1) * kBlock8);
     uint4* to = zeros + (e * R + first) * (int64_t)zero_pieces;
@@ -180,12 +182,13 @@ __global__ __launch_bounds__(256) void dequantize8_kernel(const uint8_t* __restr
 }  // namespace
 
 hipError_t launch_quantize8(const void* src, int dtype, const int32_t* counts, int64_t E, int64_t R, int64_t K, bool blocks, void* q,
-                            uint8_t* scales, void* qt, uint8_t* scales_t, hipStream_t s, void* zeros, int64_t zero_width) {
+                            uint8_t* scales, void* qt, uint8_t* scales_t, hipStream_t s, int32_t* fills, void* zeros,
+                            int64_t zero_width) {
   const dim3 grid((unsigned)(ceil_div(K, kBlock8) * ceil_div(R, kBlock8)), (unsigned)E);
 #define MOE_QUANTIZE(ET, B)                                                                                                           \
   quantize8_kernel<ET, B><<<grid, dim3(256), 0, s>>>((const ET*)src, counts, (int)R, (int)K, (int)ceil_div(K, kBlock8), (uint8_t*)q, scales, (uint8_t*)qt, scales_t, \
                                                      (int)row_bytes8(K), (int)row_scales8(K), (int)row_bytes8(R), (int)row_scales8(R), \
-                                                     (uint4*)zeros, (int)(zero_width * (dtype == MOE_F32 ? 4 : 2) / 16))
+                                                     fills, (uint4*)zeros, (int)(zero_width * (dtype == MOE_F32 ? 4 : 2) / 16))
   if (dtype == MOE_F32) { if (blocks) MOE_QUANTIZE(float, true); else MOE_QUANTIZE(float, false); }
   else { if (blocks) MOE_QUANTIZE(uint16_t, true); else MOE_QUANTIZE(uint16_t, false); }
 #undef MOE_QUANTIZE

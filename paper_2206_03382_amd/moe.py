@@ -676,7 +676,7 @@ def matmul8(A: Block8, B: Block8, bias: Optional[torch.Tensor] = None, act: int 
 
 
 class Linear8Kept(NamedTuple):
-    """What expert_linear8_backward needs of the forward."""
+    """What expert_linear8_backward needs of the forward; the counts' values as they were then are in the state."""
     state: torch.Tensor
     counts: Optional[torch.Tensor]
     shape: Tuple[int, int, int, int]                           # E, C, K, N
