@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "block8.h"
+#include "few_rules.h"
 #include "ffn_device.h"
 
 namespace moe {
@@ -784,14 +785,10 @@ template <typename ET, bool W8, int C, int STAGE> void launch_few_units(FewToken
   else if constexpr (STAGE != kFewUpAlone) few_kernel<ET, W8, C, 4, STAGE><<<grid, block, 0, s>>>(p);
 }
 
-// Blocks of 64 columns where there are enough of them for three quarters of their places (two to a CU with one tile of rows, one with four), else of 32: more blocks, and more
-// places taken, for more reads of the rows.  Rows of 32 columns of bf16 weights are half a line of 128 bytes: always 64.
-// A layer of 8-bit weights, us with 64 and with 32 columns (blocks of a product with 64): 1 token x 2 experts of 4096 x 4096 (128) 42.4, 37.3;
-// 16 x 8 of 2048 x 2048 (256) 37.2, 35.1; 16 x 32 of 1024 x 1024 (512) 49.1, 64.0; 64 x 16 of 4096 x 1024 (256 and 1024) 152.8, 171.7; 24 x 4 of 768 x 512 (32 and 48) 23.1, 21.3.
 template <typename ET, bool W8, int STAGE> void launch_few_product(const FewTokens& p, hipStream_t s) {
-  const int64_t blocks = ceil_div(STAGE != kFewDown ? p.H : p.M, 64) * few_units(p);
-  if constexpr (!W8 && sizeof(ET) == 2) launch_few_units<ET, W8, 4, STAGE>(p, s);
-  else if (blocks >= (p.T <= 16 ? 384 : 192)) launch_few_units<ET, W8, 4, STAGE>(p, s);
+  constexpr bool kBf16 = !W8 && sizeof(ET) == 2;
+  if constexpr (kBf16) launch_few_units<ET, W8, 4, STAGE>(p, s);
+  else if (few_columns(p.T, few_units(p), STAGE != kFewDown ? p.H : p.M, kBf16) == 64) launch_few_units<ET, W8, 4, STAGE>(p, s);
   else launch_few_units<ET, W8, 2, STAGE>(p, s);
 }
 
@@ -828,10 +825,7 @@ size_t few_partial_bytes(int64_t T, int64_t M, int64_t H, int64_t E, int k) {
 
 hipError_t launch_few_tokens(const FewTokens& given, hipStream_t s) {
   FewTokens p = given;
-  // The plan by every block of the first product for itself, or, where they do not all run at once (two to a CU, or one of more than 16 tokens), in a launch of its own.
-  // us, first and then: 16 tokens x 8 experts of 2048 x 2048 (256 blocks) 41.1, 42.8; 1 x 8 of 128 of 4096 x 1024, 8 bits (128) 42.3, 44.1; 4 x 8 of 64 of 1024 x 4096 (512)
-  // 44.2, 46.3; 16 x 64 of 128 of 1024 x 1024, 8 bits (1024) 61.2, 58.5; 64 x 64 of 1024 x 4096 (4096) 264.7, 213.8.
-  p.planned = ceil_div(p.H, 64) * few_units(p) > (p.T <= 16 ? 512 : 256);
+  p.planned = few_planned(p.T, p.H, p.E, p.k, p.dtype == MOE_BF16 && !p.s1);
   p.alone = !p.planned && p.T <= kAloneTokens && p.E <= kAloneExperts && p.T * p.E * p.M <= kAloneWork;
   p.slice_bits = few_slice_bits(p.T, p.M);
   p.expert_bits = p.token_bits = 0;                                 // as many threads to an expert, and to a token, as there are
