@@ -160,7 +160,7 @@ template <typename ET, int C> struct Few<ET, true, C> {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {                             // the upper 16 bits, of what is left the upper 16, and what is left then: exact
             const float v = __uint_as_float(x[t].x[q][j >> 2][j & 3]);
-            const float hi = __uint_as_float(__float_as_uint(v) & 0xffff0000u), r1 = v - hi;
+            const float hi = __uint_as_float(__float_as_uint(v) & 0xffff0000u), r1 = __builtin_isinf(v) ? 0.f : v - hi;      // nothing is left of an infinity
             const float mid = __uint_as_float(__float_as_uint(r1) & 0xffff0000u);
             a[0][j] = (__bf16)hi;
             a[1][j] = (__bf16)mid;

@@ -87,3 +87,25 @@ def test_few_tokens(moe, T, M, H, E, k, kind, act):
     got = first.forward(x)
     has = (first.routing["idx"] == e).any(1)
     assert torch.isnan(got[has]).all() and torch.equal(got[~has], clean[~has])
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32", "8bit", "8bit_fp32"])
+@pytest.mark.parametrize("T,M,H,E", [(3, 264, 520, 4), (40, 136, 264, 3)])
+def test_few_tokens_infinity(moe, T, M, H, E, kind):
+    """An infinite activation (an infinite bias under ReLU): infinities of the signs of its weights, NaN where a weight is zero."""
+    dt = torch.float32 if "fp32" in kind else torch.bfloat16
+    g = torch.Generator(device="cuda").manual_seed(T + H)
+    x, Wg = drawn(g, T, M).to(dt), drawn(g, M, E, std=1 / math.sqrt(M)).to(dt)
+    W1, W2 = drawn(g, E, M, H, std=1 / math.sqrt(M)).to(dt), drawn(g, E, H, M, std=1 / math.sqrt(H)).to(dt)
+    W2[:, 5, 7] = 0
+    row = W2[:, 5].float()
+    if kind.startswith("8bit"):
+        W1, W2 = (moe.quantize8(w, blocks=True, rows=False, transposed=True)[1] for w in (W1, W2))
+        row = moe.dequantize8(W2, torch.float32)[:, :, 5]
+    b1 = torch.zeros((E, H), dtype=dt, device="cuda")
+    b1[:, 5] = float("inf")
+    layer = moe.FewTokenLayer(Wg, None, W1, b1, W2, None, T, 1, float(E), 0, moe.ACT_RELU, keep_routing=True)
+    got = layer.forward(x).float()
+    want = row[layer.routing["idx"][:, 0].long()] * float("inf")
+    assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.isnan(got[:, 7]).all()
+    assert torch.equal(got.nan_to_num(0.0, 1.0, -1.0), want.nan_to_num(0.0, 1.0, -1.0))
