@@ -251,7 +251,7 @@ inline int64_t backward_slots(int64_t pieces, int64_t T) {
       else CALL(ET, 256, 4);                                           \
     } else {                                                           \
       if (vpl <= 2) CALL(ET, 1024, 2);                                 \
-      else CALL(ET, 1024, 4);                                          \
+      else CALL(ET, 1024, sizeof(ET) == 4 ? 4 : 2); /* rows of bf16: at most 2048 pieces */ \
     }                                                                  \
   } while (0)
 
