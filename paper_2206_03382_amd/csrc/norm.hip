@@ -168,7 +168,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_norm_backward_k
         dots += part[turn][1][i];
       }
     }
-    const float r = rsqrtf(squares / (float)M + eps), c = r * r * (dots / (float)M);
+    const float r = rsqrtf(squares / (float)M + eps), c = r * (r * (dots / (float)M));       // r * r may be no fp32 number
 #pragma unroll
     for (int i = 0; i < VPL; ++i) {
       const int p = lane + i * LANES;

@@ -65,3 +65,22 @@ def test_norm_layer_without_a_residual(moe, T):
         layer.forward(rnd(T, M), rnd(T, M))
         got, h = layer.forward(x, None)
         assert h is x and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_smallest_eps(moe, dtype):
+    """eps down to fp32's subnormals, where r^2 alone is no fp32 number: rows of zeros and of values near sqrt(eps)."""
+    rng = np.random.default_rng(2)
+    for eps in (1e-37, 1e-40):
+        h, h64 = drawn(rng, (6, 264), dtype, 1e-19)
+        h[:3] = 0
+        h64[:3] = 0
+        dy, dy64 = drawn(rng, (6, 264), dtype, 1e-3)
+        got = moe.rms_norm_backward(dy, h, None, eps)
+        eps64 = float(np.float32(eps))
+        dx64, dw64 = B.rms_norm_backward(dy64, None, h64, None, eps64)
+        r = 1.0 / np.sqrt(np.mean(h64 * h64, axis=1, keepdims=True) + eps64)
+        parts = r * np.abs(dy64) + np.abs(h64) * r ** 3 * np.sum(np.abs(dy64 * h64), axis=1, keepdims=True) / 264
+        assert_within(got["dx"], dx64, (2.0 ** -7 + UNIT[dtype]) * parts)          # squares of 1e-19 have few bits in fp32
+        y = moe.rms_norm(h, None, eps)["y"]
+        assert_within(y, h64 * r, 2.0 ** -8 * np.abs(h64 * r) + UNIT[dtype] * np.abs(h64 * r))
