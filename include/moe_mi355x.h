@@ -368,7 +368,9 @@ int64_t moe_row_scales8(int64_t K);
 int moe_quantize8(const void* src, int dtype, const int32_t* counts, int64_t E, int64_t R, int64_t K, int scale_mode, void* q, uint8_t* scales,
                   void* qt, uint8_t* scales_t, void* stream);
 
-/* Back: out [E,R,K] in `dtype`.  bf16 holds every value of the format. */
+/* Back: out [E,R,K] in `dtype`, rounded to nearest even where the format reaches further: fp32 and bf16 end below 2^128, which is what is stored for the values next to a largest magnitude
+ * of 248 * 2^120 or more (infinity comes back), and bf16's spacing is 2^-133 at least (blocks of the two smallest exponents, 2^-125 and 2^-126, have half and a quarter of it).  All other
+ * values are exact in both. */
 int moe_dequantize8(const void* q, const uint8_t* scales, int scale_mode, int64_t E, int64_t R, int64_t K, int dtype, void* out, void* stream);
 
 /* Products of 8-bit matrices on the matrix cores, which apply the blocks' exponents themselves, with fp32 sums:

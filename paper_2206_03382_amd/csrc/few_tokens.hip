@@ -26,7 +26,7 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 //   bf16 [K, N]   step of 32 k: rows k = 8 g .. + 7, columns C i .. + C - 1 in eight loads (C = 4: 128 bytes of a row to 16 lanes); column c of all lanes is a fragment, put together
 //                 from halves of two loads at a time;
 //   fp32 [K, N]   step of 16 k: rows 4 g .. + 3, columns C i .. in four loads; a component of a load is a fragment as it is;
-//   8 bit [N, K]  step of 64 k: of columns 16 c + i, the k from 16 g, widened to bf16 with the block's exponent.  fp32 tokens enter as three bf16 pieces, which hold their 24 bits.
+//   8 bit [N, K]  step of 64 k: of columns 16 c + i, the k from 16 g, widened to bf16 with the block's exponent (exact but at the format's ends, moe_dequantize8).  fp32 tokens enter as three bf16 pieces, which hold their 24 bits.
 // The result's lane (16 g + i) has row i and 4 values v of fragment c: column 4 C g + C v + c, or 16 c + 4 g + v where fragments are 16 columns next to each other (kApart).
 // at(): where a lane's first piece of step 0 is; columns past N repeat the last ones, rows that do not exist the first one (neither is stored).  load() and
 // load_rows() take the k that exist: all of them but in the last step (TAIL), where the others are zero.

@@ -6,7 +6,8 @@
 //
 // These instructions align a step's 128 products to the largest before they add them up and lose what is 2^-16 or so of it: 1.5e-5 of the result
 // (relative, 2-norm) whatever K is, which a result rounded to bf16 (1.7e-3) or to 8 bits does not show.  fp32 results go through v_mfma_f32_16x16x32_bf16 on
-// the values widened to bf16, which holds them all, exponent included: 1e-7, at less than half the rate.
+// the values widened to bf16, exponent included: 1e-7, at less than half the rate.  bf16 holds all of a block's values if its exponent is -124 to 119; values of blocks
+// below that are rounded to multiples of 2^-133, and stored ones of 2^128 are infinities.
 #include "block8.h"
 #include "ffn_device.h"
 #include "matmul8_rules.h"
@@ -16,7 +17,7 @@ namespace {
 
 typedef __attribute__((ext_vector_type(8))) int i32x8;
 
-// four bytes times 2^(exponent byte - 127), in bf16 without a rounding
+// four bytes times 2^(exponent byte - 127), in bf16: without a rounding for exponents of -124 to 119
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 __device__ __forceinline__ bf16x8 widen8(int lo, int hi, float scale) {
   const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);

@@ -144,7 +144,7 @@ __global__ __launch_bounds__(256, 4) void quantize8_kernel(const ET* __restrict_
   }
 }
 
-// 16 values a lane; bf16 holds every value of the format.
+// 16 values a lane; exact in fp32 and bf16 but at the ends of the format (moe_dequantize8).
 template <typename ET>
 __global__ __launch_bounds__(256) void dequantize8_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ scales, int blocks, int64_t R,
                                                           int64_t K, int64_t total, int64_t per_row, int64_t row8, int64_t row_sc, ET* __restrict__ out) {
