@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+import test_norm_gpu as checks
 from oracle import block8_oracle as B
 
 pytestmark = pytest.mark.gpu
@@ -84,3 +85,9 @@ def test_smallest_eps(moe, dtype):
         assert_within(got["dx"], dx64, (2.0 ** -7 + UNIT[dtype]) * parts)          # squares of 1e-19 have few bits in fp32
         y = moe.rms_norm(h, None, eps)["y"]
         assert_within(y, h64 * r, 2.0 ** -8 * np.abs(h64 * r) + UNIT[dtype] * np.abs(h64 * r))
+
+
+@pytest.mark.parametrize("T,M,dtype", [(600, 8200, torch.bfloat16), (600, 6144, torch.float32), (700, 16384, torch.float32), (521, 16384, torch.bfloat16)])
+def test_backward_of_wide_rows(moe, T, M, dtype):
+    """1024 lanes to a row, several rows to a slot."""
+    checks.test_rms_norm_backward(moe, T, M, dtype)
