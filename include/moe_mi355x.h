@@ -418,7 +418,7 @@ int moe_layer_forward8(const void* x, const void* x8, const uint8_t* x_scales, c
                        int32_t* counts, float* logits, void* ws, size_t ws_bytes, void* stream);
 
 /* moe_layer_forward for at most MOE_FEW_MAX_TOKENS tokens (decode steps of a serving batch), where reading the chosen experts' weights is all the time
- * there is.  Logits are summed in fp64 and rounded once, ties go to the lower expert, and out sums a token's choices in fp32 without a rounding in between.
+ * there is.  (With bf16 weights moe_layer_forward is the faster one from about 30 experts with tokens on.)  Logits are summed in fp64 and rounded once, ties go to the lower expert, and out sums a token's choices in fp32 without a rounding in between.
  *   s1 = s2 = NULL: W1 [E,M,H], W2 [E,H,M] in `dtype`.  Else 8-bit weights as moe_expert_ffn8 takes them, the tokens and activations staying in `dtype`.
  *   ws: moe_layer_few_workspace_bytes, 256-byte aligned.  Everything else as moe_layer_forward. */
 #define MOE_FEW_MAX_TOKENS 64

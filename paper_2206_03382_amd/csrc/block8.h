@@ -51,7 +51,7 @@ __device__ __forceinline__ float relu_or_nan(float v) { return v <= 0.f ? 0.f : 
 __device__ __forceinline__ float act_full(float v, int act) { return act == MOE_ACT_RELU ? relu_or_nan(v) : apply_act(v, act); }
 
 // The activations of results in 8 bits.  gelu(v) = v Phi(v) with Phi(-y) = 2^-P(y) / 2, P of degree 7 fitted to -log2 erfc(y / sqrt 2) on [0, 8] for the least largest error, 4.5e-5: 3e-5 of
-// Phi there, where half a step of the format is 6e-2 (and below 1e-14 beyond).  One exponential, no division; the erf form costs as much as a K-step of the products.
+// Phi there, where half a step of the format is 6e-2 (and below 1e-14 beyond).  One exponential, no division; the erf form costs as much as a K-step of the products.  SiLU's exponential and reciprocal are the hardware's, good to 2^-21 or so.
 constexpr float kPhi8C1 = 1.15079675f, kPhi8C2 = 4.59715568e-01f, kPhi8C3 = 5.27749787e-02f, kPhi8C4 = -7.98642309e-03f, kPhi8C5 = 8.14003300e-04f,
                 kPhi8C6 = -4.87606510e-05f, kPhi8C7 = 1.28089860e-06f;
 template <int ACT> __device__ __forceinline__ float act8(float v) {

@@ -10,8 +10,9 @@ static inline int64_t few_units_of(int64_t T, int64_t E, int k) { return E < T *
 
 // Columns of a block.  Blocks of 64 where there are enough of them for three quarters of their places (two to a CU with one tile of rows, one with four), else of 32: more blocks, and more
 // places taken, for more reads of the rows.  Rows of 32 columns of bf16 weights are half a line of 128 bytes: always 64.
-// A layer of 8-bit weights, us with 64 and with 32 columns (blocks of a product with 64): 1 token x 2 experts of 4096 x 4096 (128) 42.4, 37.3;
-// 16 x 8 of 2048 x 2048 (256) 37.2, 35.1; 16 x 32 of 1024 x 1024 (512) 49.1, 64.0; 64 x 16 of 4096 x 1024 (256 and 1024) 152.8, 171.7; 24 x 4 of 768 x 512 (32 and 48) 23.1, 21.3.
+// A layer of 8-bit weights, us with 64 and with 32 columns (blocks of a product with 64): 1 token x 2 experts of 4096 x 4096 (128) 36.2, 33.3; top-2 of 16 x 8 of 2048 x 2048 (256)
+// 35.3, 31.9, of 16 x 32 of 1024 x 1024 (512) 37.5, 36.2, of 64 x 16 of 4096 x 1024 (256 and 1024) 70.8, 78.4, of 24 x 4 of 768 x 512 (32 and 48) 22.5, 19.6; top-8 of 16 x 32 of 1024 x 1024
+// 41.7, 41.0, of 64 x 16 of 4096 x 1024 101.8, 116.1.
 static inline int few_columns(int64_t T, int64_t units, int64_t width, bool bf16_weights) {
   return bf16_weights || (width + 63) / 64 * units >= (T <= 16 ? 384 : 192) ? 64 : 32;
 }

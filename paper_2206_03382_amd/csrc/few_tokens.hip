@@ -4,7 +4,7 @@
 // Reading the chosen experts' weights once is all the time there is (HBM bound), so each product is cut into units of one expert and 64 or 32 columns, a block
 // each: eight waves share the sum over k, every one with loads of several steps in flight, and meet in LDS; where that makes few blocks, several share a unit's sum.  The expert's
 // rows, 16 to a tile, go through the matrix cores together, whose 16 rows cost the same whether they are filled or not.
-// Measured: 64 tokens, 64 experts of 1024 x 4096 in bf16 104 and 99 us a product = 5.2 TB/s; 16 tokens, 8 experts of 2048 x 2048 17.8 each for 13 of HBM; 1 token, 8 of 128 experts of
+// Measured: 64 tokens, top-2 of 64 experts of 1024 x 4096 in bf16 104 and 99 us a product, 0.51 and 0.49 GB read = 4.9 TB/s (0.47 are the weights of experts that have a token); 16 tokens, 8 experts of 2048 x 2048 17.8 each for 13 of HBM; 1 token, 8 of 128 experts of
 // 4096 x 1024 in 8 bits 17 and 15 for 6.5; a layer of 5 tokens, 4 experts of 256 x 512 in fp32 12.6.
 #include <type_traits>
 
@@ -681,6 +681,8 @@ __global__ __launch_bounds__(64 * kFewWaves, TILES == 1 && STAGE != kFewUpAlone 
   const ET* bias = (const ET*)(UP ? p.b1 : p.b2);
   const int64_t pairs = p.T * p.k;
   if (n_rows > 0) {
+    // Activations are stored as the second product's matrix instructions take them: bf16 is a rounding of 2^-8 of each at most, which with the output's own makes 2.3e-3 of the result
+    // where that alone is 1.7e-3; their other form, three bf16 pieces, is three times the instructions.  Partial sums stay fp32.
     auto done = [&](int r, int64_t n, float s) {
       if (bias && part == 0) s += load_as_f32(bias + (int64_t)e * N + n);
       const int64_t q = pair_of[r];
@@ -703,7 +705,8 @@ __global__ __launch_bounds__(64 * kFewWaves, TILES == 1 && STAGE != kFewUpAlone 
   }
   // The last block of these columns to arrive (first product: with this unit) adds up what there is for them, in the order of choices and parts: the same sums whoever it is, and nobody waits.  The partial sums are stored and loaded
   // past what each XCD caches for itself (agent scope), so that a wave which has waited for its stores has them where every XCD sees them, and the last block, whose loads go out after
-  // its count has come back, finds them there.  Counting needs no release then, which would write back all of an L2, and reading no acquire, which would drop it: 64 tokens x 64 experts of
+  // its count has come back, finds them there.  All accesses are atomic, but their order is none that the language's memory model promises: it is what gfx950 does, whose stores at agent scope are counted as done when they have
+  // reached what all XCDs share, and this file is built for nothing else.  Counting needs no release then, which would write back all of an L2, and reading no acquire, which would drop it: 64 tokens x 64 experts of
   // 1024 x 4096 took 259 us with a release by one wave of each block instead of 227; 1 x 2 of 8, 4096 x 4096 in 8 bits 41.6 with an acquire instead of 35.3.
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();

@@ -7,7 +7,8 @@
 // These instructions align a step's 128 products to the largest before they add them up and lose what is 2^-16 or so of it: 1.5e-5 of the result
 // (relative, 2-norm) whatever K is, which a result rounded to bf16 (1.7e-3) or to 8 bits does not show.  fp32 results go through v_mfma_f32_16x16x32_bf16 on
 // the values widened to bf16, exponent included: 1e-7, at less than half the rate.  bf16 holds all of a block's values if its exponent is -124 to 119; values of blocks
-// below that are rounded to multiples of 2^-133, and stored ones of 2^128 are infinities.
+// below that are rounded to multiples of 2^-133, and stored ones of 2^128 are infinities.  fp32 results are bound by those conversions, which each product of a fragment makes again: 8 experts x
+// 4096 rows, 2048 x 2048 960 us = 0.29 PFLOP/s, where bf16 results take 122.
 #include "block8.h"
 #include "ffn_device.h"
 #include "matmul8_rules.h"

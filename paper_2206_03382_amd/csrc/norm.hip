@@ -2,7 +2,7 @@
 //   h = x + residual;  y = h * r * w,  r = 1 / sqrt(mean(h^2) + eps);  the row's statistics and y from the fp32 sum, before h is rounded.
 //   backward, g = dy * w:  dx = r * (g - h * r^2 * mean(g * h)) + dh;  dw = sum over the rows of dy * h * r.
 // One pass: a row stays in the registers of 64, 256 or 1024 lanes between the reduction and its use.  HBM bound: every input is read once with
-// 16-byte loads and every output written once.  131072 x 4096 in bf16 with a residual, h and y: 737 us = 5.8 TB/s (a copy 5.2); 32768 x 4096 backward with the residual's gradient
+// 16-byte loads and every output written once.  131072 x 4096 in bf16 with a residual, h and y: 774 us = 5.6 TB/s (a copy 5.2); 32768 x 4096 backward with the residual's gradient
 // 203 us = 5.3 TB/s; 16 x 4096 with the 8-bit output as well 4 us, a launch and a row's latency.
 #include "block8.h"
 
