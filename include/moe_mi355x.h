@@ -376,6 +376,7 @@ int moe_dequantize8(const void* q, const uint8_t* scales, int scale_mode, int64_
 /* Products of 8-bit matrices on the matrix cores, which apply the blocks' exponents themselves, with fp32 sums:
  *   out[e][r, n] = act(sum_k A[e][r, k] * B[e][n, k] + bias[e][n])        (both operands have the summed axis contiguous)
  *   A [E,C,K] with MOE_SCALE_ROWS; B [E,N,K] with B_scale_mode; bias [E,N] in `dtype` or NULL; act: MOE_ACT_*, or MOE_ACT_NONE.
+ *   ReLU keeps a NaN here, in moe_expert_ffn8 and in moe_layer_forward_few; that of the entries above is max(v, 0), 0 for a NaN.
  *   Exactly one of out [E,C,N] in `dtype`, rounded once, and out8 / out8_scales (the 8-bit format with MOE_SCALE_ROWS, rounded once) is given.
  *   counts [E] int32 or NULL: only the first min(counts[e], C) rows of each expert are computed, the others are left untouched.
  *   k_counts [E] int32 or NULL: only the blocks of 128 that hold the first min(k_counts[e], K) k are summed; what they hold past those k has to be zero.
