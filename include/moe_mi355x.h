@@ -34,7 +34,7 @@ extern "C" {
 enum { MOE_OK = 0, MOE_INVALID_ARG = 1, MOE_UNSUPPORTED = 2, MOE_WORKSPACE_TOO_SMALL = 3, MOE_HIP_ERROR = 4,
        MOE_SCRATCH_TOO_SMALL = 5 };
 enum { MOE_F32 = 0, MOE_BF16 = 1 };
-enum { MOE_ACT_NONE = -1, MOE_ACT_RELU = 0, MOE_ACT_GELU = 1, MOE_ACT_SILU = 2 };   /* NONE: moe_matmul8 only */
+enum { MOE_ACT_NONE = -1, MOE_ACT_RELU = 0, MOE_ACT_GELU = 1, MOE_ACT_SILU = 2 };   /* NONE: moe_matmul8, moe_ragged_matmul, moe_linear */
 enum { MOE_ROUTER_LINEAR = 0, MOE_ROUTER_COSINE = 1 };
 enum { MOE_SCALE_ROWS = 0, MOE_SCALE_BLOCKS = 1 };
 
@@ -428,6 +428,62 @@ int moe_layer_forward_few(const void* x, const void* Wg, const float* gate_bias,
                           const uint8_t* s2, const void* b2, int64_t T, int64_t M, int64_t H, int64_t E, int k, double f, int normalize, int act,
                           int dtype, void* out, int32_t* idx, int32_t* loc, float* gate_w, int32_t* counts, float* logits, void* ws,
                           size_t ws_bytes, void* stream);
+
+/* Experts' rows one behind the other, without slabs or a capacity: a layer that drops nothing holds T * k rows whatever its routing is.
+ * Expert e's rows are offsets[e] up to offsets[e+1] (offsets [E+1] int32 on the device, ascending from 0) of a matrix of R rows; R is what the caller has memory for, and rows
+ * behind the last expert's are neither read nor written.  E <= 512, R < 2^30, widths multiples of 8 and at most 2^20.
+ *
+ * The rows of a router's choices, from moe_gate_topk's (or moe_gate_route's) idx, loc and counts:
+ *   expert e has min(counts[e], C) rows, or counts[e] if C is 0, in the order of loc;  offsets [E+1]: where they start;  row_of [T,k]: the row of a choice, -1 if it has none (loc
+ *   beyond the expert's rows, idx not an expert);  row_src [T*k]: the token of a row, -1 behind the last expert's.
+ * Rows that counts announces and no choice has hold unspecified tokens; products read row 0 for tokens out of range. */
+int moe_ragged_rows(const int32_t* idx, const int32_t* loc, const int32_t* counts, int64_t T, int64_t E, int k, int64_t C, int32_t* offsets, int32_t* row_src,
+                    int32_t* row_of, void* stream);
+
+/* A projection of the experts on such rows:  out[r] = act(A[r] W[e] + bias[e])  for the rows r of expert e.
+ *   A [R,K], or with gather [R] int32 row r is A[gather[r]] of [A_rows,K] (row_src: the tokens themselves); W [E,K,N]; bias [E,N] or NULL; out [R,N], all in `dtype`.
+ *   pre [R,N] or NULL: the values before the activation as well, rounded once (what the backward takes).
+ * act: MOE_ACT_*, or MOE_ACT_NONE; ReLU keeps a NaN.  fp32 sums, activation and one rounding; K * N < 2^31. */
+int moe_ragged_matmul(const void* A, const int32_t* gather, int64_t A_rows, const void* W, const void* bias, int act, int dtype, const int32_t* offsets, int64_t R,
+                      int64_t E, int64_t K, int64_t N, void* pre, void* out, void* stream);
+
+/* Its gradients from dy = dLoss/dout [R,N], with dp = dy * act'(pre) (dy itself for MOE_ACT_NONE, pre then NULL):
+ *   dx[r] = dp[r] W[e]^T, by row (a token's are summed by moe_ragged_combine without weights);  dW[e] = sum over its rows of A[r]^T dp[r];  db[e] = sum of dp[r].
+ *   x_act, x_pre [R,K] (MOE_ACT_NONE, NULL: none): dx is also multiplied by x_act'(x_pre), so that it is the gradient of the projection before, whose
+ *   activations x were, ahead of its activation.
+ *   dx [R,K], dW [E,K,N], db [E,N]; any of them may be NULL, but not all.  Experts without rows get zeros in dW and db.  dp is rounded to `dtype`, fp32 sums in an order that the sizes and
+ *   offsets fix, one rounding.  ReLU'(0) = 0.  ws: moe_ragged_matmul_backward_workspace_bytes (0: unsupported), 256-byte aligned. */
+size_t moe_ragged_matmul_backward_workspace_bytes(int64_t R, int64_t E, int64_t K, int64_t N, int act, int dtype);
+int moe_ragged_matmul_backward(const void* dy, const void* x, const int32_t* gather, int64_t x_rows, const void* W, const void* pre, int act, const void* x_pre, int x_act,
+                               int dtype, const int32_t* offsets, int64_t R, int64_t E, int64_t K, int64_t N, void* ws, size_t ws_bytes, void* dx, void* dW, void* db,
+                               void* stream);
+
+/* A dense projection (an expert that all tokens share, the projection that closes a block):  out = act(x W + bias) + residual.
+ *   x [T,K], W [K,N], bias [N] or NULL, residual [T,N] or NULL (it may be out), out and pre [T,N]; everything else as moe_ragged_matmul.  From one token on.
+ * The gradients as moe_ragged_matmul_backward's; that of the residual is dy. */
+int moe_linear(const void* x, const void* W, const void* bias, int act, const void* residual, int dtype, int64_t T, int64_t K, int64_t N, void* pre, void* out,
+               void* stream);
+size_t moe_linear_backward_workspace_bytes(int64_t T, int64_t K, int64_t N, int act, int dtype);
+int moe_linear_backward(const void* dy, const void* x, const void* W, const void* pre, int act, int dtype, int64_t T, int64_t K, int64_t N, void* ws, size_t ws_bytes,
+                        void* dx, void* dW, void* db, void* stream);
+
+/* Dropout from a counter-based generator, whose mask is never stored:  out = residual + keep * x / (1 - p), elementwise; dropped elements add 0 whatever x is.
+ *   x, residual (or NULL), out: n elements in `dtype`, n a multiple of 8; out may be x or residual.
+ *   seed [2] on the device, 8-byte aligned: the generator's seed and an offset (another one for every call that is to have a mask of its own).  With dy for x and no residual the
+ *   same call is the gradient of x; that of the residual is dy.
+ * Philox4x32-10 with the key seed[0] and, for the group i / 8 of element i, the counter (low and high word of i / 8, of seed[1]); element i has 16 bits of the result, the half i % 2
+ * (low one first) of word i % 8 / 2, and is dropped if they are below p * 2^16 rounded to a whole number; p in that rounding also gives 1 / (1 - p).  0 <= p <= 1. */
+int moe_dropout(const void* x, const void* residual, double p, const uint64_t* seed, int dtype, int64_t n, void* out, void* stream);
+
+/* The combine of such rows:  out[t] = residual[t] + dropout(sum over the choices j, ascending, of gate_w[t,j] * Y[row_of[t,j]])  in fp32, rounded once.
+ *   Y [R,M], residual [T,M] or NULL (it may be out), out [T,M] in `dtype`; row_of [T,k] (choices whose row is not one of R are left out); gate_w [T,k] fp32, or NULL: ones.
+ *   p, seed as moe_dropout for an [T,M] matrix; p = 0: nothing is dropped, seed may be NULL.
+ * Backward, with d = dropout(d_out):  dY[row_of[t,j]] = gate_w[t,j] * d[t];  dgate_w[t,j] = <d[t], Y[row_of[t,j]]>, 0 for a choice without a row.  Rows that no choice has
+ * are left untouched. */
+int moe_ragged_combine(const void* Y, int64_t R, const int32_t* row_of, const float* gate_w, const void* residual, double p, const uint64_t* seed, int dtype, int64_t T,
+                       int64_t M, int k, void* out, void* stream);
+int moe_ragged_combine_backward(const void* d_out, const void* Y, int64_t R, const int32_t* row_of, const float* gate_w, double p, const uint64_t* seed, int dtype,
+                                int64_t T, int64_t M, int k, void* dY, float* dgate_w, void* stream);
 
 /* Thin wrappers over HIP events so that a caller without HIP headers can time on the library's stream.
  * moe_event_create stores a new hipEvent_t in *event; moe_event_elapsed_ms needs both events completed. */

@@ -52,9 +52,24 @@ __device__ __forceinline__ int wave_inclusive_scan(int v) {
 
 }  // namespace
 
+// Where an expert's rows are.  Without ROWS, in a slab of C rows, of which counts[e] exist, or all if there are no counts.  With it, one expert's
+// behind the other's in one matrix of C rows: `counts` are the offsets [E + 1], expert e's rows are offsets[e] up to offsets[e + 1], and
+// without offsets there is one expert, which has all of them.  Offsets beyond the matrix, or descending ones, end at its rows.
+template <bool ROWS = false>
+__device__ __forceinline__ int64_t first_row_of(int e, int64_t C, const int32_t* __restrict__ counts) {
+  if (!ROWS) return (int64_t)e * C;
+  if (!counts) return 0;
+  const int64_t c = counts[e];
+  return c < C ? (c > 0 ? c : 0) : C;
+}
 // Rows of expert e that exist: its fill, at most C.
+template <bool ROWS = false>
 __device__ __forceinline__ int live_rows_of(int e, int64_t C, const int32_t* __restrict__ counts) {
   if (!counts) return (int)C;
+  if (ROWS) {
+    const int64_t lo = first_row_of<true>(e, C, counts), c = counts[e + 1], hi = c < C ? c : C;
+    return hi > lo ? (int)(hi - lo) : 0;
+  }
   const int64_t c = counts[e];
   return (int)(c < C ? (c > 0 ? c : 0) : C);
 }
@@ -63,13 +78,13 @@ __device__ __forceinline__ int live_rows_of(int e, int64_t C, const int32_t* __r
 // An expert's live tiles are its row tiles below the fill x all column tiles; how they are numbered and dealt to the XCDs: ffn_rules.h.  Every wave
 // finds its tile by prefix sums over the experts, 64 to a step; no host has to know the fills.
 // SHIFT: log2 of the blocks that share a unit, where groups are to hold as many more tiles.  SHORTS: short row tiles may come last.
-template <int TILE_ROWS, int SHIFT, bool SHORTS, bool CUTS, int CHUNKS>
+template <int TILE_ROWS, int SHIFT, bool SHORTS, bool CUTS, int CHUNKS, bool ROWS>
 __device__ __forceinline__ bool search_tile(int b, int lane, int E, int64_t C, const int32_t* __restrict__ counts, int NT,
                                             int& e_out, int& mt_out, int& nt_out, int& rows_out, TileHalf& half) {
   int rowsv[CHUNKS], upto[CHUNKS], groups[CHUNKS];                  // lane l of chunk c: rows of expert 64 c + l; tall tiles, full groups of them up to it
   unsigned long long shortv[CHUNKS];                                // experts with a short row tile
 #pragma unroll
-  for (int c = 0; c < CHUNKS; ++c) rowsv[c] = c * 64 + lane < E ? live_rows_of(c * 64 + lane, C, counts) : 0;      // all loads in flight at once
+  for (int c = 0; c < CHUNKS; ++c) rowsv[c] = c * 64 + lane < E ? live_rows_of<ROWS>(c * 64 + lane, C, counts) : 0;      // all loads in flight at once
   int tall = 0, shorts = 0;
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c) {                                // as if all row tiles were tall
@@ -161,7 +176,7 @@ __device__ __forceinline__ bool search_tile(int b, int lane, int E, int64_t C, c
 // EQUAL: every expert has all of its C rows (weight gradients), see equal_tile.  Up to 64 experts, and up to 128, have code of their own, nearly one
 // straight piece: what a launch of few tiles pays for is fetching it (decode step of 16 tokens 47.8 -> 46.9 us; second product of 128 experts x 8192 rows, 264
 // tiles to a unit, 8150 -> 8080).
-template <int TILE_ROWS, bool EQUAL = false, int SHIFT = 0, bool SHORTS = false, bool CUTS = false>
+template <int TILE_ROWS, bool EQUAL = false, int SHIFT = 0, bool SHORTS = false, bool CUTS = false, bool ROWS = false>
 __device__ __forceinline__ bool find_tile(int b, int lane, int E, int64_t C, const int32_t* __restrict__ counts, int NT,
                                           int& e_out, int& mt_out, int& nt_out, int& rows_out, TileHalf& half) {
   if (EQUAL) {
@@ -174,23 +189,23 @@ __device__ __forceinline__ bool find_tile(int b, int lane, int E, int64_t C, con
     half = {-1, -1};
     return true;
   }
-  if (E <= 64) return search_tile<TILE_ROWS, SHIFT, SHORTS, CUTS, 1>(b, lane, E, C, counts, NT, e_out, mt_out, nt_out, rows_out, half);
-  if (E <= 128) return search_tile<TILE_ROWS, SHIFT, SHORTS, CUTS, 2>(b, lane, E, C, counts, NT, e_out, mt_out, nt_out, rows_out, half);
-  return search_tile<TILE_ROWS, SHIFT, SHORTS, CUTS, kMaxExperts / 64>(b, lane, E, C, counts, NT, e_out, mt_out, nt_out, rows_out, half);
+  if (E <= 64) return search_tile<TILE_ROWS, SHIFT, SHORTS, CUTS, 1, ROWS>(b, lane, E, C, counts, NT, e_out, mt_out, nt_out, rows_out, half);
+  if (E <= 128) return search_tile<TILE_ROWS, SHIFT, SHORTS, CUTS, 2, ROWS>(b, lane, E, C, counts, NT, e_out, mt_out, nt_out, rows_out, half);
+  return search_tile<TILE_ROWS, SHIFT, SHORTS, CUTS, kMaxExperts / 64, ROWS>(b, lane, E, C, counts, NT, e_out, mt_out, nt_out, rows_out, half);
 }
 
-template <int TILE_ROWS, bool EQUAL = false, int SHIFT = 0, bool SHORTS = false>
+template <int TILE_ROWS, bool EQUAL = false, int SHIFT = 0, bool SHORTS = false, bool ROWS = false>
 __device__ __forceinline__ bool find_tile(int b, int lane, int E, int64_t C, const int32_t* __restrict__ counts, int NT,
                                           int& e_out, int& mt_out, int& nt_out, int& rows_out) {
   TileHalf half;
-  return find_tile<TILE_ROWS, EQUAL, SHIFT, SHORTS>(b, lane, E, C, counts, NT, e_out, mt_out, nt_out, rows_out, half);
+  return find_tile<TILE_ROWS, EQUAL, SHIFT, SHORTS, false, ROWS>(b, lane, E, C, counts, NT, e_out, mt_out, nt_out, rows_out, half);
 }
 
 struct TileArgs {
   const void* A;
   const void* B;
   const void* bias;
-  const int32_t* counts;
+  const int32_t* counts;        // ROWS: the offsets, as in kfill
   const int32_t* gather;        // slot -> row [E, slots]: A is one matrix of gather_rows rows, [., K] (kNN) or [., C] (kTN, GK)
   int64_t gather_rows;
   int64_t C;                    // rows of A (kNN, kNT) or its width (kTN)
@@ -199,7 +214,7 @@ struct TileArgs {
   int plain;                    // block y, x = expert, tile of it; else the numbering of find_tile in x
   void* out;
   const int32_t* kfill;         // kTN: live slots per expert
-  const void* pre;              // kNT: multiply by act'(pre) (act >= 0) or add pre (act < 0)
+  const void* pre;              // kNT: multiply by act'(pre) (act >= 0) or add pre (act < 0); ROWS, kNN: add pre
   void* pre_out;                // kNN: the values before the activation go here as well
   int act;                      // MOE_ACT_*, + kFullAct (bf16 results) for the form with erf and true divisions; < 0: none
   int64_t ktotal;               // PART: length of the whole reduction, of which every "expert" is K consecutive k

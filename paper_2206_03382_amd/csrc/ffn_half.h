@@ -1,5 +1,5 @@
-// The grouped GEMM of ffn_mfma.hip on half of its large tile: 128 x 256, two blocks to a compute unit, for launches where whole
-// tiles of 256 rows divide badly: experts of a few hundred rows, or few tiles per unit.  Included by ffn_mfma.hip (same helpers,
+// The grouped GEMM of ffn_large.h on half of its large tile: 128 x 256, two blocks to a compute unit, for launches where whole
+// tiles of 256 rows divide badly: experts of a few hundred rows, or few tiles per unit.  Included by ffn_large.h (same helpers,
 // forward layout, shapes and results: the sums of an output run over k in the same order).
 //
 // Four waves side by side, each 128 rows x 64 columns as 8 x 4 tiles of v_mfma_f32_16x16x32_bf16 (128 accumulator registers): two

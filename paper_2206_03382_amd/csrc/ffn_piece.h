@@ -1,4 +1,4 @@
-// A part of TM x TN of one of the large tile's last tiles (ffn_rules.h: cut_tile).  Included by ffn_mfma.hip; same shapes and results: the sums of
+// A part of TM x TN of one of the large tile's last tiles (ffn_rules.h: cut_tile).  Included by ffn_large.h; same shapes and results: the sums of
 // an output run over k in the same order.
 //
 // A whole tile has its unit for itself and hides the way from memory behind its own products.  A part has half or a quarter of those, so what it

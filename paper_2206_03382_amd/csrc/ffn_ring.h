@@ -1,5 +1,5 @@
-// The grouped GEMM of ffn_mfma.hip for bf16 products that its large tile does not cover or does not suit and that have the rows and
-// columns for tiles of TM x TN: any K and N that are multiples of 8, the layouts kNN, kNT and kTN.  Included by ffn_mfma.hip.
+// The grouped GEMM of ffn_large.h for bf16 products that its large tile does not cover or does not suit and that have the rows and
+// columns for tiles of TM x TN: any K and N that are multiples of 8, the layouts kNN, kNT and kTN.  Included by ffn_large.h.
 //
 //   out[e] = epilogue(A[e] * B[e] + bias[e])
 //
@@ -32,7 +32,9 @@ constexpr int divisor_up_to_8(int n) {
 }
 
 // GK (kTN): A's k rows (slots) are gathered.
-template <int MODE, int TM, int TN, bool GK = false>
+// ROWS: experts' rows one behind the other (first_row_of), activations and what they are joined with before the one rounding (rows_act.h): kNN act(sum) +
+// pre, kNT sum * act'(pre).
+template <int MODE, int TM, int TN, bool GK = false, bool ROWS = false>
 __global__ __launch_bounds__(256, 2 * ring_bytes(TM, TN) <= 163840 ? 2 : 1) void grouped_gemm_ring_kernel(const TileArgs p) {
   constexpr bool TRA = MODE == kTN, TRB = MODE != kNT;              // k-slow operands
   constexpr int WTM = TM / 2, WTN = TN / 2, RA = WTM / 16, RB = WTN / 16;
@@ -47,17 +49,19 @@ __global__ __launch_bounds__(256, 2 * ring_bytes(TM, TN) <= 163840 ? 2 : 1) void
   const int wm = wave >> 1, wn = wave & 1, kq = lane >> 4;
   int e, mt, nt, rows;
   if (!p.plain) {
-    if (!find_tile<TM, MODE == kTN>(blockIdx.x, lane, p.E, p.C, p.counts, p.NT, e, mt, nt, rows)) return;
+    if (!find_tile<TM, MODE == kTN, 0, false, ROWS>(blockIdx.x, lane, p.E, p.C, p.counts, p.NT, e, mt, nt, rows)) return;
   } else {
     e = blockIdx.y;
     mt = blockIdx.x / p.NT;
     nt = blockIdx.x % p.NT;
-    rows = live_rows_of(e, p.C, p.counts);
+    rows = MODE == kTN ? live_rows_of(e, p.C, p.counts) : live_rows_of<ROWS>(e, p.C, p.counts);
   }
   const int64_t m0 = (int64_t)mt * TM, n0 = (int64_t)nt * TN;
   if (m0 >= rows) return;
   int64_t kend = p.K;                                               // k that exist
-  if (MODE == kTN && p.kfill) { const int64_t c = p.kfill[e]; kend = c < p.K ? (c > 0 ? c : 0) : p.K; }
+  if (MODE == kTN && ROWS) kend = live_rows_of<ROWS>(e, p.K, p.kfill);
+  else if (MODE == kTN && p.kfill) { const int64_t c = p.kfill[e]; kend = c < p.K ? (c > 0 ? c : 0) : p.K; }
+  const int64_t first = MODE == kTN ? first_row_of<ROWS>(e, p.K, p.kfill) : first_row_of<ROWS>(e, p.C, p.counts);   // of the expert's rows
   const int KT = kend > 0 ? (int)((kend + 63) / 64) : 1;
 
   // ---- this lane's direct loads.  k-contiguous: block q * 4 + wave = 8 rows, lane l row + l / 8, position l % 8.  k-slow: pieces in order.
@@ -74,24 +78,24 @@ __global__ __launch_bounds__(256, 2 * ring_bytes(TM, TN) <= 163840 ? 2 : 1) void
 #pragma unroll
   for (int q = 0; q < LA; ++q) {
     if (TRA) {
-      a_ptr[q] = slow_source((const uint16_t*)p.A + (GK ? 0 : (int64_t)e * p.K * p.C), p.C, m0, TM, q);
+      a_ptr[q] = slow_source((const uint16_t*)p.A + (GK ? 0 : first * p.C), p.C, m0, TM, q);
       if (GK) a_ptr[q] -= (int64_t)slow_k(q, TM) * p.C * 2;         // of row 0 of the gathered matrix
     } else {
       int64_t row = m0 + (q * 4 + wave) * 8 + (lane >> 3);
       row = row < rows ? row : rows - 1;                            // rows past the fill repeat the last one
       const uint16_t* base = (const uint16_t*)p.A;
       if (p.gather) {
-        const int64_t t = p.gather[(int64_t)e * p.C + row];
+        const int64_t t = p.gather[first + row];
         row = t >= 0 && t < p.gather_rows ? t : 0;
       } else {
-        base += (int64_t)e * p.C * p.K;
+        base += first * p.K;
       }
       a_ptr[q] = (const char*)(base + row * p.K + fast_k);
     }
   }
 #pragma unroll
   for (int q = 0; q < LB; ++q) {
-    const uint16_t* base = (const uint16_t*)p.B + (int64_t)e * p.K * p.N;
+    const uint16_t* base = (const uint16_t*)p.B + (MODE == kTN ? first : (int64_t)e * p.K) * p.N;
     if (TRB) {
       b_ptr[q] = slow_source(base, p.N, n0, TN, q);
     } else {
@@ -116,8 +120,8 @@ __global__ __launch_bounds__(256, 2 * ring_bytes(TM, TN) <= 163840 ? 2 : 1) void
     if constexpr (GK) {
 #pragma unroll
       for (int q = 0; q < LA; ++q) {
-        const int64_t slot = (int64_t)t * 64 + slow_k(q, TM);
-        g[q] = p.gather[(int64_t)e * p.K + (slot < p.K ? slot : p.K - 1)];
+        const int64_t slot = (int64_t)t * 64 + slow_k(q, TM), last = ROWS ? p.K - 1 - first : p.K - 1;
+        g[q] = p.gather[first + (slot < last ? slot : last)];
       }
     }
   };
@@ -315,7 +319,7 @@ __global__ __launch_bounds__(256, 2 * ring_bytes(TM, TN) <= 163840 ? 2 : 1) void
   static_assert(WTM * CPR % 64 == 0, "whole stores");
   auto out_swz = [](int r) -> int { return r % CPR; };
   char* wtile = smem + wave * (WTM * WTN * 2);
-  const int64_t out_at = ((int64_t)e * p.C + m0 + wm * WTM) * p.N + nw;
+  const int64_t out_at = ((MODE == kTN ? (int64_t)e * p.C : first) + m0 + wm * WTM) * p.N + nw;
   auto write_tile = [&](auto act_tag, uint16_t* dst, const uint16_t* pre) __attribute__((always_inline)) {
     constexpr int ACT = decltype(act_tag)::value;
 #pragma unroll
@@ -363,6 +367,61 @@ __global__ __launch_bounds__(256, 2 * ring_bytes(TM, TN) <= 163840 ? 2 : 1) void
     }
     __builtin_amdgcn_wave_barrier();
   };
+  if constexpr (ROWS) {
+    // What the sums are joined with comes into the pieces that the results go to, by direct loads; a lane joins its own.
+    const uint32_t wtile_addr = (uint32_t)(uintptr_t)LDS_PTR(char, wtile);
+    auto write_rows = [&](auto act_tag, uint16_t* dst, const uint16_t* with) __attribute__((always_inline)) {
+      constexpr int ACT = decltype(act_tag)::value;
+      if (with) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll 1
+        for (int it = 0; it < STORES; ++it) {
+          const int n = it * 64 + lane, r = n / CPR, c = (n % CPR) ^ out_swz(r);
+          global_to_lds_16((const char*)(with + (r < live && nw + c * 8 < p.N ? out_at + (int64_t)r * p.N + c * 8 : out_at)), wtile_addr + it * 1024);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      }
+#pragma unroll
+      for (int i = 0; i < RA; ++i) {
+        if (i >= ni) break;
+        const int r = i * 16 + (lane & 15);
+#pragma unroll
+        for (int j = 0; j < RB; ++j) {
+          auto* at = LDS_PTR(u32x2, wtile + r * (CPR * 16) + (((2 * j + (kq >> 1)) ^ out_swz(r)) << 4) + 8 * (kq & 1));
+          float v[4], w[4] = {0.f, 0.f, 0.f, 0.f};
+          if (with) {
+            const u32x2 q = *at;
+            w[0] = __uint_as_float(q.x << 16); w[1] = __uint_as_float(q.x & 0xffff0000u);
+            w[2] = __uint_as_float(q.y << 16); w[3] = __uint_as_float(q.y & 0xffff0000u);
+          }
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            if (MODE == kNT) v[u] = with ? acc[i][j][u] * rows_act_grad<ACT>(w[u]) : acc[i][j][u];
+            else v[u] = rows_act<ACT>(acc[i][j][u]) + (with ? w[u] : 0.f);
+          }
+          *at = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+        }
+      }
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll 4
+      for (int it = 0; it < STORES; ++it) {
+        const int n = it * 64 + lane, r = n / CPR, c = (n % CPR) ^ out_swz(r);
+        if (r < live && nw + c * 8 < p.N)
+          *reinterpret_cast<u32x4*>(dst + out_at + (int64_t)r * p.N + c * 8) = *LDS_PTR(u32x4, wtile + n * 16);
+      }
+      __builtin_amdgcn_wave_barrier();
+    };
+    const uint16_t* with = MODE == kTN ? nullptr : (const uint16_t*)p.pre;
+    if (MODE == kNN && p.pre_out) write_rows(std::integral_constant<int, -1>{}, (uint16_t*)p.pre_out, nullptr);
+    if (MODE == kTN) write_rows(std::integral_constant<int, -1>{}, (uint16_t*)p.out, nullptr);
+    else switch (p.act) {
+      case MOE_ACT_RELU: write_rows(std::integral_constant<int, MOE_ACT_RELU>{}, (uint16_t*)p.out, with); break;
+      case MOE_ACT_GELU: write_rows(std::integral_constant<int, MOE_ACT_GELU>{}, (uint16_t*)p.out, with); break;
+      case MOE_ACT_SILU: write_rows(std::integral_constant<int, MOE_ACT_SILU>{}, (uint16_t*)p.out, with); break;
+      default: write_rows(std::integral_constant<int, -1>{}, (uint16_t*)p.out, with); break;
+    }
+    return;
+  }
   uint16_t* out = (uint16_t*)p.out;
   const uint16_t* pre = MODE == kNT ? (const uint16_t*)p.pre : nullptr;
   if (MODE == kNN && p.pre_out) write_tile(std::integral_constant<int, -1>{}, (uint16_t*)p.pre_out, nullptr);
@@ -379,11 +438,11 @@ __global__ __launch_bounds__(256, 2 * ring_bytes(TM, TN) <= 163840 ? 2 : 1) void
 
 }  // namespace
 
-template <int MODE, int TM, int TN>
+template <int MODE, int TM, int TN, bool ROWS = false>
 static hipError_t launch_ring(TileArgs p, int64_t total, hipStream_t s) {
   dim3 grid;
   if (!tile_launch(p, TM, TN, total, grid)) return hipErrorInvalidValue;
-  if (MODE == kTN && p.gather) grouped_gemm_ring_kernel<MODE, TM, TN, MODE == kTN><<<grid, dim3(256), 0, s>>>(p);
-  else grouped_gemm_ring_kernel<MODE, TM, TN><<<grid, dim3(256), 0, s>>>(p);
+  if (MODE == kTN && p.gather) grouped_gemm_ring_kernel<MODE, TM, TN, MODE == kTN, ROWS><<<grid, dim3(256), 0, s>>>(p);
+  else grouped_gemm_ring_kernel<MODE, TM, TN, false, ROWS><<<grid, dim3(256), 0, s>>>(p);
   return hipGetLastError();
 }

@@ -12,7 +12,7 @@
 
 namespace moe {
 
-constexpr int kNN = 0, kNT = 1, kTN = 2;    // operand layouts, see the head of ffn_mfma.hip
+constexpr int kNN = 0, kNT = 1, kTN = 2;    // operand layouts, see the head of ffn_large.h
 constexpr int kLargeTile = 256, kLargeK = 64;   // rows and columns of the large tile, its K-step
 constexpr int kMaxExperts = 512;            // the tile search keeps one register per 64 experts
 constexpr int64_t kMaxBlocks = (int64_t)1 << 24;   // of 256 threads, in a grid dimension: launches beyond 2^32 threads run cut short

@@ -1,5 +1,5 @@
-// The grouped GEMM of ffn_mfma.hip for what its larger tiles do not cover or do not suit: fp32 storage, and bf16 launches with few
-// tiles, with any K and N that are multiples of 8.  Included by ffn_mfma.hip (same helpers, same operand layouts).
+// The grouped GEMM of ffn_large.h for what its larger tiles do not cover or do not suit: fp32 storage, and bf16 launches with few
+// tiles, with any K and N that are multiples of 8.  Included by ffn_large.h (same helpers, same operand layouts).
 //
 //   out[e] = epilogue(A[e] * B[e] + bias[e]) in the layouts kNN, kNT and kTN, bf16 (v_mfma_f32_32x32x16_bf16) or fp32
 //   (v_mfma_f32_32x32x2_f32: full fp32 products and sums), fp32 accumulation.
@@ -42,7 +42,8 @@ template <int MOST, int L> __device__ __forceinline__ void wait_for_loads(int la
 // (no barrier until their sums meet, which the first wave adds up in order).  For fp32 launches of few tiles, whose time is one chain
 // of matrix instructions per wave on a part of the units: see fp32_split.  Two stages (64 KB, two blocks to a unit): three or four
 // leave room for one block, 4 experts x 256 rows, 256 x 512, two products: 15.4 us against 19.4 and 19.7.
-template <typename ET, int MODE, int BM, int BN, int WR, int WC, int NS, bool GK = false, bool PART = false, bool STREAM = false, int KS = 1>
+// ROWS: as in ffn_ring.h.
+template <typename ET, int MODE, int BM, int BN, int WR, int WC, int NS, bool GK = false, bool PART = false, bool STREAM = false, int KS = 1, bool ROWS = false>
 __global__ __launch_bounds__(WR * WC * KS * 64, 2) void grouped_gemm_tile_kernel(const TileArgs p) {
   constexpr int ES = (int)sizeof(ET), EC = 16 / ES;                 // elements per 16-byte piece
   constexpr int BKE = 128 / ES;                                     // k per K-step
@@ -68,18 +69,20 @@ __global__ __launch_bounds__(WR * WC * KS * 64, 2) void grouped_gemm_tile_kernel
   // ---- which tile: the search of the large kernel, or plain numbering where that does not do ---------------------
   int e, mt, nt, rows;
   if (!p.plain) {
-    if (!find_tile<BM, MODE == kTN>(blockIdx.x, lane, p.E, p.C, p.counts, p.NT, e, mt, nt, rows)) return;
+    if (!find_tile<BM, MODE == kTN, 0, false, ROWS && MODE != kTN>(blockIdx.x, lane, p.E, p.C, p.counts, p.NT, e, mt, nt, rows)) return;
   } else {
     e = blockIdx.y;
     mt = blockIdx.x / p.NT;
     nt = blockIdx.x % p.NT;
-    rows = live_rows_of(e, p.C, p.counts);
+    rows = MODE == kTN ? live_rows_of(e, p.C, p.counts) : live_rows_of<ROWS>(e, p.C, p.counts);
   }
   const int64_t m0 = (int64_t)mt * BM;
   if (m0 >= rows) return;
   const int64_t n0 = (int64_t)nt * BN;
   int64_t kend = p.K;                                               // k that exist
-  if (MODE == kTN && p.kfill) { const int64_t c = p.kfill[e]; kend = c < p.K ? (c > 0 ? c : 0) : p.K; }
+  if (MODE == kTN && ROWS) kend = live_rows_of<ROWS>(e, p.K, p.kfill);
+  else if (MODE == kTN && p.kfill) { const int64_t c = p.kfill[e]; kend = c < p.K ? (c > 0 ? c : 0) : p.K; }
+  const int64_t first = MODE == kTN ? first_row_of<ROWS>(e, p.K, p.kfill) : first_row_of<ROWS>(e, p.C, p.counts);   // of the expert's rows
   if (PART) { const int64_t left = p.ktotal - (int64_t)e * p.K; kend = left < p.K ? (left > 0 ? left : 0) : p.K; }
   const int KT_all = kend > 0 ? (int)((kend + BKE - 1) / BKE) : 1;
   const int KT = KS > 1 ? (KT_all - part + KS - 1) / KS : KT_all;   // K-steps of this wave (none where there are fewer than waves)
@@ -109,23 +112,23 @@ __global__ __launch_bounds__(WR * WC * KS * 64, 2) void grouped_gemm_tile_kernel
 #pragma unroll
   for (int i = 0; i < LA; ++i) {
     if (TRA) {
-      const char* base = (const char*)p.A + (GK ? 0 : (int64_t)e * p.K * p.C * ES);
+      const char* base = (const char*)p.A + (GK ? 0 : first * p.C * ES);
       a_ptr[i] = slow_source(base, p.C, m0, BM, i, a_k[i]);
       if (GK) a_ptr[i] -= (int64_t)a_k[i] * p.C * ES;              // row 0 of the gathered matrix
     } else {
       int64_t row = m0 + (i * NW + wave) * 8 + (lane >> 3);
       row = row < rows ? row : rows - 1;                            // rows past the fill repeat the last one
       if (p.gather) {
-        const int64_t t = p.gather[(int64_t)e * p.C + row];
+        const int64_t t = p.gather[first + row];
         a_ptr[i] = fast_source((const char*)p.A, p.K, t >= 0 && t < p.gather_rows ? t : 0, i, a_k[i]);
       } else {
-        a_ptr[i] = fast_source((const char*)p.A + (int64_t)e * p.C * p.K * ES, p.K, row, i, a_k[i]);
+        a_ptr[i] = fast_source((const char*)p.A + first * p.K * ES, p.K, row, i, a_k[i]);
       }
     }
   }
 #pragma unroll
   for (int i = 0; i < LB; ++i) {
-    const char* base = (const char*)p.B + (int64_t)e * p.K * p.N * ES;
+    const char* base = (const char*)p.B + (MODE == kTN ? first : (int64_t)e * p.K) * p.N * ES;
     if (TRB) {
       b_ptr[i] = slow_source(base, p.N, n0, BN, i, b_k[i]);
     } else {
@@ -148,8 +151,8 @@ __global__ __launch_bounds__(WR * WC * KS * 64, 2) void grouped_gemm_tile_kernel
     if constexpr (GK) {
 #pragma unroll
       for (int i = 0; i < LA; ++i) {
-        const int64_t slot = (int64_t)t * BKE + a_k[i];
-        g[i] = p.gather[(int64_t)e * p.K + (slot < p.K ? slot : p.K - 1)];
+        const int64_t slot = (int64_t)t * BKE + a_k[i], last = ROWS ? p.K - 1 - first : p.K - 1;
+        g[i] = p.gather[first + (slot < last ? slot : last)];
       }
     }
   };
@@ -365,7 +368,7 @@ __global__ __launch_bounds__(WR * WC * KS * 64, 2) void grouped_gemm_tile_kernel
   constexpr int CPR = WTN * OS / 16, RPI = 64 / CPR;                // pieces per row, rows per store
   char* wtile = smem + wave * (WTM * WTN * OS);
   const int64_t nw = n0 + wn * WTN;
-  const int64_t out_at = ((int64_t)e * p.C + m0 + wm * WTM) * p.N + nw;
+  const int64_t out_at = ((MODE == kTN ? (int64_t)e * p.C : first) + m0 + wm * WTM) * p.N + nw;
   using OT = std::conditional_t<BF16O, uint16_t, float>;
   auto write_tile = [&](auto act_tag, OT* dst, const OT* pre) __attribute__((always_inline)) {
     constexpr int ACT = decltype(act_tag)::value;
@@ -414,6 +417,75 @@ __global__ __launch_bounds__(WR * WC * KS * 64, 2) void grouped_gemm_tile_kernel
     }
     __builtin_amdgcn_wave_barrier();
   };
+  if constexpr (ROWS) {
+    // What the sums are joined with comes into the pieces that the results go to, by direct loads; a lane joins its own.
+    const uint32_t wtile_addr = (uint32_t)(uintptr_t)LDS_PTR(char, wtile);
+    auto write_rows = [&](auto act_tag, OT* dst, const OT* with) __attribute__((always_inline)) {
+      constexpr int ACT = decltype(act_tag)::value;
+      if (with && live > 0 && nw < p.N) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll 1
+        for (int it = 0; it < WTM / RPI; ++it) {
+          const int r = it * RPI + lane / CPR, ch = (lane % CPR) ^ (r % CPR);
+          global_to_lds_16((const char*)(with + (r < live && nw + ch * OC < p.N ? out_at + (int64_t)r * p.N + ch * OC : out_at)), wtile_addr + it * 1024);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      }
+      auto join = [&](float v, float w) __attribute__((always_inline)) -> float {
+        if (MODE == kNT) return with ? v * rows_act_grad_as<OT, ACT>(w) : v;
+        return rows_act_as<OT, ACT>(v) + (with ? w : 0.f);
+      };
+#pragma unroll
+      for (int i = 0; i < TI; ++i) {
+        const int r = i * 32 + (lane & 31);
+#pragma unroll
+        for (int j = 0; j < TJ; ++j)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            float v[4], w[4] = {0.f, 0.f, 0.f, 0.f};
+            if constexpr (BF16O) {
+              auto* at = LDS_PTR(u32x2, wtile + r * (CPR * 16) + (((4 * j + g) ^ (r % CPR)) << 4) + 8 * kg);
+              if (with) {
+                const u32x2 q = *at;
+                w[0] = __uint_as_float(q.x << 16); w[1] = __uint_as_float(q.x & 0xffff0000u);
+                w[2] = __uint_as_float(q.y << 16); w[3] = __uint_as_float(q.y & 0xffff0000u);
+              }
+#pragma unroll
+              for (int u = 0; u < 4; ++u) v[u] = join(acc[i][j][4 * g + u], w[u]);
+              *at = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+            } else {
+              auto* at = LDS_PTR(u32x4, wtile + r * (CPR * 16) + (((8 * j + 2 * g + kg) ^ (r % CPR)) << 4));
+              if (with) {
+                const u32x4 q = *at;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) w[u] = __uint_as_float(q[u]);
+              }
+#pragma unroll
+              for (int u = 0; u < 4; ++u) v[u] = join(acc[i][j][4 * g + u], w[u]);
+              *at = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+            }
+          }
+      }
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll 4
+      for (int it = 0; it < WTM / RPI; ++it) {
+        const int r = it * RPI + lane / CPR, ch = (lane % CPR) ^ (r % CPR);
+        const u32x4 q = *LDS_PTR(u32x4, wtile + r * (CPR * 16) + ((lane % CPR) << 4));
+        if (r < live && nw + ch * OC < p.N) *reinterpret_cast<u32x4*>(dst + out_at + (int64_t)r * p.N + ch * OC) = q;
+      }
+      __builtin_amdgcn_wave_barrier();
+    };
+    const OT* with = MODE == kTN ? nullptr : (const OT*)p.pre;
+    if (MODE == kNN && p.pre_out) write_rows(std::integral_constant<int, -1>{}, (OT*)p.pre_out, nullptr);
+    if (MODE == kTN) write_rows(std::integral_constant<int, -1>{}, (OT*)p.out, nullptr);
+    else switch (p.act) {
+      case MOE_ACT_RELU: write_rows(std::integral_constant<int, MOE_ACT_RELU>{}, (OT*)p.out, with); break;
+      case MOE_ACT_GELU: write_rows(std::integral_constant<int, MOE_ACT_GELU>{}, (OT*)p.out, with); break;
+      case MOE_ACT_SILU: write_rows(std::integral_constant<int, MOE_ACT_SILU>{}, (OT*)p.out, with); break;
+      default: write_rows(std::integral_constant<int, -1>{}, (OT*)p.out, with); break;
+    }
+    return;
+  }
   OT* out = (OT*)p.out;
   const OT* pre = MODE == kNT ? (const OT*)p.pre : nullptr;
   if (MODE == kNN && p.pre_out) write_tile(std::integral_constant<int, -1>{}, (OT*)p.pre_out, nullptr);
@@ -430,38 +502,38 @@ __global__ __launch_bounds__(WR * WC * KS * 64, 2) void grouped_gemm_tile_kernel
 
 }  // namespace
 
-template <typename ET, int MODE, int BM, int BN, int NS, bool STREAM = false, int KS = 1>
+template <typename ET, int MODE, int BM, int BN, int NS, bool STREAM = false, int KS = 1, bool ROWS = false>
 static hipError_t launch_tile(TileArgs p, int64_t total, hipStream_t s) {
   dim3 grid;
   if (!tile_launch(p, BM, BN, total, grid)) return hipErrorInvalidValue;
   if constexpr (MODE == kTN) {
     if (p.gather) {
-      grouped_gemm_tile_kernel<ET, MODE, BM, BN, 2, 2, NS, true><<<grid, dim3(256), 0, s>>>(p);
+      grouped_gemm_tile_kernel<ET, MODE, BM, BN, 2, 2, NS, true, false, false, 1, ROWS><<<grid, dim3(256), 0, s>>>(p);
       return hipGetLastError();
     }
   }
   constexpr int W = KS > 1 ? 1 : 2;
-  grouped_gemm_tile_kernel<ET, MODE, BM, BN, W, W, NS, false, false, STREAM, KS><<<grid, dim3(256), 0, s>>>(p);
+  grouped_gemm_tile_kernel<ET, MODE, BM, BN, W, W, NS, false, false, STREAM, KS, ROWS><<<grid, dim3(256), 0, s>>>(p);
   return hipGetLastError();
 }
 
 // The launches below the large tile (`total`: rows of all experts that exist, at most).  fp32: the matrix instruction is 16 times slower, loads hardly matter, and the finest
 // tile divides best (64 x 64, five blocks per unit: within 2-4 % of the best of four shapes over 442 launches), but for launches too
 // small to fill the chip with it (fp32_split).
-template <int MODE>
+template <int MODE, bool ROWS = false>
 static hipError_t launch_small(int dtype, Tile tile, const TileArgs& p, int64_t total, hipStream_t s) {
   if constexpr (MODE != kTN) {
-    if (dtype == MOE_F32 && fp32_split(p.E, p.C, p.K, p.N)) return launch_tile<float, MODE, kSplitTile, kSplitTile, 2, false, kSplitParts>(p, total, s);
+    if (dtype == MOE_F32 && fp32_split(p.E, p.C, p.K, p.N)) return launch_tile<float, MODE, kSplitTile, kSplitTile, 2, false, kSplitParts, ROWS>(p, total, s);
   }
-  if (dtype == MOE_F32) return launch_tile<float, MODE, 64, 64, 2>(p, total, s);
+  if (dtype == MOE_F32) return launch_tile<float, MODE, 64, 64, 2, false, 1, ROWS>(p, total, s);
   if constexpr (MODE != kTN) {
     switch (tile) {
-      case Tile::k64: return launch_tile<uint16_t, MODE, 64, 64, 3>(p, total, s);
-      case Tile::k64x128: return launch_tile<uint16_t, MODE, 64, 128, 3>(p, total, s);
-      case Tile::k64_stream: return launch_tile<uint16_t, MODE, 64, 64, 4, true>(p, total, s);
-      case Tile::k64x128_stream: return launch_tile<uint16_t, MODE, 64, 128, 3, true>(p, total, s);
+      case Tile::k64: return launch_tile<uint16_t, MODE, 64, 64, 3, false, 1, ROWS>(p, total, s);
+      case Tile::k64x128: return launch_tile<uint16_t, MODE, 64, 128, 3, false, 1, ROWS>(p, total, s);
+      case Tile::k64_stream: return launch_tile<uint16_t, MODE, 64, 64, 4, true, 1, ROWS>(p, total, s);
+      case Tile::k64x128_stream: return launch_tile<uint16_t, MODE, 64, 128, 3, true, 1, ROWS>(p, total, s);
       default: break;
     }
   }
-  return launch_ring<MODE, 128, 128>(p, total, s);
+  return launch_ring<MODE, 128, 128, ROWS>(p, total, s);
 }

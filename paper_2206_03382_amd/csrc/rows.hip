@@ -1,0 +1,497 @@
+// Operators around the products of experts' rows that lie one behind the other: the rows of a router's choices, the weighted combine of their results, dropout,
+// the activation's derivative with the bias gradient.  All of them move memory once, 16 bytes a lane; what bounds them is HBM.
+#include "rows.h"
+#include "rows_act.h"
+
+namespace moe {
+namespace {
+
+// ---- dropout -------------------------------------------------------------------------------------------------------------
+// Philox4x32-10 (Salmon, Moraes, Dror, Shaw, SC 2011), key = seed[0], counter = (number of the group of eight elements, seed[1]).  16 of the 128 bits for an element: a group is one
+// 16-byte piece of bf16, and ten rounds of four 32-bit products serve eight elements, which HBM takes longer for than the rounds do (32 bits for an element would not be).
+// The probability is therefore a multiple of 2^-16.  Seed and offset are read on the device, so that a captured step can be given others.
+constexpr int kGroup = 8;
+
+struct Philox {
+  uint32_t k0, k1, o0, o1;
+  __device__ __forceinline__ explicit Philox(const uint64_t* seed) {
+    const uint64_t s = seed[0], o = seed[1];
+    k0 = (uint32_t)s, k1 = (uint32_t)(s >> 32), o0 = (uint32_t)o, o1 = (uint32_t)(o >> 32);
+  }
+  // the 16-bit numbers of group g, the lower one of a word first
+  __device__ __forceinline__ void bits(uint64_t g, uint32_t (&w)[4]) const {
+    uint32_t c0 = (uint32_t)g, c1 = (uint32_t)(g >> 32), c2 = o0, c3 = o1, a = k0, b = k1;
+#pragma unroll
+    for (int i = 0; i < 10; ++i) {
+      const uint64_t p0 = (uint64_t)0xD2511F53u * c0, p1 = (uint64_t)0xCD9E8D57u * c2;
+      c0 = (uint32_t)(p1 >> 32) ^ c1 ^ a;
+      c1 = (uint32_t)p1;
+      c2 = (uint32_t)(p0 >> 32) ^ c3 ^ b;
+      c3 = (uint32_t)p0;
+      a += 0x9E3779B9u;
+      b += 0xBB67AE85u;
+    }
+    w[0] = c0, w[1] = c1, w[2] = c2, w[3] = c3;
+  }
+};
+
+// v of group g: dropped elements become zero whatever they were.
+__device__ __forceinline__ void drop(float (&v)[kGroup], const Philox& rng, uint64_t g, uint32_t below, float scale) {
+  uint32_t w[4];
+  rng.bits(g, w);
+#pragma unroll
+  for (int i = 0; i < kGroup; ++i) {
+    const uint32_t u = i & 1 ? w[i >> 1] >> 16 : w[i >> 1] & 0xffffu;
+    v[i] = u < below ? 0.f : v[i] * scale;
+  }
+}
+
+// A group of eight elements: one 16-byte piece of bf16, two of fp32.
+template <typename ET> constexpr int kPieces = (int)sizeof(ET) / 2;
+template <typename ET> struct Group { uint4 piece[kPieces<ET>]; };
+template <typename ET, bool STREAM> __device__ __forceinline__ Group<ET> load_group(const uint4* at) {
+  Group<ET> r;
+#pragma unroll
+  for (int i = 0; i < kPieces<ET>; ++i) r.piece[i] = STREAM ? load_stream(at + i) : at[i];
+  return r;
+}
+template <typename ET> __device__ __forceinline__ void unpack_group(const Group<ET>& r, float (&v)[kGroup]) {
+  constexpr int N = Vec16<ET>::N;
+#pragma unroll
+  for (int i = 0; i < kPieces<ET>; ++i) {
+    float f[N];
+    Vec16<ET>::unpack(r.piece[i], f);
+#pragma unroll
+    for (int u = 0; u < N; ++u) v[i * N + u] = f[u];
+  }
+}
+template <typename ET> __device__ __forceinline__ void store_group(uint4* at, const float (&v)[kGroup]) {
+  constexpr int N = Vec16<ET>::N;
+#pragma unroll
+  for (int i = 0; i < kPieces<ET>; ++i) {
+    float f[N];
+#pragma unroll
+    for (int u = 0; u < N; ++u) f[u] = v[i * N + u];
+    at[i] = Vec16<ET>::pack(f);
+  }
+}
+
+// out = residual + dropout(x); one rounding.
+template <typename ET, bool RES, bool DROP>
+__global__ __launch_bounds__(256) void dropout_kernel(const uint4* __restrict__ x, const uint4* residual, const uint64_t* __restrict__ seed, uint32_t below, float scale,
+                                                      int64_t groups, uint4* out) {
+  constexpr int P = kPieces<ET>;
+  const int64_t stride = (int64_t)gridDim.x * 256;
+  const Philox rng = DROP ? Philox(seed) : Philox((const uint64_t*)nullptr);
+  for (int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x; g < groups; g += stride) {
+    float v[kGroup], r[kGroup];
+    const Group<ET> a = load_group<ET, false>(x + g * P);
+    Group<ET> b;
+    if (RES) b = load_group<ET, false>(residual + g * P);
+    unpack_group<ET>(a, v);
+    if (DROP) drop(v, rng, (uint64_t)g, below, scale);
+    if (RES) {
+      unpack_group<ET>(b, r);
+#pragma unroll
+      for (int i = 0; i < kGroup; ++i) v[i] += r[i];
+    }
+    store_group<ET>(out + g * P, v);
+  }
+}
+
+// ---- the rows of a router's choices --------------------------------------------------------------------------------------
+// Expert e has min(counts[e], C) rows behind those of the experts before it; the choice (t, j) has row offsets[idx] + loc.  Every block adds up the counts by itself: they are 2 KB at
+// most, and a launch for them would take longer than all the rest.
+constexpr int kMaxRowExperts = 512;
+
+__global__ __launch_bounds__(256) void ragged_rows_kernel(const int32_t* __restrict__ idx, const int32_t* __restrict__ loc, const int32_t* __restrict__ counts, int64_t n,
+                                                          int E, int k, int64_t C, int32_t* __restrict__ offsets, int32_t* __restrict__ row_src,
+                                                          int32_t* __restrict__ row_of) {
+  __shared__ int32_t at[kMaxRowExperts + 1];
+  __shared__ int64_t sums[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  // two experts to a thread; prefix sums of the threads' pairs
+  int64_t own[2], pair = 0;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int e = 2 * tid + i;
+    int64_t c = e < E ? counts[e] : 0;
+    c = c < 0 ? 0 : c;
+    c = c < C ? c : C;
+    own[i] = c < n ? c : n;
+    pair += own[i];
+  }
+  int64_t upto = pair;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t v = __shfl_up(upto, d, 64);
+    if (lane >= d) upto += v;
+  }
+  if (lane == 63) sums[wave] = upto;
+  __syncthreads();
+  int64_t first = upto - pair;
+  for (int w = 0; w < wave; ++w) first += sums[w];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int e = 2 * tid + i;
+    if (e <= E) at[e] = (int32_t)(first < n ? first : n);
+    first += own[i];
+  }
+  if (tid == 255 && E == kMaxRowExperts) at[E] = (int32_t)(first < n ? first : n);
+  __syncthreads();
+  if (blockIdx.x == 0)
+    for (int e = tid; e <= E; e += 256) offsets[e] = at[e];
+  const int total = at[E];
+  for (int64_t p = (int64_t)blockIdx.x * 256 + tid; p < n; p += (int64_t)gridDim.x * 256) {
+    const int e = idx[p], l = loc[p];
+    int row = -1;
+    if ((unsigned)e < (unsigned)E && l >= 0 && l < at[e + 1] - at[e]) row = at[e] + l;
+    row_of[p] = row;
+    if (row >= 0) row_src[row] = (int32_t)(p / k);
+    if (p >= total) row_src[p] = -1;
+  }
+}
+
+// ---- combine -------------------------------------------------------------------------------------------------------------
+// out[t] = residual[t] + dropout(sum over the choices j, ascending, of gate_w[t,j] * Y[row_of[t,j]]), in fp32, rounded once; choices without a row are left out.  A wave has 64 groups of
+// one token's row: its rows and weights are the same for all lanes, and it has up to eight rows in flight.
+template <typename ET, bool STREAM, bool DROP>
+__global__ __launch_bounds__(256) void ragged_combine_kernel(const uint4* __restrict__ Y, int64_t R, const int32_t* __restrict__ row_of, const float* __restrict__ gate_w,
+                                                             const uint4* residual, const uint64_t* __restrict__ seed, uint32_t below, float scale, int64_t units, int per_row,
+                                                             int groups, int k, uint4* out) {
+  constexpr int P = kPieces<ET>;
+  const int lane = threadIdx.x & 63;
+  const Philox rng = DROP ? Philox(seed) : Philox((const uint64_t*)nullptr);
+  for (int64_t u = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6))); u < units; u += (int64_t)gridDim.x * 4) {
+    const int64_t t = u / per_row;
+    const int g = (int)(u - t * per_row) * 64 + lane;
+    if (g >= groups) continue;
+    float v[kGroup];
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i) v[i] = 0.f;
+    const int64_t here = (t * groups + g) * P;
+    Group<ET> res;
+    if (residual) res = load_group<ET, STREAM>(residual + here);
+    for (int j0 = 0; j0 < k; j0 += 8) {
+      Group<ET> y[8];
+      float w[8];
+      bool on[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        on[j] = false;
+        if (j0 + j < k) {
+          const int64_t row = row_of[t * k + j0 + j];
+          on[j] = row >= 0 && row < R;
+          if (on[j]) {
+            w[j] = gate_w ? gate_w[t * k + j0 + j] : 1.0f;
+            y[j] = load_group<ET, STREAM>(Y + (row * groups + g) * P);
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (!on[j]) continue;
+        float f[kGroup];
+        unpack_group<ET>(y[j], f);
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) v[i] = fmaf(w[j], f[i], v[i]);
+      }
+    }
+    if (DROP) drop(v, rng, (uint64_t)(t * groups + g), below, scale);
+    if (residual) {
+      float f[kGroup];
+      unpack_group<ET>(res, f);
+#pragma unroll
+      for (int i = 0; i < kGroup; ++i) v[i] += f[i];
+    }
+    store_group<ET>(out + here, v);
+  }
+}
+
+// d = dropout(d_out), dY[row_of[t,j]] = gate_w[t,j] * d[t], dgate_w[t,j] = <d[t], Y[row_of[t,j]]>.  W waves to a token (4: rows of more than 128 groups); d_out is read once for
+// eight choices.  The order of the sums is fixed by the sizes.
+template <typename ET, bool STREAM, bool DROP, int W>
+__global__ __launch_bounds__(256) void ragged_combine_backward_kernel(const uint4* __restrict__ d_out, const uint4* __restrict__ Y, int64_t R, const int32_t* __restrict__ row_of,
+                                                                      const float* __restrict__ gate_w, const uint64_t* __restrict__ seed, uint32_t below, float scale,
+                                                                      int64_t T, int groups, int k, uint4* __restrict__ dY, float* __restrict__ dgate_w) {
+  constexpr int P = kPieces<ET>;
+  __shared__ float part[4][8];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Philox rng = DROP ? Philox(seed) : Philox((const uint64_t*)nullptr);
+  const int64_t step = (int64_t)gridDim.x * (4 / W);
+  for (int64_t t = (int64_t)blockIdx.x * (4 / W) + (W == 4 ? 0 : wave); t < T; t += step) {
+    for (int j0 = 0; j0 < k; j0 += 8) {
+      int64_t row[8];
+      float w[8], acc[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        row[j] = -1;
+        w[j] = acc[j] = 0.f;
+        if (j0 + j < k) {
+          const int64_t r = row_of[t * k + j0 + j];
+          if (r >= 0 && r < R) {
+            row[j] = r;
+            w[j] = gate_w ? gate_w[t * k + j0 + j] : 1.0f;
+          }
+        }
+      }
+      for (int g = (W == 4 ? wave * 64 : 0) + lane; g < groups; g += W * 64) {
+        const Group<ET> a = load_group<ET, false>(d_out + (t * groups + g) * P);
+        Group<ET> y[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (row[j] >= 0) y[j] = load_group<ET, STREAM>(Y + (row[j] * groups + g) * P);
+        float d[kGroup];
+        unpack_group<ET>(a, d);
+        if (DROP) drop(d, rng, (uint64_t)(t * groups + g), below, scale);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (row[j] < 0) continue;
+          float f[kGroup], o[kGroup];
+          unpack_group<ET>(y[j], f);
+#pragma unroll
+          for (int i = 0; i < kGroup; ++i) {
+            acc[j] = fmaf(d[i], f[i], acc[j]);
+            o[i] = w[j] * d[i];
+          }
+          store_group<ET>(dY + (row[j] * groups + g) * P, o);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (j0 + j >= k) break;
+#pragma unroll
+        for (int m = 32; m >= 1; m >>= 1) acc[j] += __shfl_xor(acc[j], m, 64);
+        if (W == 1) {
+          if (lane == 0) dgate_w[t * k + j0 + j] = acc[j];
+        } else if (lane == 0) {
+          part[wave][j] = acc[j];
+        }
+      }
+      if (W == 4) {
+        __syncthreads();
+        if ((int)threadIdx.x < 8 && j0 + (int)threadIdx.x < k) {
+          const int j = threadIdx.x;
+          dgate_w[t * k + j0 + j] = part[0][j] + part[1][j] + part[2][j] + part[3][j];
+        }
+        __syncthreads();
+      }
+    }
+  }
+}
+
+// ---- the activation's derivative and the bias gradient ---------------------------------------------------------------------
+// dp[r] = dy[r] * act'(pre[r]) and, in the same pass, db[e] = sum of dp over the expert's rows.  A block has a strip of 16 groups (256 bytes of bf16) and a slice of an expert's rows; 16
+// classes of rows, each summed in ascending order by one thread, then class by class, then, by a second launch, slice by slice: in an order that the sizes fix.  The sums are of
+// dp before its rounding.  dp is rounded to the storage type: the matrix cores take it as an operand.
+constexpr int kStrip = 16, kClasses = 16;
+
+__device__ __forceinline__ int64_t clamp_row(int64_t v, int64_t R) { return v < 0 ? 0 : (v < R ? v : R); }
+
+template <typename ET, int ACT, bool SUM>
+__global__ __launch_bounds__(256) void rows_act_backward_kernel(const uint4* __restrict__ dy, const uint4* __restrict__ pre, const int32_t* __restrict__ offsets, int64_t R, int groups,
+                                                                int slices, uint4* __restrict__ dp, float* __restrict__ sums, ET* __restrict__ db) {
+  constexpr int P = kPieces<ET>;
+  __shared__ float part[kClasses][kStrip * kGroup + 1];
+  const int e = blockIdx.y, slice = blockIdx.z;
+  const int64_t lo = offsets ? clamp_row(offsets[e], R) : 0, end = offsets ? clamp_row(offsets[e + 1], R) : R;
+  const int64_t each = (end - lo + slices - 1) / slices;
+  const int64_t from = lo + slice * each, to = from + each < end ? from + each : end;
+  const int cls = threadIdx.x / kStrip, g = blockIdx.x * kStrip + threadIdx.x % kStrip;
+  float s[kGroup];
+#pragma unroll
+  for (int i = 0; i < kGroup; ++i) s[i] = 0.f;
+  if (g < groups) {
+    constexpr int U = 4;                                            // rows of a class in flight
+    auto one = [&](int64_t at, const Group<ET>& a, const Group<ET>& b) __attribute__((always_inline)) {
+      float v[kGroup], p[kGroup];
+      unpack_group<ET>(a, v);
+      if (ACT >= 0) {
+        unpack_group<ET>(b, p);
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) v[i] *= rows_act_grad_as<ET, ACT>(p[i]);
+        store_group<ET>(dp + at, v);
+      }
+      if (SUM) {
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) s[i] += v[i];
+      }
+    };
+    int64_t r = from + cls;
+    for (; r + (U - 1) * kClasses < to; r += U * kClasses) {
+      Group<ET> a[U], b[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i) a[i] = load_group<ET, false>(dy + ((r + i * kClasses) * groups + g) * P);
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (ACT >= 0) b[i] = load_group<ET, false>(pre + ((r + i * kClasses) * groups + g) * P);
+#pragma unroll
+      for (int i = 0; i < U; ++i) one(((r + i * kClasses) * groups + g) * P, a[i], b[i]);
+    }
+    for (; r < to; r += kClasses) {
+      const int64_t at = (r * groups + g) * P;
+      const Group<ET> a = load_group<ET, false>(dy + at);
+      Group<ET> b;
+      if (ACT >= 0) b = load_group<ET, false>(pre + at);
+      one(at, a, b);
+    }
+  }
+  if (SUM) {
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i) part[cls][threadIdx.x % kStrip * kGroup + i] = s[i];
+    __syncthreads();
+    const int col = blockIdx.x * kStrip * kGroup + threadIdx.x;
+    if (threadIdx.x < kStrip * kGroup && col < groups * kGroup) {
+      float t = 0.f;
+#pragma unroll
+      for (int c = 0; c < kClasses; ++c) t += part[c][threadIdx.x];
+      if (slices == 1) store_from_f32<ET>(db + (int64_t)e * groups * kGroup + col, t);
+      else sums[((int64_t)slice * gridDim.y + e) * groups * kGroup + col] = t;
+    }
+  }
+}
+
+// db[i] = the sum of the slices' sums, n of them apart
+template <typename ET>
+__global__ __launch_bounds__(256) void slice_sum_kernel(const float* __restrict__ sums, int slices, int64_t n, ET* __restrict__ db) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  float t = 0.f;
+  for (int s = 0; s < slices; ++s) t += sums[s * n + i];
+  store_from_f32<ET>(db + i, t);
+}
+
+// Slices of an expert's rows: about eight blocks to a unit, no fewer than 64 rows on average, at most 64.
+int act_backward_slices(int64_t R, int64_t E, int64_t N) {
+  const int64_t strips = ceil_div(N / kGroup, kStrip);
+  int64_t n = ceil_div(2048, strips * E), most = ceil_div(ceil_div(R, E), 64);
+  n = n < most ? n : most;
+  return (int)(n < 1 ? 1 : (n > 64 ? 64 : n));
+}
+
+unsigned blocks_for(int64_t work, int64_t per_block, int64_t most) {
+  const int64_t b = ceil_div(work, per_block);
+  return (unsigned)(b < most ? b : most);
+}
+
+// beyond this, data that is read once is loaded past the caches
+constexpr double kStreamBytes = 536870912.0;
+
+}  // namespace
+
+hipError_t launch_dropout(const void* x, const void* residual, const Dropout& d, int dtype, int64_t n, void* out, hipStream_t s) {
+  const int64_t groups = n / kGroup;
+  const dim3 grid(blocks_for(groups, 256, 1 << 20)), block(256);
+#define MOE_LAUNCH_DROPOUT(ET, RES, DROP) \
+  dropout_kernel<ET, RES, DROP><<<grid, block, 0, s>>>((const uint4*)x, (const uint4*)residual, d.seed, d.below, d.scale, groups, (uint4*)out)
+#define MOE_LAUNCH_DROPOUT_ET(ET)                              \
+  do {                                                         \
+    if (residual && d.below) MOE_LAUNCH_DROPOUT(ET, true, true);   \
+    else if (residual) MOE_LAUNCH_DROPOUT(ET, true, false);    \
+    else if (d.below) MOE_LAUNCH_DROPOUT(ET, false, true);     \
+    else MOE_LAUNCH_DROPOUT(ET, false, false);                 \
+  } while (0)
+  if (dtype == MOE_F32) MOE_LAUNCH_DROPOUT_ET(float);
+  else MOE_LAUNCH_DROPOUT_ET(uint16_t);
+#undef MOE_LAUNCH_DROPOUT_ET
+#undef MOE_LAUNCH_DROPOUT
+  return hipGetLastError();
+}
+
+hipError_t launch_ragged_rows(const int32_t* idx, const int32_t* loc, const int32_t* counts, int64_t T, int64_t E, int k, int64_t C, int32_t* offsets, int32_t* row_src,
+                              int32_t* row_of, hipStream_t s) {
+  ragged_rows_kernel<<<dim3(blocks_for(T * k, 256, 1024)), dim3(256), 0, s>>>(idx, loc, counts, T * k, (int)E, k, C > 0 ? C : T * k, offsets, row_src, row_of);
+  return hipGetLastError();
+}
+
+hipError_t launch_ragged_combine(const void* Y, int64_t R, const int32_t* row_of, const float* gate_w, const void* residual, const Dropout& d, int dtype, int64_t T,
+                                 int64_t M, int k, void* out, hipStream_t s) {
+  const int groups = (int)(M / kGroup), per_row = (int)ceil_div(groups, 64);
+  const int64_t units = T * per_row;
+  const dim3 grid(blocks_for(units, 4, 1 << 20)), block(256);
+  const bool stream = (double)R * M * (dtype == MOE_F32 ? 4 : 2) >= kStreamBytes;
+#define MOE_LAUNCH_COMBINE(ET, STREAM, DROP)                                                                                                                        \
+  ragged_combine_kernel<ET, STREAM, DROP><<<grid, block, 0, s>>>((const uint4*)Y, R, row_of, gate_w, (const uint4*)residual, d.seed, d.below, d.scale, units, per_row, \
+                                                                 groups, k, (uint4*)out)
+#define MOE_LAUNCH_COMBINE_ET(ET)                                \
+  do {                                                           \
+    if (stream && d.below) MOE_LAUNCH_COMBINE(ET, true, true);   \
+    else if (stream) MOE_LAUNCH_COMBINE(ET, true, false);        \
+    else if (d.below) MOE_LAUNCH_COMBINE(ET, false, true);       \
+    else MOE_LAUNCH_COMBINE(ET, false, false);                   \
+  } while (0)
+  if (dtype == MOE_F32) MOE_LAUNCH_COMBINE_ET(float);
+  else MOE_LAUNCH_COMBINE_ET(uint16_t);
+#undef MOE_LAUNCH_COMBINE_ET
+#undef MOE_LAUNCH_COMBINE
+  return hipGetLastError();
+}
+
+hipError_t launch_ragged_combine_backward(const void* d_out, const void* Y, int64_t R, const int32_t* row_of, const float* gate_w, const Dropout& d, int dtype, int64_t T,
+                                          int64_t M, int k, void* dY, float* dgate_w, hipStream_t s) {
+  const int groups = (int)(M / kGroup);
+  const bool stream = (double)R * M * (dtype == MOE_F32 ? 4 : 2) >= kStreamBytes, wide = groups > 128;
+  const dim3 grid(blocks_for(T, wide ? 1 : 4, 1 << 20)), block(256);
+#define MOE_LAUNCH_BACKWARD(ET, STREAM, DROP, W)                                                                                                                      \
+  ragged_combine_backward_kernel<ET, STREAM, DROP, W><<<grid, block, 0, s>>>((const uint4*)d_out, (const uint4*)Y, R, row_of, gate_w, d.seed, d.below, d.scale, T, groups, \
+                                                                             k, (uint4*)dY, dgate_w)
+#define MOE_LAUNCH_BACKWARD_W(ET, STREAM, DROP)                \
+  do {                                                         \
+    if (wide) MOE_LAUNCH_BACKWARD(ET, STREAM, DROP, 4);        \
+    else MOE_LAUNCH_BACKWARD(ET, STREAM, DROP, 1);             \
+  } while (0)
+#define MOE_LAUNCH_BACKWARD_ET(ET)                               \
+  do {                                                           \
+    if (stream && d.below) MOE_LAUNCH_BACKWARD_W(ET, true, true);   \
+    else if (stream) MOE_LAUNCH_BACKWARD_W(ET, true, false);     \
+    else if (d.below) MOE_LAUNCH_BACKWARD_W(ET, false, true);    \
+    else MOE_LAUNCH_BACKWARD_W(ET, false, false);                \
+  } while (0)
+  if (dtype == MOE_F32) MOE_LAUNCH_BACKWARD_ET(float);
+  else MOE_LAUNCH_BACKWARD_ET(uint16_t);
+#undef MOE_LAUNCH_BACKWARD_ET
+#undef MOE_LAUNCH_BACKWARD_W
+#undef MOE_LAUNCH_BACKWARD
+  return hipGetLastError();
+}
+
+size_t rows_act_backward_bytes(int64_t R, int64_t E, int64_t N) {
+  const int slices = act_backward_slices(R, E, N);
+  return slices > 1 ? (size_t)slices * E * N * 4 : 0;
+}
+
+hipError_t launch_rows_act_backward(const void* dy, const void* pre, int act, int dtype, const int32_t* offsets, int64_t R, int64_t E, int64_t N, void* ws, void* dp,
+                                    void* db, hipStream_t s) {
+  if (act < 0 && !db) return hipSuccess;
+  const int groups = (int)(N / kGroup), slices = act_backward_slices(R, E, N);
+  const dim3 grid((unsigned)ceil_div(groups, kStrip), (unsigned)E, (unsigned)slices), block(256);
+#define MOE_LAUNCH_ACT(ET, ACT, SUM) \
+  rows_act_backward_kernel<ET, ACT, SUM><<<grid, block, 0, s>>>((const uint4*)dy, (const uint4*)pre, offsets, R, groups, slices, (uint4*)dp, (float*)ws, (ET*)db)
+#define MOE_LAUNCH_ACT_SUM(ET, ACT)              \
+  do {                                           \
+    if (db) MOE_LAUNCH_ACT(ET, ACT, true);       \
+    else MOE_LAUNCH_ACT(ET, ACT, false);         \
+  } while (0)
+#define MOE_LAUNCH_ACT_ET(ET)                                                   \
+  do {                                                                          \
+    switch (act) {                                                              \
+      case MOE_ACT_RELU: MOE_LAUNCH_ACT_SUM(ET, MOE_ACT_RELU); break;           \
+      case MOE_ACT_GELU: MOE_LAUNCH_ACT_SUM(ET, MOE_ACT_GELU); break;           \
+      case MOE_ACT_SILU: MOE_LAUNCH_ACT_SUM(ET, MOE_ACT_SILU); break;           \
+      default: MOE_LAUNCH_ACT(ET, -1, true);                                    \
+    }                                                                           \
+  } while (0)
+  if (dtype == MOE_F32) MOE_LAUNCH_ACT_ET(float);
+  else MOE_LAUNCH_ACT_ET(uint16_t);
+#undef MOE_LAUNCH_ACT_ET
+#undef MOE_LAUNCH_ACT_SUM
+#undef MOE_LAUNCH_ACT
+  if (hipError_t err = hipGetLastError()) return err;
+  if (!db || slices == 1) return hipSuccess;
+  const int64_t n = E * N;
+  if (dtype == MOE_F32) slice_sum_kernel<float><<<dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, s>>>((const float*)ws, slices, n, (float*)db);
+  else slice_sum_kernel<uint16_t><<<dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, s>>>((const float*)ws, slices, n, (uint16_t*)db);
+  return hipGetLastError();
+}
+
+}  // namespace moe

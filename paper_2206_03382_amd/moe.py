@@ -84,6 +84,16 @@ SIGNATURES = {
     "moe_layer_forward8": (_i32, [_vp] * 11 + [_i64, _i64, _i64, _i64, _i32, _dbl, _i32, _i32, _i32] + [_vp] * 7 + [_sz, _vp]),
     "moe_layer_few_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64, _i32, _i32]),
     "moe_layer_forward_few": (_i32, [_vp] * 9 + [_i64, _i64, _i64, _i64, _i32, _dbl, _i32, _i32, _i32] + [_vp] * 7 + [_sz, _vp]),
+    "moe_ragged_rows": (_i32, [_vp, _vp, _vp, _i64, _i64, _i32, _i64, _vp, _vp, _vp, _vp]),
+    "moe_ragged_matmul": (_i32, [_vp, _vp, _i64, _vp, _vp, _i32, _i32, _vp, _i64, _i64, _i64, _i64, _vp, _vp, _vp]),
+    "moe_ragged_matmul_backward_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64, _i32, _i32]),
+    "moe_ragged_matmul_backward": (_i32, [_vp, _vp, _vp, _i64, _vp, _vp, _i32, _vp, _i32, _i32, _vp, _i64, _i64, _i64, _i64, _vp, _sz, _vp, _vp, _vp, _vp]),
+    "moe_linear": (_i32, [_vp, _vp, _vp, _i32, _vp, _i32, _i64, _i64, _i64, _vp, _vp, _vp]),
+    "moe_linear_backward_workspace_bytes": (_sz, [_i64, _i64, _i64, _i32, _i32]),
+    "moe_linear_backward": (_i32, [_vp, _vp, _vp, _vp, _i32, _i32, _i64, _i64, _i64, _vp, _sz, _vp, _vp, _vp, _vp]),
+    "moe_dropout": (_i32, [_vp, _vp, _dbl, _vp, _i32, _i64, _vp, _vp]),
+    "moe_ragged_combine": (_i32, [_vp, _i64, _vp, _vp, _vp, _dbl, _vp, _i32, _i64, _i64, _i32, _vp, _vp]),
+    "moe_ragged_combine_backward": (_i32, [_vp, _vp, _i64, _vp, _vp, _dbl, _vp, _i32, _i64, _i64, _i32, _vp, _vp, _vp]),
     "moe_event_create": (_i32, [_c.POINTER(_vp)]),
     "moe_event_destroy": (_i32, [_vp]),
     "moe_event_record": (_i32, [_vp, _vp]),
@@ -847,3 +857,215 @@ class NormMoELayer8:
             return self.few.forward(n["y"]), n["h"]
         _check(lib().moe_layer_forward8(_p(n["y"]), _p(n["y8"].q), _p(n["y8"].s), *self._args, _stream()), "moe_layer_forward8")
         return self.out, n["h"]
+
+
+# ---- experts' rows one behind the other, dense projections, dropout ------------------------------------------------------
+
+def _here(*tensors: Optional[torch.Tensor]) -> None:
+    """The library launches on the current device's stream: all tensors have to be there."""
+    device = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError("tensors must be on the current device")
+
+
+def _as_stored(t: torch.Tensor, like: torch.Tensor, what: str, *shape: int) -> None:
+    if t.dtype != like.dtype or t.shape != shape:
+        raise ValueError(f"{what}: expected {list(shape)} in {like.dtype}")
+
+
+def _check_offsets(offsets: torch.Tensor, E: int) -> None:
+    if offsets.dtype != torch.int32 or offsets.shape != (E + 1,):
+        raise ValueError(f"offsets: expected {[E + 1]} in torch.int32")
+
+
+def _check_gather(gather: Optional[torch.Tensor]) -> None:
+    if gather is not None and (gather.dtype != torch.int32 or gather.dim() != 1):
+        raise ValueError("gather must be int32 [R]")
+
+
+class RaggedRows(NamedTuple):
+    """Where a router's choices are: expert e's rows are offsets[e] up to offsets[e + 1]; row_src the token of a row, row_of [T,k] the row of a choice (-1: none)."""
+    offsets: torch.Tensor
+    row_src: torch.Tensor
+    row_of: torch.Tensor
+
+
+def ragged_rows(idx: torch.Tensor, loc: torch.Tensor, counts: torch.Tensor, C: int = 0) -> RaggedRows:
+    """The rows of the choices of gate_topk or gate_route, one expert's behind the other's; C: a capacity beyond which they are dropped (0: none is)."""
+    if idx.dim() != 2 or idx.dtype != torch.int32:
+        raise ValueError("idx must be int32 [T,k]")
+    T, k = idx.shape
+    E = counts.shape[0]
+    _check_int32(loc, T, k)
+    _check_int32(counts, E)
+    _here(idx, loc, counts)
+    dev = idx.device
+    r = RaggedRows(torch.empty((E + 1,), dtype=torch.int32, device=dev), torch.empty((T * k,), dtype=torch.int32, device=dev),
+                   torch.empty((T, k), dtype=torch.int32, device=dev))
+    _check(lib().moe_ragged_rows(_p(idx), _p(loc), _p(counts), T, E, k, C, _p(r.offsets), _p(r.row_src), _p(r.row_of), _stream()), "moe_ragged_rows")
+    return r
+
+
+def ragged_matmul(A: torch.Tensor, W: torch.Tensor, offsets: torch.Tensor, bias: Optional[torch.Tensor] = None, act: int = ACT_NONE,
+                  gather: Optional[torch.Tensor] = None, keep_pre: bool = False, out: Optional[torch.Tensor] = None):
+    """out[r] = act(A[r] W[e] + bias[e]) for the rows r of expert e (offsets [E+1]): A [R,K], or [tokens,K] with gather [R] (ragged_rows' row_src), W [E,K,N].  Rows behind the
+    last expert's hold whatever the memory did.  keep_pre: (out, the values before the activation), which ragged_matmul_backward takes."""
+    E, K, N = W.shape
+    _check_gather(gather)
+    rows = A.shape[0]
+    R = rows if gather is None else gather.shape[0]
+    code = _dtype_code(W)
+    _as_stored(A, W, "A", rows, K)
+    _check_offsets(offsets, E)
+    if bias is not None:
+        _as_stored(bias, W, "bias", E, N)
+    if out is None:
+        out = torch.empty((R, N), dtype=W.dtype, device=W.device)
+    else:
+        _check_out(out, (R, N), W.dtype)
+    pre = torch.empty_like(out) if keep_pre else None
+    _here(A, W, offsets, bias, gather, out)
+    _check(lib().moe_ragged_matmul(_p(A), _p(gather), rows, _p(W), _p(bias), act, code, _p(offsets), R, E, K, N, _p(pre), _p(out), _stream()), "moe_ragged_matmul")
+    return (out, pre) if keep_pre else out
+
+
+def ragged_matmul_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, offsets: torch.Tensor, act: int = ACT_NONE, pre: Optional[torch.Tensor] = None,
+                           gather: Optional[torch.Tensor] = None, x_act: int = ACT_NONE, x_pre: Optional[torch.Tensor] = None, want_dx: bool = True, want_dW: bool = True,
+                           want_db: bool = True) -> Dict[str, Optional[torch.Tensor]]:
+    """dx [R,K] (by row: a token's are summed by ragged_combine without weights), dW and db of ragged_matmul from dy [R,N] and, with an activation, the pre that it kept.
+    x_act, x_pre: x are the activations of values x_pre, and dx is the gradient of those."""
+    E, K, N = W.shape
+    _check_gather(gather)
+    rows, R = x.shape[0], dy.shape[0]
+    if R != (rows if gather is None else gather.shape[0]):
+        raise ValueError("dy must have a row for every row of x, or of gather")
+    code = _dtype_code(W)
+    _as_stored(x, W, "x", rows, K)
+    _as_stored(dy, W, "dy", R, N)
+    _check_offsets(offsets, E)
+    if pre is not None:
+        _as_stored(pre, W, "pre", R, N)
+    if x_pre is not None:
+        _as_stored(x_pre, W, "x_pre", R, K)
+    _here(dy, x, W, offsets, pre, gather, x_pre)
+    nbytes = int(lib().moe_ragged_matmul_backward_workspace_bytes(R, E, K, N, act, code))
+    if nbytes == 0:
+        raise MoEError(UNSUPPORTED, "moe_ragged_matmul_backward_workspace_bytes")
+    dev = W.device
+    ws = torch.empty((nbytes,), dtype=torch.uint8, device=dev)
+    g = dict(dx=torch.empty((R, K), dtype=W.dtype, device=dev) if want_dx else None, dW=torch.empty_like(W) if want_dW else None,
+             db=torch.empty((E, N), dtype=W.dtype, device=dev) if want_db else None)
+    _check(lib().moe_ragged_matmul_backward(_p(dy), _p(x), _p(gather), rows, _p(W), _p(pre), act, _p(x_pre), x_act, code, _p(offsets), R, E, K, N, _p(ws), nbytes,
+                                            _p(g["dx"]), _p(g["dW"]), _p(g["db"]), _stream()), "moe_ragged_matmul_backward")
+    return g
+
+
+def linear(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None, act: int = ACT_NONE, residual: Optional[torch.Tensor] = None, keep_pre: bool = False,
+           out: Optional[torch.Tensor] = None):
+    """out = act(x W + bias) + residual: x [T,K], W [K,N].  keep_pre: (out, the values before the activation), which linear_backward takes.  out may be residual."""
+    T, (K, N) = x.shape[0], W.shape
+    code = _dtype_code(W)
+    _as_stored(x, W, "x", T, K)
+    if bias is not None:
+        _as_stored(bias, W, "bias", N)
+    if residual is not None:
+        _as_stored(residual, W, "residual", T, N)
+    if out is None:
+        out = torch.empty((T, N), dtype=W.dtype, device=W.device)
+    else:
+        _check_out(out, (T, N), W.dtype)
+    pre = torch.empty_like(out) if keep_pre else None
+    _here(x, W, bias, residual, out)
+    _check(lib().moe_linear(_p(x), _p(W), _p(bias), act, _p(residual), code, T, K, N, _p(pre), _p(out), _stream()), "moe_linear")
+    return (out, pre) if keep_pre else out
+
+
+def linear_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, act: int = ACT_NONE, pre: Optional[torch.Tensor] = None, want_dx: bool = True, want_dW: bool = True,
+                    want_db: bool = True) -> Dict[str, Optional[torch.Tensor]]:
+    """dx, dW and db of linear from dy [T,N] and, with an activation, the pre that it kept; the residual's gradient is dy."""
+    T, (K, N) = x.shape[0], W.shape
+    code = _dtype_code(W)
+    _as_stored(x, W, "x", T, K)
+    _as_stored(dy, W, "dy", T, N)
+    if pre is not None:
+        _as_stored(pre, W, "pre", T, N)
+    _here(dy, x, W, pre)
+    nbytes = int(lib().moe_linear_backward_workspace_bytes(T, K, N, act, code))
+    if nbytes == 0:
+        raise MoEError(UNSUPPORTED, "moe_linear_backward_workspace_bytes")
+    dev = W.device
+    ws = torch.empty((nbytes,), dtype=torch.uint8, device=dev)
+    g = dict(dx=torch.empty((T, K), dtype=W.dtype, device=dev) if want_dx else None, dW=torch.empty_like(W) if want_dW else None,
+             db=torch.empty((N,), dtype=W.dtype, device=dev) if want_db else None)
+    _check(lib().moe_linear_backward(_p(dy), _p(x), _p(W), _p(pre), act, code, T, K, N, _p(ws), nbytes, _p(g["dx"]), _p(g["dW"]), _p(g["db"]), _stream()),
+           "moe_linear_backward")
+    return g
+
+
+def _check_seed(seed: torch.Tensor) -> None:
+    if seed.dtype != torch.int64 or seed.shape != (2,):
+        raise ValueError("seed must be int64 [2] on the device: the generator's seed and an offset")
+
+
+def dropout(x: torch.Tensor, p: float, seed: torch.Tensor, residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """residual + dropout(x) with probability p: the mask comes from the numbers in seed (int64 [2] on the device: seed and offset) and an element's place, and is never stored.
+    dropout(dy, p, seed) is the gradient of x.  out may be x or residual."""
+    code = _dtype_code(x)
+    _check_seed(seed)
+    if residual is not None and (residual.shape != x.shape or residual.dtype != x.dtype):
+        raise ValueError("residual must have x's shape and type")
+    if out is None:
+        out = torch.empty_like(x)
+    else:
+        _check_out(out, x.shape, x.dtype)
+    _here(x, seed, residual, out)
+    _check(lib().moe_dropout(_p(x), _p(residual), p, _p(seed), code, x.numel(), _p(out), _stream()), "moe_dropout")
+    return out
+
+
+def _check_combine(Y: torch.Tensor, row_of: torch.Tensor, gate_w: Optional[torch.Tensor], dropout: Optional[Tuple[float, torch.Tensor]]) -> Tuple[float, Optional[torch.Tensor]]:
+    if Y.dim() != 2 or row_of.dim() != 2 or row_of.dtype != torch.int32:
+        raise ValueError("Y must be [R,M] and row_of int32 [T,k]")
+    if gate_w is not None and (gate_w.dtype != torch.float32 or gate_w.shape != row_of.shape):
+        raise ValueError("gate_w must be float32 [T,k]")
+    if dropout is None:
+        return 0.0, None
+    _check_seed(dropout[1])
+    return dropout
+
+
+def ragged_combine(Y: torch.Tensor, row_of: torch.Tensor, gate_w: Optional[torch.Tensor], residual: Optional[torch.Tensor] = None,
+                   dropout: Optional[Tuple[float, torch.Tensor]] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """out[t] = residual[t] + dropout(sum_j gate_w[t,j] Y[row_of[t,j]]): Y [R,M], row_of of ragged_rows, gate_w [T,k] or None (ones), dropout (p, seed) as in dropout().  out may be
+    residual."""
+    p, seed = _check_combine(Y, row_of, gate_w, dropout)
+    (T, k), (R, M) = row_of.shape, Y.shape
+    code = _dtype_code(Y)
+    if residual is not None:
+        _as_stored(residual, Y, "residual", T, M)
+    if out is None:
+        out = torch.empty((T, M), dtype=Y.dtype, device=Y.device)
+    else:
+        _check_out(out, (T, M), Y.dtype)
+    _here(Y, row_of, gate_w, residual, seed, out)
+    _check(lib().moe_ragged_combine(_p(Y), R, _p(row_of), _p(gate_w), _p(residual), p, _p(seed), code, T, M, k, _p(out), _stream()), "moe_ragged_combine")
+    return out
+
+
+def ragged_combine_backward(d_out: torch.Tensor, Y: torch.Tensor, row_of: torch.Tensor, gate_w: Optional[torch.Tensor], dropout: Optional[Tuple[float, torch.Tensor]] = None,
+                            dY: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(dY [R,M], dgate_w [T,k]) of ragged_combine, with the same dropout; the residual's gradient is d_out.  Rows that no choice has hold whatever dY's memory did."""
+    p, seed = _check_combine(Y, row_of, gate_w, dropout)
+    (T, k), (R, M) = row_of.shape, Y.shape
+    code = _dtype_code(Y)
+    _as_stored(d_out, Y, "d_out", T, M)
+    if dY is None:
+        dY = torch.empty_like(Y)
+    else:
+        _check_out(dY, Y.shape, Y.dtype)
+    dgate_w = torch.empty((T, k), dtype=torch.float32, device=Y.device)
+    _here(d_out, Y, row_of, gate_w, seed, dY)
+    _check(lib().moe_ragged_combine_backward(_p(d_out), _p(Y), R, _p(row_of), _p(gate_w), p, _p(seed), code, T, M, k, _p(dY), _p(dgate_w), _stream()),
+           "moe_ragged_combine_backward")
+    return dY, dgate_w
