@@ -460,9 +460,11 @@ int moe_ragged_matmul_backward(const void* dy, const void* x, const int32_t* gat
 
 /* A dense projection (an expert that all tokens share, the projection that closes a block):  out = act(x W + bias) + residual.
  *   x [T,K], W [K,N], bias [N] or NULL, residual [T,N] or NULL (it may be out), out and pre [T,N]; everything else as moe_ragged_matmul.  From one token on.
+ *   ws: moe_linear_workspace_bytes, 256-byte aligned; 0 where none is needed, which may then be NULL.
  * The gradients as moe_ragged_matmul_backward's; that of the residual is dy. */
-int moe_linear(const void* x, const void* W, const void* bias, int act, const void* residual, int dtype, int64_t T, int64_t K, int64_t N, void* pre, void* out,
-               void* stream);
+size_t moe_linear_workspace_bytes(int64_t T, int64_t K, int64_t N, int dtype);
+int moe_linear(const void* x, const void* W, const void* bias, int act, const void* residual, int dtype, int64_t T, int64_t K, int64_t N, void* ws, size_t ws_bytes,
+               void* pre, void* out, void* stream);
 size_t moe_linear_backward_workspace_bytes(int64_t T, int64_t K, int64_t N, int act, int dtype);
 int moe_linear_backward(const void* dy, const void* x, const void* W, const void* pre, int act, int dtype, int64_t T, int64_t K, int64_t N, void* ws, size_t ws_bytes,
                         void* dx, void* dW, void* db, void* stream);

@@ -90,7 +90,7 @@ int moe_ragged_matmul(const void* A, const int32_t* gather, int64_t A_rows, cons
   if (int st = product_status(R, E, K, N)) return st;
   if ((gather && A_rows >= kMaxRows) || !all_aligned({A, W, bias, pre, out}, 16) || !all_aligned({gather, offsets}, 4)) return MOE_UNSUPPORTED;
   const RowsProduct p = {A, W, bias, nullptr, offsets, gather, A_rows, R, E, K, N, act, dtype, out, pre};
-  return status_of(launch_rows_product(p, (hipStream_t)stream));
+  return status_of(launch_rows_product(p, nullptr, (hipStream_t)stream));
 }
 
 size_t moe_ragged_matmul_backward_workspace_bytes(int64_t R, int64_t E, int64_t K, int64_t N, int act, int dtype) {
@@ -110,13 +110,20 @@ int moe_ragged_matmul_backward(const void* dy, const void* x, const int32_t* gat
   return backward(dy, x, gather, x_rows, W, pre, act, x_pre, x_act, dtype, offsets, R, E, K, N, (char*)ws, dx, dW, db, (hipStream_t)stream);
 }
 
-int moe_linear(const void* x, const void* W, const void* bias, int act, const void* residual, int dtype, int64_t T, int64_t K, int64_t N, void* pre, void* out,
-               void* stream) {
+size_t moe_linear_workspace_bytes(int64_t T, int64_t K, int64_t N, int dtype) {
+  return dtype_ok(dtype) && product_status(T, 1, K, N) == MOE_OK ? rows_product_bytes(dtype, T, K, N) : 0;
+}
+
+int moe_linear(const void* x, const void* W, const void* bias, int act, const void* residual, int dtype, int64_t T, int64_t K, int64_t N, void* ws, size_t ws_bytes,
+               void* pre, void* out, void* stream) {
   if (!x || !W || !out || !dtype_ok(dtype) || !any_act(act)) return MOE_INVALID_ARG;
   if (int st = product_status(T, 1, K, N)) return st;
-  if (!all_aligned({x, W, bias, residual, pre, out}, 16)) return MOE_UNSUPPORTED;
+  const size_t need = rows_product_bytes(dtype, T, K, N);
+  if (need > 0 && !ws) return MOE_INVALID_ARG;
+  if (!all_aligned({x, W, bias, residual, pre, out}, 16) || !all_aligned({ws}, 256)) return MOE_UNSUPPORTED;
+  if (need > ws_bytes) return MOE_WORKSPACE_TOO_SMALL;
   const RowsProduct p = {x, W, bias, residual, nullptr, nullptr, 0, T, 1, K, N, act, dtype, out, pre};
-  return status_of(launch_rows_product(p, (hipStream_t)stream));
+  return status_of(launch_rows_product(p, ws, (hipStream_t)stream));
 }
 
 size_t moe_linear_backward_workspace_bytes(int64_t T, int64_t K, int64_t N, int act, int dtype) {

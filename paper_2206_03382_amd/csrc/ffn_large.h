@@ -493,53 +493,76 @@ __global__ __launch_bounds__(kThreads) void grouped_gemm_mfma_kernel(const uint1
   const int64_t out_at = ((MODE == kTN ? (int64_t)e * C : first) + m0 + wm * 128) * N + n0 + wn * 128;
   const int64_t live = rows - m0 - wm * 128;                        // rows of this wave's tile that exist
   if constexpr (ROWS) {
-    // What the sums are joined with comes into the pieces that the results go to, by direct loads; a lane joins its own.
+    // 32 rows after the other: activations into the wave's LDS, from there whole pieces of rows to memory, which takes the stores of one part while the next one's activations
+    // are computed.  What the sums are joined with comes into the same places of LDS before, by direct loads that all go out first; a lane joins its own.
     if (live <= 0) return;                                          // no barrier follows
-    const uint32_t wtile_addr = (uint32_t)(uintptr_t)LDS_PTR(char, wtile);
-    auto write_rows = [&](auto raw_tag, uint16_t* dst, const uint16_t* with) {
-      constexpr bool RAW = decltype(raw_tag)::value;
-      constexpr int A_ = RAW ? -1 : ACT;
-      if (with) {
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    auto write_rows = [&](auto with_tag) __attribute__((always_inline)) {
+      constexpr bool WITH = decltype(with_tag)::value;
+      if (WITH) {
+        const uint32_t wtile_addr = (uint32_t)(uintptr_t)LDS_PTR(char, wtile);
         for (int it0 = 0; it0 < ni * 8; it0 += 8)
 #pragma unroll
           for (int u = 0; u < 8; ++u) {
             const int it = it0 + u, r = it * 4 + (lane >> 4);
-            global_to_lds_16((const char*)(with + out_at + (int64_t)(r < live ? r : 0) * N + (((lane & 15) ^ (r & 15)) << 3)), wtile_addr + it * 1024);
+            global_to_lds_16((const char*)(pre + out_at + (int64_t)(r < live ? r : 0) * N + (((lane & 15) ^ (r & 15)) << 3)), wtile_addr + it * 1024);
           }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (i >= 2 * ni) break;
-        const int r = i * 16 + (lane & 15);
+      for (int c = 0; c < 4; ++c) {
+        if (c >= ni) break;
+        u32x2 w[2][8];
+        auto at = [&](int i, int j) __attribute__((always_inline)) {
+          const int r = c * 32 + i * 16 + (lane & 15);
+          return LDS_PTR(u32x2, wtile + r * 256 + (((2 * j + (kq >> 1)) ^ (r & 15)) << 4) + 8 * (kq & 1));
+        };
+        if (WITH) {                                                 // loads return in order; counting the stores in between waits for more at most
+          if (ni == 4 && c == 0) asm volatile("s_waitcnt vmcnt(24)" ::: "memory");
+          else if (ni == 4 && c == 1) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+          else if (ni == 4 && c == 2) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+          else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          auto* at = LDS_PTR(u32x2, wtile + r * 256 + (((2 * j + (kq >> 1)) ^ (r & 15)) << 4) + 8 * (kq & 1));
-          float v[4], w[4] = {0.f, 0.f, 0.f, 0.f};
-          if (with) {
-            const u32x2 q = *at;
-            w[0] = __uint_as_float(q.x << 16); w[1] = __uint_as_float(q.x & 0xffff0000u);
-            w[2] = __uint_as_float(q.y << 16); w[3] = __uint_as_float(q.y & 0xffff0000u);
-          }
+          for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            if (MODE == kNN) v[u] = rows_act<A_>(acc[i][j][u]) + (with ? w[u] : 0.f);
-            else v[u] = GRAD ? acc[i][j][u] * rows_act_grad<A_>(w[u]) : acc[i][j][u];
-          }
-          *at = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+            for (int j = 0; j < 8; ++j) w[i][j] = *at(i, j);
         }
+        auto store = [&](uint16_t* dst) __attribute__((always_inline)) {
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {
+            const int r = c * 32 + u * 4 + (lane >> 4);
+            const u32x4 q = *LDS_PTR(u32x4, wtile + r * 256 + ((lane & 15) << 4));
+            if (r < live) *reinterpret_cast<u32x4*>(dst + out_at + (int64_t)r * N + (((lane & 15) ^ (r & 15)) << 3)) = q;
+          }
+        };
+        if (DUAL) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const f32x4& a = acc[2 * c + i][j];
+              *at(i, j) = u32x2{pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3])};
+            }
+          store(pre_out);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const f32x4& a = acc[2 * c + i][j];
+            float v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const float x = WITH ? __uint_as_float(u & 1 ? w[i][j][u >> 1] & 0xffff0000u : w[i][j][u >> 1] << 16) : 0.f;
+              if (MODE == kNN) v[u] = WITH ? rows_act<ACT>(a[u]) + x : rows_act<ACT>(a[u]);
+              else v[u] = GRAD ? a[u] * rows_act_grad<ACT>(x) : a[u];
+            }
+            *at(i, j) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+          }
+        store(out);
       }
-      for (int it0 = 0; it0 < ni * 8; it0 += 8)
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const int r = (it0 + u) * 4 + (lane >> 4);
-          const u32x4 q = *LDS_PTR(u32x4, wtile + r * 256 + ((lane & 15) << 4));
-          if (r < live) *reinterpret_cast<u32x4*>(dst + out_at + (int64_t)r * N + (((lane & 15) ^ (r & 15)) << 3)) = q;
-        }
     };
-    if (DUAL) write_rows(std::true_type{}, pre_out, nullptr);
-    write_rows(std::false_type{}, out, pre);
+    if (MODE == kNT && GRAD) write_rows(std::true_type{});
+    else if (MODE == kNN && pre) write_rows(std::true_type{});
+    else write_rows(std::false_type{});
     return;
   }
   auto write_tile = [&](auto raw_tag, uint16_t* dst) {

@@ -21,6 +21,9 @@ template <int ACT> __device__ __forceinline__ float tile_act_grad(float v) { ret
 #include "ffn_large.h"
 
 namespace moe {
+
+#include "rows_thin.h"
+
 namespace {
 
 int64_t mean_rows(int64_t R, int64_t E) { return ceil_div(R, E); }
@@ -36,8 +39,19 @@ Tile rows_tile(int mode, int dtype, bool large_ok, int64_t E, int64_t rows, doub
 
 }  // namespace
 
-hipError_t launch_rows_product(const RowsProduct& p, hipStream_t s) {
+size_t rows_product_bytes(int dtype, int64_t R, int64_t K, int64_t N) {
+  if (dtype != MOE_BF16) return 0;
+  const ThinPlan plan = thin_plan(false, 1, R, K, N);
+  return plan.parts > 1 ? (size_t)plan.parts * R * N * 4 : 0;
+}
+
+hipError_t launch_rows_product(const RowsProduct& p, void* ws, hipStream_t s) {
   const bool dual = p.pre && p.act >= 0;
+  if (p.dtype == MOE_BF16) {
+    const ThinPlan plan = thin_plan(p.offsets != nullptr, p.E, p.R, p.K, p.N);
+    const TileArgs t = {p.A, p.W, p.bias, p.offsets, p.gather, p.gather_rows, p.R, p.K, (int)p.N, (int)p.E, 0, 0, 0, p.out, nullptr, p.residual, p.pre, p.act, 0};
+    if (plan.ri > 0) return launch_thin(t, plan, (float*)ws, s);
+  }
   const Tile tile = rows_tile(kNN, p.dtype, large_takes(p.E, p.K, p.N, p.gather ? p.gather_rows : 0, p.K), p.E, p.R, (double)mean_rows(p.R, p.E), p.K, p.N, p.gather != nullptr);
   if (tile != Tile::k256) {
     const TileArgs t = {p.A, p.W, p.bias, p.offsets, p.gather, p.gather_rows, p.R, p.K, (int)p.N, (int)p.E, 0, 0, 0, p.out, nullptr, p.residual, p.pre, p.act, 0};

@@ -13,7 +13,9 @@ struct RowsProduct {
   int act, dtype;
   void *out, *pre;
 };
-hipError_t launch_rows_product(const RowsProduct& p, hipStream_t s);
+// ws: rows_product_bytes where there are no offsets, else none
+size_t rows_product_bytes(int dtype, int64_t R, int64_t K, int64_t N);
+hipError_t launch_rows_product(const RowsProduct& p, void* ws, hipStream_t s);
 // dx[r] = d[r] W[e]^T, times act'(x_pre[r]) if that is given; d [R,N], W [E,K,N], dx [R,K]
 hipError_t launch_rows_product_nt(const void* d, const void* W, const void* x_pre, int x_act, int dtype, const int32_t* offsets, int64_t R, int64_t E, int64_t K,
                                   int64_t N, void* dx, hipStream_t s);

@@ -10,26 +10,30 @@ namespace {
 // fp32 evaluation).  One exponential, no division.
 constexpr float kPhi[9] = {1.151095026e+00f, 4.586445080e-01f, 5.404893616e-02f, -8.699391121e-03f, 1.027744177e-03f, -8.451740843e-05f, 4.530642880e-06f, -1.413703882e-07f, 1.939663995e-09f};
 constexpr float kPhiEnd = 13.2f;
-__device__ __forceinline__ float normal_cdf(float v) {
-  const float y = fminf(fabsf(v), kPhiEnd);
+__device__ __forceinline__ float normal_tail(float y) {             // Phi(-y), 0 <= y <= kPhiEnd
   float p = kPhi[8];
 #pragma unroll
   for (int i = 7; i >= 0; --i) p = fmaf(p, y, kPhi[i]);
-  const float e = 0.5f * __builtin_amdgcn_exp2f(-(p * y));
-  return v < 0.f ? e : 1.f - e;
+  return __builtin_amdgcn_exp2f(fmaf(-p, y, -1.0f));
 }
 
 // bf16 results.  ReLU keeps a NaN; SiLU by the hardware's exponential and reciprocal, 1e-6.
 template <int ACT> __device__ __forceinline__ float rows_act(float v) {
   if (ACT == MOE_ACT_RELU) return v < 0.f ? 0.f : v;
-  if (ACT == MOE_ACT_GELU) return v * normal_cdf(v);
+  if (ACT == MOE_ACT_GELU) {                                        // v Phi(v) = max(v, 0) - |v| Phi(-|v|); a NaN stays one
+    const float y = fminf(fabsf(v), kPhiEnd);
+    return fmaf(-y, normal_tail(y), v < 0.f ? 0.f : v);
+  }
   if (ACT == MOE_ACT_SILU) return v * __builtin_amdgcn_rcpf(1.0f + __expf(-v));
   return v;
 }
 // The derivative: phi(v) = exp2(-v^2 / (2 ln 2)) / sqrt(2 pi); 7e-6 for GeLU.
 template <int ACT> __device__ __forceinline__ float rows_act_grad(float v) {
   if (ACT == MOE_ACT_RELU) return v > 0.f ? 1.f : 0.f;
-  if (ACT == MOE_ACT_GELU) return fmaf(v, __builtin_amdgcn_exp2f(-0.72134752f * v * v) * 0.39894228f, normal_cdf(v));
+  if (ACT == MOE_ACT_GELU) {
+    const float t = normal_tail(fminf(fabsf(v), kPhiEnd));
+    return fmaf(v, __builtin_amdgcn_exp2f(-0.72134752f * v * v) * 0.39894228f, v < 0.f ? t : 1.f - t);
+  }
   if (ACT == MOE_ACT_SILU) {
     const float sg = __builtin_amdgcn_rcpf(1.0f + __expf(-v));
     return sg * fmaf(v, 1.f - sg, 1.f);

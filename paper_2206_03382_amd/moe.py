@@ -88,7 +88,8 @@ SIGNATURES = {
     "moe_ragged_matmul": (_i32, [_vp, _vp, _i64, _vp, _vp, _i32, _i32, _vp, _i64, _i64, _i64, _i64, _vp, _vp, _vp]),
     "moe_ragged_matmul_backward_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64, _i32, _i32]),
     "moe_ragged_matmul_backward": (_i32, [_vp, _vp, _vp, _i64, _vp, _vp, _i32, _vp, _i32, _i32, _vp, _i64, _i64, _i64, _i64, _vp, _sz, _vp, _vp, _vp, _vp]),
-    "moe_linear": (_i32, [_vp, _vp, _vp, _i32, _vp, _i32, _i64, _i64, _i64, _vp, _vp, _vp]),
+    "moe_linear_workspace_bytes": (_sz, [_i64, _i64, _i64, _i32]),
+    "moe_linear": (_i32, [_vp, _vp, _vp, _i32, _vp, _i32, _i64, _i64, _i64, _vp, _sz, _vp, _vp, _vp]),
     "moe_linear_backward_workspace_bytes": (_sz, [_i64, _i64, _i64, _i32, _i32]),
     "moe_linear_backward": (_i32, [_vp, _vp, _vp, _vp, _i32, _i32, _i64, _i64, _i64, _vp, _sz, _vp, _vp, _vp, _vp]),
     "moe_dropout": (_i32, [_vp, _vp, _dbl, _vp, _i32, _i64, _vp, _vp]),
@@ -977,7 +978,9 @@ def linear(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None
         _check_out(out, (T, N), W.dtype)
     pre = torch.empty_like(out) if keep_pre else None
     _here(x, W, bias, residual, out)
-    _check(lib().moe_linear(_p(x), _p(W), _p(bias), act, _p(residual), code, T, K, N, _p(pre), _p(out), _stream()), "moe_linear")
+    nbytes = lib().moe_linear_workspace_bytes(T, K, N, code)
+    ws = torch.empty((nbytes,), dtype=torch.uint8, device=W.device) if nbytes else None
+    _check(lib().moe_linear(_p(x), _p(W), _p(bias), act, _p(residual), code, T, K, N, _p(ws), nbytes, _p(pre), _p(out), _stream()), "moe_linear")
     return (out, pre) if keep_pre else out
 
 

@@ -50,9 +50,13 @@ def test_product_refusals(moe):
 
 def test_linear_refusals(moe):
     L = moe.lib()
-    lin = lambda x=FAKE, W=FAKE, b=None, act=-1, res=None, dt=1, T=1, K=64, N=64, pre=None, out=FAKE: L.moe_linear(x, W, b, act, res, dt, T, K, N, pre, out, None)   # noqa: E731
+    lin = lambda x=FAKE, W=FAKE, b=None, act=-1, res=None, dt=1, T=1, K=64, N=64, ws=None, n=0, pre=None, out=FAKE: L.moe_linear(   # noqa: E731
+        x, W, b, act, res, dt, T, K, N, ws, n, pre, out, None)
     assert lin(x=None) == lin(W=None) == lin(out=None) == lin(act=4) == lin(dt=-1) == lin(T=0) == lin(K=0) == moe.INVALID_ARG
     assert lin(K=4) == lin(N=4) == lin(x=FAKE + 8) == lin(res=FAKE + 4) == lin(b=FAKE + 8) == lin(K=1 << 20, N=1 << 12) == moe.UNSUPPORTED
+    need = L.moe_linear_workspace_bytes(1, 4096, 64, 1)
+    assert need > 0 and L.moe_linear_workspace_bytes(1, 64, 64, 1) == L.moe_linear_workspace_bytes(1, 4096, 64, 0) == L.moe_linear_workspace_bytes(1, 4096, 60, 1) == 0
+    assert lin(K=4096) == moe.INVALID_ARG and lin(K=4096, ws=FAKE, n=need - 1) == moe.WORKSPACE_TOO_SMALL and lin(K=4096, ws=FAKE + 128, n=need) == moe.UNSUPPORTED
     back = lambda dy=FAKE, x=FAKE, W=FAKE, pre=None, act=-1, T=4, K=64, ws=FAKE, n=1 << 40, dx=FAKE, dW=FAKE, db=FAKE: L.moe_linear_backward(   # noqa: E731
         dy, x, W, pre, act, 1, T, K, 64, ws, n, dx, dW, db, None)
     assert back(dy=None) == back(x=None) == back(W=None) == back(ws=None) == back(act=0) == back(pre=FAKE) == back(dx=None, dW=None, db=None) == back(T=0) == moe.INVALID_ARG
