@@ -525,7 +525,9 @@ static hipError_t launch_small(int dtype, Tile tile, const TileArgs& p, int64_t 
   if constexpr (MODE != kTN) {
     if (dtype == MOE_F32 && fp32_split(p.E, p.C, p.K, p.N)) return launch_tile<float, MODE, kSplitTile, kSplitTile, 2, false, kSplitParts, ROWS>(p, total, s);
   }
-  if (dtype == MOE_F32) return launch_tile<float, MODE, 64, 64, 2, false, 1, ROWS>(p, total, s);
+  if constexpr (!ROWS) {                                            // ROWS: rows_fp32.h
+    if (dtype == MOE_F32) return launch_tile<float, MODE, 64, 64, 2>(p, total, s);
+  }
   if constexpr (MODE != kTN) {
     switch (tile) {
       case Tile::k64: return launch_tile<uint16_t, MODE, 64, 64, 3, false, 1, ROWS>(p, total, s);

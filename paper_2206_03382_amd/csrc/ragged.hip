@@ -23,6 +23,7 @@ template <int ACT> __device__ __forceinline__ float tile_act_grad(float v) { ret
 namespace moe {
 
 #include "rows_thin.h"
+#include "rows_fp32.h"
 
 namespace {
 
@@ -31,6 +32,12 @@ int64_t mean_rows(int64_t R, int64_t E) { return ceil_div(R, E); }
 // Whether the large tile takes a product of K x N weights; gather_rows > 0: of rows of so many elements that 32-bit offsets reach.
 bool large_takes(int64_t E, int64_t K, int64_t N, int64_t gather_rows, int64_t gather_width) {
   return K % kLargeK == 0 && N % kLargeTile == 0 && E <= kMaxExperts && gather_rows * gather_width * 2 < ((int64_t)1 << 32);
+}
+
+// The products on tiles below the large one.  fp32 of few tiles: the reduction of 32 x 32 cut among a block's waves (fp32_split).
+template <int MODE> hipError_t launch_small_rows(int dtype, Tile tile, const TileArgs& t, int64_t total, hipStream_t s) {
+  if (dtype == MOE_F32 && (MODE == kTN || !fp32_split(t.E, t.C, t.K, t.N))) return launch_rows_fp32<MODE>(t, total, s);
+  return launch_small<MODE, true>(dtype, tile, t, total, s);
 }
 
 Tile rows_tile(int mode, int dtype, bool large_ok, int64_t E, int64_t rows, double mean, int64_t K, int64_t N, bool gathered) {
@@ -55,7 +62,7 @@ hipError_t launch_rows_product(const RowsProduct& p, void* ws, hipStream_t s) {
   const Tile tile = rows_tile(kNN, p.dtype, large_takes(p.E, p.K, p.N, p.gather ? p.gather_rows : 0, p.K), p.E, p.R, (double)mean_rows(p.R, p.E), p.K, p.N, p.gather != nullptr);
   if (tile != Tile::k256) {
     const TileArgs t = {p.A, p.W, p.bias, p.offsets, p.gather, p.gather_rows, p.R, p.K, (int)p.N, (int)p.E, 0, 0, 0, p.out, nullptr, p.residual, p.pre, p.act, 0};
-    return launch_small<kNN, true>(p.dtype, tile, t, p.R, s);
+    return launch_small_rows<kNN>(p.dtype, tile, t, p.R, s);
   }
   const int MT = (int)ceil_div(p.R, BM), NT = (int)(p.N / BN);
   const int64_t blocks = tile_grid(NT, live_row_tiles(p.E, p.R, p.R, BM), true, false);
@@ -88,7 +95,7 @@ hipError_t launch_rows_product_nt(const void* d, const void* W, const void* x_pr
   const Tile tile = rows_tile(kNT, dtype, large_takes(E, N, K, 0, 0), E, R, (double)mean_rows(R, E), N, K, false);
   if (tile != Tile::k256) {
     const TileArgs t = {d, W, nullptr, offsets, nullptr, 0, R, N, (int)K, (int)E, 0, 0, 0, dx, nullptr, x_pre, nullptr, x_pre ? x_act : -1, 0};
-    return launch_small<kNT, true>(dtype, tile, t, R, s);
+    return launch_small_rows<kNT>(dtype, tile, t, R, s);
   }
   const int MT = (int)ceil_div(R, BM), NT = (int)(K / BN);
   const int64_t blocks = tile_grid(NT, live_row_tiles(E, R, R, BM), true, false);
@@ -127,7 +134,7 @@ hipError_t launch_rows_weight_grad(const void* A, const int32_t* gather, int64_t
   const Tile tile = weight_grad_tile(dtype, R, E, K, N, gather != nullptr, gather_rows);
   if (tile != Tile::k256) {
     const TileArgs t = {A, d, nullptr, nullptr, gather, gather_rows, K, R, (int)N, (int)E, 0, 0, 0, dW, offsets, nullptr, nullptr, -1, 0};
-    return launch_small<kTN, true>(dtype, tile, t, E * K, s);
+    return launch_small_rows<kTN>(dtype, tile, t, E * K, s);
   }
   uint16_t* a_tail = (uint16_t*)ws;
   uint16_t* b_tail = a_tail + grouped_gemm_tn_tail_bytes(E, K) / 2;

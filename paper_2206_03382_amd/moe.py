@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Tuple, Dict, NamedTuple, Optional, Sequence
+from typing import Tuple, Dict, List, NamedTuple, Optional, Sequence
 
 import torch
 
@@ -574,7 +574,7 @@ def _check_out(t: Optional[torch.Tensor], shape, dtype: torch.dtype) -> None:
 
 
 def _check_int32(t: Optional[torch.Tensor], *shape: int) -> None:
-    if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != shape):
+    if t is not None and (t.dtype != torch.int32 or t.shape != shape):
         raise ValueError(f"counts and indices must be int32 {list(shape)}")
 
 
@@ -862,12 +862,18 @@ class NormMoELayer8:
 
 # ---- experts' rows one behind the other, dense projections, dropout ------------------------------------------------------
 
-def _here(*tensors: Optional[torch.Tensor]) -> None:
-    """The library launches on the current device's stream: all tensors have to be there."""
+def _here(*tensors: Optional[torch.Tensor]) -> List[Optional[int]]:
+    """Their addresses.  The library launches on the current device's stream: all tensors have to be there, and contiguous."""
     device = torch._C._cuda_getDevice()
+    at = []
     for t in tensors:
-        if t is not None and t.get_device() != device:
-            raise ValueError("tensors must be on the current device")
+        if t is None:
+            at.append(None)
+        elif t.get_device() != device or not t.is_contiguous():
+            raise ValueError("tensors must be contiguous and on the current device")
+        else:
+            at.append(t.data_ptr())
+    return at
 
 
 def _as_stored(t: torch.Tensor, like: torch.Tensor, what: str, *shape: int) -> None:
@@ -900,18 +906,16 @@ def ragged_rows(idx: torch.Tensor, loc: torch.Tensor, counts: torch.Tensor, C: i
     E = counts.shape[0]
     _check_int32(loc, T, k)
     _check_int32(counts, E)
-    _here(idx, loc, counts)
-    dev = idx.device
-    r = RaggedRows(torch.empty((E + 1,), dtype=torch.int32, device=dev), torch.empty((T * k,), dtype=torch.int32, device=dev),
-                   torch.empty((T, k), dtype=torch.int32, device=dev))
-    _check(lib().moe_ragged_rows(_p(idx), _p(loc), _p(counts), T, E, k, C, _p(r.offsets), _p(r.row_src), _p(r.row_of), _stream()), "moe_ragged_rows")
+    r = RaggedRows(counts.new_empty((E + 1,)), counts.new_empty((T * k,)), torch.empty_like(loc))
+    at = _here(idx, loc, counts, *r)
+    _check(lib().moe_ragged_rows(*at[:3], T, E, k, C, *at[3:], _stream()), "moe_ragged_rows")
     return r
 
 
 def ragged_matmul(A: torch.Tensor, W: torch.Tensor, offsets: torch.Tensor, bias: Optional[torch.Tensor] = None, act: int = ACT_NONE,
                   gather: Optional[torch.Tensor] = None, keep_pre: bool = False, out: Optional[torch.Tensor] = None):
     """out[r] = act(A[r] W[e] + bias[e]) for the rows r of expert e (offsets [E+1]): A [R,K], or [tokens,K] with gather [R] (ragged_rows' row_src), W [E,K,N].  Rows behind the
-    last expert's hold whatever the memory did.  keep_pre: (out, the values before the activation), which ragged_matmul_backward takes."""
+    last expert's hold whatever the memory did.  keep_pre: (out, the values before the activation), which ragged_matmul_backward takes (None for ACT_NONE, which needs none)."""
     E, K, N = W.shape
     _check_gather(gather)
     rows = A.shape[0]
@@ -922,12 +926,12 @@ def ragged_matmul(A: torch.Tensor, W: torch.Tensor, offsets: torch.Tensor, bias:
     if bias is not None:
         _as_stored(bias, W, "bias", E, N)
     if out is None:
-        out = torch.empty((R, N), dtype=W.dtype, device=W.device)
+        out = A.new_empty((R, N))
     else:
         _check_out(out, (R, N), W.dtype)
-    pre = torch.empty_like(out) if keep_pre else None
-    _here(A, W, offsets, bias, gather, out)
-    _check(lib().moe_ragged_matmul(_p(A), _p(gather), rows, _p(W), _p(bias), act, code, _p(offsets), R, E, K, N, _p(pre), _p(out), _stream()), "moe_ragged_matmul")
+    pre = torch.empty_like(out) if keep_pre and act != ACT_NONE else None
+    A_, gather_, W_, bias_, offsets_, pre_, out_ = _here(A, gather, W, bias, offsets, pre, out)
+    _check(lib().moe_ragged_matmul(A_, gather_, rows, W_, bias_, act, code, offsets_, R, E, K, N, pre_, out_, _stream()), "moe_ragged_matmul")
     return (out, pre) if keep_pre else out
 
 
@@ -949,22 +953,21 @@ def ragged_matmul_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, o
         _as_stored(pre, W, "pre", R, N)
     if x_pre is not None:
         _as_stored(x_pre, W, "x_pre", R, K)
-    _here(dy, x, W, offsets, pre, gather, x_pre)
-    nbytes = int(lib().moe_ragged_matmul_backward_workspace_bytes(R, E, K, N, act, code))
+    nbytes = lib().moe_ragged_matmul_backward_workspace_bytes(R, E, K, N, act, code)
     if nbytes == 0:
         raise MoEError(UNSUPPORTED, "moe_ragged_matmul_backward_workspace_bytes")
-    dev = W.device
-    ws = torch.empty((nbytes,), dtype=torch.uint8, device=dev)
-    g = dict(dx=torch.empty((R, K), dtype=W.dtype, device=dev) if want_dx else None, dW=torch.empty_like(W) if want_dW else None,
-             db=torch.empty((E, N), dtype=W.dtype, device=dev) if want_db else None)
-    _check(lib().moe_ragged_matmul_backward(_p(dy), _p(x), _p(gather), rows, _p(W), _p(pre), act, _p(x_pre), x_act, code, _p(offsets), R, E, K, N, _p(ws), nbytes,
-                                            _p(g["dx"]), _p(g["dW"]), _p(g["db"]), _stream()), "moe_ragged_matmul_backward")
+    ws = torch.empty((nbytes,), dtype=torch.uint8, device=W.device)
+    g = dict(dx=x.new_empty((R, K)) if want_dx else None, dW=torch.empty_like(W) if want_dW else None, db=W.new_empty((E, N)) if want_db else None)
+    dy_, x_, gather_, W_, pre_, x_pre_, offsets_, ws_, *out = _here(dy, x, gather, W, pre, x_pre, offsets, ws, *g.values())
+    _check(lib().moe_ragged_matmul_backward(dy_, x_, gather_, rows, W_, pre_, act, x_pre_, x_act, code, offsets_, R, E, K, N, ws_, nbytes, *out, _stream()),
+           "moe_ragged_matmul_backward")
     return g
 
 
 def linear(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None, act: int = ACT_NONE, residual: Optional[torch.Tensor] = None, keep_pre: bool = False,
            out: Optional[torch.Tensor] = None):
-    """out = act(x W + bias) + residual: x [T,K], W [K,N].  keep_pre: (out, the values before the activation), which linear_backward takes.  out may be residual."""
+    """out = act(x W + bias) + residual: x [T,K], W [K,N].  keep_pre: (out, the values before the activation), which linear_backward takes (None for ACT_NONE, which needs none).  out
+    may be residual."""
     T, (K, N) = x.shape[0], W.shape
     code = _dtype_code(W)
     _as_stored(x, W, "x", T, K)
@@ -973,14 +976,14 @@ def linear(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None
     if residual is not None:
         _as_stored(residual, W, "residual", T, N)
     if out is None:
-        out = torch.empty((T, N), dtype=W.dtype, device=W.device)
+        out = x.new_empty((T, N)) if residual is None else torch.empty_like(residual)
     else:
         _check_out(out, (T, N), W.dtype)
-    pre = torch.empty_like(out) if keep_pre else None
-    _here(x, W, bias, residual, out)
+    pre = torch.empty_like(out) if keep_pre and act != ACT_NONE else None
     nbytes = lib().moe_linear_workspace_bytes(T, K, N, code)
     ws = torch.empty((nbytes,), dtype=torch.uint8, device=W.device) if nbytes else None
-    _check(lib().moe_linear(_p(x), _p(W), _p(bias), act, _p(residual), code, T, K, N, _p(ws), nbytes, _p(pre), _p(out), _stream()), "moe_linear")
+    x_, W_, bias_, residual_, ws_, pre_, out_ = _here(x, W, bias, residual, ws, pre, out)
+    _check(lib().moe_linear(x_, W_, bias_, act, residual_, code, T, K, N, ws_, nbytes, pre_, out_, _stream()), "moe_linear")
     return (out, pre) if keep_pre else out
 
 
@@ -993,16 +996,13 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, act: int
     _as_stored(dy, W, "dy", T, N)
     if pre is not None:
         _as_stored(pre, W, "pre", T, N)
-    _here(dy, x, W, pre)
-    nbytes = int(lib().moe_linear_backward_workspace_bytes(T, K, N, act, code))
+    nbytes = lib().moe_linear_backward_workspace_bytes(T, K, N, act, code)
     if nbytes == 0:
         raise MoEError(UNSUPPORTED, "moe_linear_backward_workspace_bytes")
-    dev = W.device
-    ws = torch.empty((nbytes,), dtype=torch.uint8, device=dev)
-    g = dict(dx=torch.empty((T, K), dtype=W.dtype, device=dev) if want_dx else None, dW=torch.empty_like(W) if want_dW else None,
-             db=torch.empty((N,), dtype=W.dtype, device=dev) if want_db else None)
-    _check(lib().moe_linear_backward(_p(dy), _p(x), _p(W), _p(pre), act, code, T, K, N, _p(ws), nbytes, _p(g["dx"]), _p(g["dW"]), _p(g["db"]), _stream()),
-           "moe_linear_backward")
+    ws = torch.empty((nbytes,), dtype=torch.uint8, device=W.device)
+    g = dict(dx=torch.empty_like(x) if want_dx else None, dW=torch.empty_like(W) if want_dW else None, db=W.new_empty((N,)) if want_db else None)
+    dy_, x_, W_, pre_, ws_, *out = _here(dy, x, W, pre, ws, *g.values())
+    _check(lib().moe_linear_backward(dy_, x_, W_, pre_, act, code, T, K, N, ws_, nbytes, *out, _stream()), "moe_linear_backward")
     return g
 
 
@@ -1013,17 +1013,20 @@ def _check_seed(seed: torch.Tensor) -> None:
 
 def dropout(x: torch.Tensor, p: float, seed: torch.Tensor, residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """residual + dropout(x) with probability p: the mask comes from the numbers in seed (int64 [2] on the device: seed and offset) and an element's place, and is never stored.
-    dropout(dy, p, seed) is the gradient of x.  out may be x or residual."""
+    dropout(dy, p, seed) is the gradient of x.  out may be x or residual.  With p = 0, no residual and no out the result is x itself."""
     code = _dtype_code(x)
     _check_seed(seed)
     if residual is not None and (residual.shape != x.shape or residual.dtype != x.dtype):
         raise ValueError("residual must have x's shape and type")
     if out is None:
+        if p == 0 and residual is None:
+            _here(x, seed)
+            return x
         out = torch.empty_like(x)
     else:
         _check_out(out, x.shape, x.dtype)
-    _here(x, seed, residual, out)
-    _check(lib().moe_dropout(_p(x), _p(residual), p, _p(seed), code, x.numel(), _p(out), _stream()), "moe_dropout")
+    x_, residual_, seed_, out_ = _here(x, residual, seed, out)
+    _check(lib().moe_dropout(x_, residual_, p, seed_, code, x.numel(), out_, _stream()), "moe_dropout")
     return out
 
 
@@ -1048,11 +1051,11 @@ def ragged_combine(Y: torch.Tensor, row_of: torch.Tensor, gate_w: Optional[torch
     if residual is not None:
         _as_stored(residual, Y, "residual", T, M)
     if out is None:
-        out = torch.empty((T, M), dtype=Y.dtype, device=Y.device)
+        out = Y.new_empty((T, M)) if residual is None else torch.empty_like(residual)
     else:
         _check_out(out, (T, M), Y.dtype)
-    _here(Y, row_of, gate_w, residual, seed, out)
-    _check(lib().moe_ragged_combine(_p(Y), R, _p(row_of), _p(gate_w), _p(residual), p, _p(seed), code, T, M, k, _p(out), _stream()), "moe_ragged_combine")
+    Y_, row_of_, gate_w_, residual_, seed_, out_ = _here(Y, row_of, gate_w, residual, seed, out)
+    _check(lib().moe_ragged_combine(Y_, R, row_of_, gate_w_, residual_, p, seed_, code, T, M, k, out_, _stream()), "moe_ragged_combine")
     return out
 
 
@@ -1068,7 +1071,6 @@ def ragged_combine_backward(d_out: torch.Tensor, Y: torch.Tensor, row_of: torch.
     else:
         _check_out(dY, Y.shape, Y.dtype)
     dgate_w = torch.empty((T, k), dtype=torch.float32, device=Y.device)
-    _here(d_out, Y, row_of, gate_w, seed, dY)
-    _check(lib().moe_ragged_combine_backward(_p(d_out), _p(Y), R, _p(row_of), _p(gate_w), p, _p(seed), code, T, M, k, _p(dY), _p(dgate_w), _stream()),
-           "moe_ragged_combine_backward")
+    d_out_, Y_, row_of_, gate_w_, seed_, dY_, dgate_w_ = _here(d_out, Y, row_of, gate_w, seed, dY, dgate_w)
+    _check(lib().moe_ragged_combine_backward(d_out_, Y_, R, row_of_, gate_w_, p, seed_, code, T, M, k, dY_, dgate_w_, _stream()), "moe_ragged_combine_backward")
     return dY, dgate_w

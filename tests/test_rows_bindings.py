@@ -26,9 +26,8 @@ class Recorder:
 def library(monkeypatch):
     r = Recorder()
     monkeypatch.setattr(moe, "lib", lambda: r)
-    monkeypatch.setattr(moe, "_p", lambda t: None if t is None else t.data_ptr())
     monkeypatch.setattr(moe, "_stream", lambda: 0)
-    monkeypatch.setattr(moe, "_here", lambda *t: None)
+    monkeypatch.setattr(moe, "_here", lambda *t: [None if x is None else x.data_ptr() for x in t])
     return r
 
 
@@ -59,6 +58,7 @@ def test_ragged_matmul(library):
     A, W, off = z(10, 16), z(3, 16, 24), i32(4)
     out, pre = moe.ragged_matmul(A, W, off, z(3, 24), moe.ACT_SILU, gather=i32(30), keep_pre=True)
     assert out.shape == pre.shape == (30, 24) and library.calls["moe_ragged_matmul"][8:12] == (30, 3, 16, 24) and library.calls["moe_ragged_matmul"][2] == 10
+    assert moe.ragged_matmul(A, W, off, keep_pre=True)[1] is None and library.calls["moe_ragged_matmul"][12] is None
     mine = z(10, 24)
     assert moe.ragged_matmul(A, W, off, out=mine) is mine
     for bad in (dict(A=z(10, 24)), dict(A=z(10, 16, dtype=torch.float32)), dict(offsets=i32(3)), dict(offsets=z(4)), dict(bias=z(24)), dict(bias=z(3, 24, dtype=torch.float32)),
@@ -84,7 +84,8 @@ def test_ragged_matmul_backward(library):
 def test_linear(library):
     x, W, res = z(5, 16), z(16, 24), z(5, 24)
     assert moe.linear(x, W, z(24), moe.ACT_RELU, residual=res, out=res) is res
-    assert moe.linear(x, W, keep_pre=True)[1].shape == (5, 24)
+    assert moe.linear(x, W, None, moe.ACT_GELU, keep_pre=True)[1].shape == (5, 24) and library.calls["moe_linear"][10] == 4096
+    assert moe.linear(x, W, keep_pre=True)[1] is None and library.calls["moe_linear"][11] is None
     for bad in (dict(x=z(5, 24)), dict(bias=z(16)), dict(residual=z(4, 24)), dict(residual=z(5, 24, dtype=torch.float32)), dict(out=z(5, 16))):
         with pytest.raises(ValueError):
             moe.linear(**{**dict(x=x, W=W), **bad})
@@ -98,6 +99,9 @@ def test_linear(library):
 def test_dropout_and_combine(library):
     x, seed = z(4, 16), torch.zeros(2, dtype=torch.int64)
     assert moe.dropout(x, 0.1, seed, residual=x, out=x) is x and library.calls["moe_dropout"][5] == 64
+    library.calls.clear()
+    assert moe.dropout(x, 0.0, seed) is x and not library.calls
+    assert moe.dropout(x, 0.0, seed, residual=x) is not x and library.calls.pop("moe_dropout") and moe.dropout(x, 0.0, seed, out=z(4, 16)) is not x and library.calls
     for bad in (dict(seed=seed[:1]), dict(seed=seed.int()), dict(residual=z(4, 8)), dict(residual=z(4, 16, dtype=torch.float32)), dict(out=z(8, 8))):
         with pytest.raises(ValueError):
             moe.dropout(**{**dict(x=x, p=0.1, seed=seed), **bad})

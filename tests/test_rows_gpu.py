@@ -111,7 +111,9 @@ def test_ragged_product_and_gradients(moe, R, E, K, N, kind, behind, dtype):
     mark = 77.0
     out = torch.full((R + behind, N), mark, dtype=dtype, device="cuda")
     got, pre = moe.ragged_matmul(A, W, off, b, ACT[act], gather=gather, keep_pre=True, out=out)
-    assert got is out and (out[R:] == mark).all()
+    assert got is out and (out[R:] == mark).all() and (pre is None) == (act == "none")
+    if pre is None:                                                 # the values before no activation
+        pre = out.clone()
     v, S = O.product(A64, gather64, W64, b64, offsets)
     y, _ = O.act(v, act)
     e = sum_error(dtype, K) * S
@@ -192,7 +194,9 @@ def test_linear_and_gradients(moe, T, K, N, dtype):
     e = sum_error(dtype, K) * S
     bound = 1.13 * e + act_error(dtype, act, v, y) + 2.0 ** -23 * np.abs(res64)
     got, pre = moe.linear(x, W, b, ACT[act], residual=res, keep_pre=True)
-    assert_within(pre, v, e + HALF[dtype] * np.abs(v), "pre")
+    assert (pre is None) == (act == "none")
+    if pre is not None:
+        assert_within(pre, v, e + HALF[dtype] * np.abs(v), "pre")
     assert_within(got, y + res64, bound + HALF[dtype] * np.abs(y + res64), "out")
     assert torch.equal(moe.linear(x, W, b, ACT[act], residual=res), got)
     assert_within(moe.linear(x, W, b, ACT[act]), y, bound + HALF[dtype] * np.abs(y), "without a residual")
@@ -202,7 +206,7 @@ def test_linear_and_gradients(moe, T, K, N, dtype):
     assert moe.linear(x, W, b, ACT[act], residual=own, out=own) is own and torch.equal(own, got)
 
     dy, dy64 = draw(rng, (T, N), dtype)
-    p64 = up(pre)
+    p64 = v if pre is None else up(pre)
     _, slope = O.act(p64, act)
     d = dy64 * slope
     dx, dW, db = O.product_backward(d, x64, None, W64[None], offsets)
