@@ -1074,3 +1074,77 @@ def ragged_combine_backward(d_out: torch.Tensor, Y: torch.Tensor, row_of: torch.
     d_out_, Y_, row_of_, gate_w_, seed_, dY_, dgate_w_ = _here(d_out, Y, row_of, gate_w, seed, dY, dgate_w)
     _check(lib().moe_ragged_combine_backward(d_out_, Y_, R, row_of_, gate_w_, p, seed_, code, T, M, k, dY_, dgate_w_, _stream()), "moe_ragged_combine_backward")
     return dY, dgate_w
+
+
+class DroplessKept(NamedTuple):
+    """What DroplessLayer.backward takes of a forward pass."""
+    x: torch.Tensor
+    routing: Dict[str, torch.Tensor]
+    rows: RaggedRows
+    pre: Optional[torch.Tensor]
+    hidden: torch.Tensor
+    Y: torch.Tensor
+    shared_pre: Optional[torch.Tensor]
+    shared_hidden: Optional[torch.Tensor]
+    dropout: Optional[Tuple[float, torch.Tensor]]
+
+
+class DroplessLayer:
+    """An MoE layer without a capacity, whose experts hold the rows that their tokens are and no others:
+    out = residual + shared(x) + dropout(sum_j gate_w[t,j] expert_j(x)), expert(x) = act(x W1[e] + b1[e]) W2[e] + b2[e].
+    shared (Ws1 [M,Hs], bs1, Ws2 [Hs,M], bs2; biases may be None): a dense expert for all tokens, of the same activation.  Any number of tokens a call; everything can be captured."""
+
+    def __init__(self, Wg: torch.Tensor, gate_bias: Optional[torch.Tensor], W1: torch.Tensor, b1: Optional[torch.Tensor], W2: torch.Tensor, b2: Optional[torch.Tensor], k: int,
+                 normalize: int, act: int, shared: Optional[Tuple[torch.Tensor, Optional[torch.Tensor], torch.Tensor, Optional[torch.Tensor]]] = None):
+        self.E, self.M, self.H = W1.shape
+        code = _dtype_code(W1)
+        _check_gate(Wg, gate_bias, self.M, self.E)
+        _check_storage(code, Wg, W2)
+        if W2.shape != (self.E, self.H, self.M):
+            raise ValueError("W2 must be [E,H,M]")
+        _check_biases(self.E, self.M, self.H, b1, b2, code)
+        if shared is not None:
+            Ws1, bs1, Ws2, bs2 = shared
+            _check_storage(code, Ws1, bs1, Ws2, bs2)
+            if Ws1.dim() != 2 or Ws1.shape[0] != self.M or Ws2.shape != (Ws1.shape[1], self.M):
+                raise ValueError("shared must be (Ws1 [M,Hs], bs1, Ws2 [Hs,M], bs2)")
+        self.Wg, self.gate_bias, self.W1, self.b1, self.W2, self.b2, self.shared = Wg, gate_bias, W1, b1, W2, b2, shared
+        self.k, self.normalize, self.act, self.code = k, int(normalize), int(act), code
+
+    def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None, dropout: Optional[Tuple[float, torch.Tensor]] = None, keep: bool = False):
+        """out [T,M]; keep: (out, what backward takes).  dropout: (p, seed) as in dropout()."""
+        if x.dim() != 2 or x.shape[1] != self.M or _dtype_code(x) != self.code:
+            raise ValueError(f"x must be [T,{self.M}] in the weights' type")
+        r = gate_route(x, self.Wg, self.gate_bias, self.k, 1, self.normalize)          # its slots are not used: one to an expert
+        rows = ragged_rows(r["idx"], r["loc"], r["counts"])
+        hidden = ragged_matmul(x, self.W1, rows.offsets, self.b1, self.act, gather=rows.row_src, keep_pre=keep)
+        hidden, pre = hidden if keep else (hidden, None)
+        Y = ragged_matmul(hidden, self.W2, rows.offsets, self.b2)
+        base, shared_hidden, shared_pre = residual, None, None
+        if self.shared is not None:
+            Ws1, bs1, Ws2, bs2 = self.shared
+            shared_hidden = linear(x, Ws1, bs1, self.act, keep_pre=keep)
+            shared_hidden, shared_pre = shared_hidden if keep else (shared_hidden, None)
+            base = linear(shared_hidden, Ws2, bs2, residual=residual)
+        out = ragged_combine(Y, rows.row_of, r["gate_w"], residual=base, dropout=dropout)
+        return (out, DroplessKept(x, r, rows, pre, hidden, Y, shared_pre, shared_hidden, dropout)) if keep else out
+
+    def backward(self, kept: DroplessKept, d_out: torch.Tensor) -> Dict[str, Optional[torch.Tensor]]:
+        """dx, dWg, dgate_bias, dW1, db1, dW2, db2 and, with a shared expert, dWs1, dbs1, dWs2, dbs2; the residual's gradient is d_out."""
+        r, rows = kept.routing, kept.rows
+        g = {}
+        base = None
+        if self.shared is not None:
+            Ws1, _, Ws2, _ = self.shared
+            s2 = linear_backward(d_out, kept.shared_hidden, Ws2)
+            s1 = linear_backward(s2["dx"], kept.x, Ws1, self.act, kept.shared_pre)
+            base = s1["dx"]
+            g.update(dWs1=s1["dW"], dbs1=s1["db"], dWs2=s2["dW"], dbs2=s2["db"])
+        dY, dgate_w = ragged_combine_backward(d_out, kept.Y, rows.row_of, r["gate_w"], dropout=kept.dropout)
+        # x_act: dx of the second projection is already the gradient ahead of the first one's activation
+        g2 = ragged_matmul_backward(dY, kept.hidden, self.W2, rows.offsets, x_act=self.act, x_pre=kept.pre)
+        g1 = ragged_matmul_backward(g2["dx"], kept.x, self.W1, rows.offsets, gather=rows.row_src)
+        dx = ragged_combine(g1["dx"], rows.row_of, None, residual=base)
+        gg = gate_backward(kept.x, self.Wg, r["logits"], r["idx"], dgate_w, self.normalize, dx=dx)
+        g.update(dx=gg["dx"], dWg=gg["dWg"], dgate_bias=gg["dbias"], dW1=g1["dW"], db1=g1["db"], dW2=g2["dW"], db2=g2["db"])
+        return g
