@@ -61,7 +61,7 @@ def expert(x, W1, b1, W2, b2, act, dtype):
 def expert_backward(x, W1, W2, hidden, slope, dY, dtype):
     dp = times(mm(dY, W2.T, dtype), slope).rounded(dtype)
     n = x.v.shape[0]
-    sums = lambda d: Q(d.v.sum(0), d.e.sum(0) + (n / 16 + 96) * 2.0 ** -24 * (np.abs(d.v) + d.e).sum(0)).rounded(dtype)   # noqa: E731
+    sums = lambda d: Q(d.v.sum(0), d.e.sum(0) + (n / 8 + 96) * 2.0 ** -24 * (np.abs(d.v) + d.e).sum(0)).rounded(dtype)   # noqa: E731
     return mm(dp, W1.T, dtype), mm(x.T, dp, dtype).rounded(dtype), sums(dp), mm(hidden.T, dY, dtype).rounded(dtype), sums(dY)
 
 

@@ -145,7 +145,7 @@ def test_ragged_product_and_gradients(moe, R, E, K, N, kind, behind, dtype):
     assert_within(g["dx"][:R], dx[:R], (ex + sum_error(dtype, N) * sx + HALF[dtype] * np.abs(dx))[:R], "dx")
     longest = int(fills.max())
     assert_within(g["dW"], dW, eW + sum_error(dtype, longest) * sW + HALF[dtype] * np.abs(dW), "dW")
-    assert_within(g["db"], db, eb + (longest / 16 + 96) * 2.0 ** -24 * sb + HALF[dtype] * np.abs(db), "db")
+    assert_within(g["db"], db, eb + (longest / 8 + 96) * 2.0 ** -24 * sb + HALF[dtype] * np.abs(db), "db")
     for want in ("dx", "dW", "db"):                                  # each by itself, the same bits
         only = moe.ragged_matmul_backward(dy, A, W, off, ACT[act], None if act == "none" else pre, gather=gather, **{f"want_{w}": w == want for w in ("dx", "dW", "db")})
         rows = slice(0, R) if want == "dx" else slice(None)
@@ -217,7 +217,7 @@ def test_linear_and_gradients(moe, T, K, N, dtype):
     g = moe.linear_backward(dy, x, W, ACT[act], None if act == "none" else pre)
     assert_within(g["dx"], dx, ex + sum_error(dtype, N) * sx + HALF[dtype] * np.abs(dx), "dx")
     assert_within(g["dW"], dW[0], (eW + sum_error(dtype, T) * sW)[0] + HALF[dtype] * np.abs(dW[0]), "dW")
-    assert_within(g["db"], db[0], (eb + (T / 16 + 96) * 2.0 ** -24 * sb)[0] + HALF[dtype] * np.abs(db[0]), "db")
+    assert_within(g["db"], db[0], (eb + (T / 8 + 96) * 2.0 ** -24 * sb)[0] + HALF[dtype] * np.abs(db[0]), "db")
 
 
 def test_gradients_against_differences(moe):
