@@ -19,6 +19,13 @@ bool all_aligned(std::initializer_list<const void*> ps, size_t a) {
   return true;
 }
 
+// whether a result would go onto one of what it is made of
+bool among(const void* out, std::initializer_list<const void*> ps) {
+  for (const void* p : ps)
+    if (out && p == out) return true;
+  return false;
+}
+
 bool any_act(int act) { return act == MOE_ACT_NONE || act_ok(act); }
 inline int status_of(hipError_t err) { return err == hipSuccess ? MOE_OK : MOE_HIP_ERROR; }
 
@@ -86,7 +93,8 @@ int moe_ragged_rows(const int32_t* idx, const int32_t* loc, const int32_t* count
 
 int moe_ragged_matmul(const void* A, const int32_t* gather, int64_t A_rows, const void* W, const void* bias, int act, int dtype, const int32_t* offsets, int64_t R,
                       int64_t E, int64_t K, int64_t N, void* pre, void* out, void* stream) {
-  if (!A || !W || !offsets || !out || !dtype_ok(dtype) || !any_act(act) || (gather && A_rows < 1)) return MOE_INVALID_ARG;
+  if (!A || !W || !offsets || !out || !dtype_ok(dtype) || !any_act(act) || (gather && A_rows < 1) || among(out, {A, W, bias}) || among(pre, {A, W, bias, out}))
+    return MOE_INVALID_ARG;
   if (int st = product_status(R, E, K, N)) return st;
   if ((gather && A_rows >= kMaxRows) || !all_aligned({A, W, bias, pre, out}, 16) || !all_aligned({gather, offsets}, 4)) return MOE_UNSUPPORTED;
   const RowsProduct p = {A, W, bias, nullptr, offsets, gather, A_rows, R, E, K, N, act, dtype, out, pre};
@@ -102,7 +110,8 @@ int moe_ragged_matmul_backward(const void* dy, const void* x, const int32_t* gat
                                int dtype, const int32_t* offsets, int64_t R, int64_t E, int64_t K, int64_t N, void* ws, size_t ws_bytes, void* dx, void* dW, void* db,
                                void* stream) {
   if (!dy || !offsets || !dtype_ok(dtype) || !any_act(act) || !any_act(x_act) || (act >= 0) != (pre != nullptr) || (x_act >= 0) != (x_pre != nullptr) || (!dx && !dW && !db) ||
-      (dx && !W) || (dW && !x) || (gather && x_rows < 1) || !ws || (x_pre && !dx))
+      (dx && !W) || (dW && !x) || (gather && x_rows < 1) || !ws || (x_pre && !dx) || among(dx, {dy, x, W, pre, dW, db}) || among(dW, {dy, x, W, pre, x_pre, db}) ||
+      among(db, {dy, x, W, pre, x_pre}))
     return MOE_INVALID_ARG;
   if (int st = product_status(R, E, K, N)) return st;
   if ((gather && x_rows >= kMaxRows) || !all_aligned({dy, x, W, pre, x_pre, dx, dW, db}, 16) || !all_aligned({gather, offsets}, 4) || !aligned(ws, 256)) return MOE_UNSUPPORTED;
@@ -116,7 +125,7 @@ size_t moe_linear_workspace_bytes(int64_t T, int64_t K, int64_t N, int dtype) {
 
 int moe_linear(const void* x, const void* W, const void* bias, int act, const void* residual, int dtype, int64_t T, int64_t K, int64_t N, void* ws, size_t ws_bytes,
                void* pre, void* out, void* stream) {
-  if (!x || !W || !out || !dtype_ok(dtype) || !any_act(act)) return MOE_INVALID_ARG;
+  if (!x || !W || !out || !dtype_ok(dtype) || !any_act(act) || among(out, {x, W, bias}) || among(pre, {x, W, bias, residual, out})) return MOE_INVALID_ARG;
   if (int st = product_status(T, 1, K, N)) return st;
   const size_t need = rows_product_bytes(dtype, T, K, N);
   if (need > 0 && !ws) return MOE_INVALID_ARG;
@@ -132,7 +141,9 @@ size_t moe_linear_backward_workspace_bytes(int64_t T, int64_t K, int64_t N, int 
 
 int moe_linear_backward(const void* dy, const void* x, const void* W, const void* pre, int act, int dtype, int64_t T, int64_t K, int64_t N, void* ws, size_t ws_bytes,
                         void* dx, void* dW, void* db, void* stream) {
-  if (!dy || !dtype_ok(dtype) || !any_act(act) || (act >= 0) != (pre != nullptr) || (!dx && !dW && !db) || (dx && !W) || (dW && !x) || !ws) return MOE_INVALID_ARG;
+  if (!dy || !dtype_ok(dtype) || !any_act(act) || (act >= 0) != (pre != nullptr) || (!dx && !dW && !db) || (dx && !W) || (dW && !x) || !ws ||
+      among(dx, {dy, x, W, pre, dW, db}) || among(dW, {dy, x, W, pre, db}) || among(db, {dy, x, W, pre}))
+    return MOE_INVALID_ARG;
   if (int st = product_status(T, 1, K, N)) return st;
   if (!all_aligned({dy, x, W, pre, dx, dW, db}, 16) || !aligned(ws, 256)) return MOE_UNSUPPORTED;
   if (ws_bytes < backward_layout(T, 1, K, N, act, dtype).total) return MOE_WORKSPACE_TOO_SMALL;
@@ -156,7 +167,7 @@ static int combine_status(int64_t T, int64_t M, int k, int64_t R) {
 int moe_ragged_combine(const void* Y, int64_t R, const int32_t* row_of, const float* gate_w, const void* residual, double p, const uint64_t* seed, int dtype, int64_t T,
                        int64_t M, int k, void* out, void* stream) {
   Dropout d;
-  if (!Y || !row_of || !out || !dtype_ok(dtype) || !dropout_of(p, seed, d)) return MOE_INVALID_ARG;
+  if (!Y || !row_of || !out || !dtype_ok(dtype) || !dropout_of(p, seed, d) || out == Y) return MOE_INVALID_ARG;
   if (int st = combine_status(T, M, k, R)) return st;
   if (!all_aligned({Y, residual, out}, 16) || !all_aligned({seed}, 8) || !all_aligned({row_of, gate_w}, 4)) return MOE_UNSUPPORTED;
   return status_of(launch_ragged_combine(Y, R, row_of, gate_w, residual, d, dtype, T, M, k, out, (hipStream_t)stream));
@@ -165,7 +176,7 @@ int moe_ragged_combine(const void* Y, int64_t R, const int32_t* row_of, const fl
 int moe_ragged_combine_backward(const void* d_out, const void* Y, int64_t R, const int32_t* row_of, const float* gate_w, double p, const uint64_t* seed, int dtype,
                                 int64_t T, int64_t M, int k, void* dY, float* dgate_w, void* stream) {
   Dropout d;
-  if (!d_out || !Y || !row_of || !dY || !dgate_w || !dtype_ok(dtype) || !dropout_of(p, seed, d)) return MOE_INVALID_ARG;
+  if (!d_out || !Y || !row_of || !dY || !dgate_w || !dtype_ok(dtype) || !dropout_of(p, seed, d) || dY == d_out || dY == Y) return MOE_INVALID_ARG;
   if (int st = combine_status(T, M, k, R)) return st;
   if (!all_aligned({d_out, Y, dY}, 16) || !all_aligned({seed}, 8) || !all_aligned({row_of, gate_w, dgate_w}, 4)) return MOE_UNSUPPORTED;
   return status_of(launch_ragged_combine_backward(d_out, Y, R, row_of, gate_w, d, dtype, T, M, k, dY, dgate_w, (hipStream_t)stream));
