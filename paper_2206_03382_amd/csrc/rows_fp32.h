@@ -167,11 +167,7 @@ __global__ __launch_bounds__(256, 5) void rows_fp32_kernel(const TileArgs p) {
     constexpr int NR = NA + NB, SPAN = NM * 3 / 4, BAR = NM * 7 / 8, GAP = (2 * NM - BAR) / (2 * L);
     auto kstep = [&](auto dma_tag, int kt, uint32_t cur, uint32_t nxt) __attribute__((always_inline)) {
       constexpr bool DMA = decltype(dma_tag)::value;                  // K-step kt + NS exists
-      if (DMA) {
-        if (kt + NS == KT - 1) end_loads((int)(kend - (int64_t)(kt + NS) * BKE));
-        gather_fetch(kt + NS, grow);
-        PIN();
-      }
+      if (DMA && kt + NS == KT - 1) end_loads((int)(kend - (int64_t)(kt + NS) * BKE));
 #pragma unroll
       for (int m = 0; m < 2 * NM; ++m) {
         const int s = m / NM, at = m % NM;
@@ -185,7 +181,11 @@ __global__ __launch_bounds__(256, 5) void rows_fp32_kernel(const TileArgs p) {
           PIN();
           asm volatile("s_barrier" ::: "memory");
           PIN();
-          if (DMA) { gather_resolve(kt + NS, grow, a_row); PIN(); }
+          if (DMA) {
+            gather_resolve(kt + NS, grow, a_row);
+            gather_fetch(kt + NS + 1, grow);
+            PIN();
+          }
         }
         if (DMA && m >= BAR && (m - BAR) % GAP == 0 && (m - BAR) / GAP < 2 * L) load((m - BAR) / GAP, a_row, smem_addr + cur);
         PIN();
@@ -196,6 +196,7 @@ __global__ __launch_bounds__(256, 5) void rows_fp32_kernel(const TileArgs p) {
       Sources from[NS];
 #pragma unroll
       for (int t = 0; t < NS; ++t) gather_fetch(t, g[t]);
+      gather_fetch(NS, grow);
 #pragma unroll
       for (int t = 0; t < NS; ++t) gather_resolve(t, g[t], from[t]);
 #pragma unroll
