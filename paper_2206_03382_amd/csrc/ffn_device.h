@@ -218,6 +218,8 @@ struct TileArgs {
   void* pre_out;                // kNN: the values before the activation go here as well
   int act;                      // MOE_ACT_*, + kFullAct (bf16 results) for the form with erf and true divisions; < 0: none
   int64_t ktotal;               // PART: length of the whole reduction, of which every "expert" is K consecutive k
+  int parts;                    // ROWS, kTN, > 1: blocks (grid z) that share a tile's reduction, in whole K-steps; their sums go to part_sums [part][E][C][N]
+  float* part_sums;
 };
 
 // Fills in the tile counts and the grid of a launch on tiles of bm x bn (total: rows of all experts that exist, at most); false

@@ -61,7 +61,12 @@ __global__ __launch_bounds__(256, 2 * ring_bytes(TM, TN) <= 163840 ? 2 : 1) void
   int64_t kend = p.K;                                               // k that exist
   if (MODE == kTN && ROWS) kend = live_rows_of<ROWS>(e, p.K, p.kfill);
   else if (MODE == kTN && p.kfill) { const int64_t c = p.kfill[e]; kend = c < p.K ? (c > 0 ? c : 0) : p.K; }
-  const int64_t first = MODE == kTN ? first_row_of<ROWS>(e, p.K, p.kfill) : first_row_of<ROWS>(e, p.C, p.counts);   // of the expert's rows
+  int64_t first = MODE == kTN ? first_row_of<ROWS>(e, p.K, p.kfill) : first_row_of<ROWS>(e, p.C, p.counts);   // of the expert's rows
+  if (MODE == kTN && ROWS && p.parts > 1) {
+    const int64_t each = ((kend + 63) / 64 + p.parts - 1) / p.parts * 64, from = blockIdx.z * each < kend ? blockIdx.z * each : kend;
+    first += from;
+    kend = kend - from < each ? kend - from : each;
+  }
   const int KT = kend > 0 ? (int)((kend + 63) / 64) : 1;
 
   // ---- this lane's direct loads.  k-contiguous: block q * 4 + wave = 8 rows, lane l row + l / 8, position l % 8.  k-slow: pieces in order.
@@ -411,6 +416,17 @@ __global__ __launch_bounds__(256, 2 * ring_bytes(TM, TN) <= 163840 ? 2 : 1) void
       }
       __builtin_amdgcn_wave_barrier();
     };
+    if (MODE == kTN && p.parts > 1) {
+#pragma unroll
+      for (int i = 0; i < RA; ++i)
+#pragma unroll
+        for (int j = 0; j < RB; ++j) {
+          const int64_t r = i * 16 + (lane & 15), col = nw + j * 16 + 4 * kq;
+          if (r < live && col < p.N)
+            *reinterpret_cast<f32x4*>(p.part_sums + (((int64_t)blockIdx.z * p.E + e) * p.C + m0 + wm * WTM + r) * p.N + col) = acc[i][j];
+        }
+      return;
+    }
     const uint16_t* with = MODE == kTN ? nullptr : (const uint16_t*)p.pre;
     if (MODE == kNN && p.pre_out) write_rows(std::integral_constant<int, -1>{}, (uint16_t*)p.pre_out, nullptr);
     if (MODE == kTN) write_rows(std::integral_constant<int, -1>{}, (uint16_t*)p.out, nullptr);
@@ -442,6 +458,7 @@ template <int MODE, int TM, int TN, bool ROWS = false>
 static hipError_t launch_ring(TileArgs p, int64_t total, hipStream_t s) {
   dim3 grid;
   if (!tile_launch(p, TM, TN, total, grid)) return hipErrorInvalidValue;
+  if (MODE == kTN && ROWS && p.parts > 1) grid.z = (unsigned)p.parts;
   if (MODE == kTN && p.gather) grouped_gemm_ring_kernel<MODE, TM, TN, MODE == kTN, ROWS><<<grid, dim3(256), 0, s>>>(p);
   else grouped_gemm_ring_kernel<MODE, TM, TN, false, ROWS><<<grid, dim3(256), 0, s>>>(p);
   return hipGetLastError();

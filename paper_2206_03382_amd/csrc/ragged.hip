@@ -24,6 +24,7 @@ namespace moe {
 
 #include "rows_thin.h"
 #include "rows_fp32.h"
+#include "rows_outer.h"
 
 namespace {
 
@@ -116,26 +117,39 @@ hipError_t launch_rows_product_nt(const void* d, const void* W, const void* x_pr
 
 namespace {
 
+bool weight_grad_large(int64_t E, int64_t K, int64_t N, int64_t gather_rows) {
+  return K % kLargeTile == 0 && N % kLargeTile == 0 && large_takes(E, K, N, gather_rows, K);
+}
 Tile weight_grad_tile(int dtype, int64_t R, int64_t E, int64_t K, int64_t N, bool gathered, int64_t gather_rows) {
-  const bool large_ok = K % kLargeTile == 0 && N % kLargeTile == 0 && large_takes(E, K, N, gathered ? gather_rows : 0, K);
-  return rows_tile(kTN, dtype, large_ok, E, K, (double)mean_rows(R, E), R, N, gathered);
+  return rows_tile(kTN, dtype, weight_grad_large(E, K, N, gathered ? gather_rows : 0), E, K, (double)mean_rows(R, E), R, N, gathered);
+}
+int weight_grad_shares(int dtype, int64_t R, int64_t E, int64_t K, int64_t N) {
+  return weight_grad_parts(dtype, weight_grad_large(E, K, N, 0), E, (double)mean_rows(R, E), K, N);
 }
 
 }  // namespace
 
-// The large tile's last K-step of 64 rows comes from side buffers of both operands.
+// Sums of the blocks that share a tile; or the large tile's last K-step of 64 rows, which comes from side buffers of both operands.
 size_t rows_weight_grad_bytes(int dtype, int64_t R, int64_t E, int64_t K, int64_t N) {
+  const int parts = weight_grad_shares(dtype, R, E, K, N);
+  if (parts > 1) return (size_t)parts * E * K * N * 4;
   if (weight_grad_tile(dtype, R, E, K, N, false, 0) != Tile::k256 && weight_grad_tile(dtype, R, E, K, N, true, 1) != Tile::k256) return 0;
   return grouped_gemm_tn_tail_bytes(E, K) + grouped_gemm_tn_tail_bytes(E, N);
 }
 
 hipError_t launch_rows_weight_grad(const void* A, const int32_t* gather, int64_t gather_rows, const void* d, int dtype, const int32_t* offsets, int64_t R, int64_t E,
                                    int64_t K, int64_t N, void* ws, void* dW, hipStream_t s) {
+  const int parts = weight_grad_shares(dtype, R, E, K, N);
   const Tile tile = weight_grad_tile(dtype, R, E, K, N, gather != nullptr, gather_rows);
-  if (tile != Tile::k256) {
-    const TileArgs t = {A, d, nullptr, nullptr, gather, gather_rows, K, R, (int)N, (int)E, 0, 0, 0, dW, offsets, nullptr, nullptr, -1, 0};
-    return launch_small_rows<kTN>(dtype, tile, t, E * K, s);
+  TileArgs t = {A, d, nullptr, nullptr, gather, gather_rows, K, R, (int)N, (int)E, 0, 0, 0, dW, offsets, nullptr, nullptr, -1, 0};
+  if (parts > 1) {
+    t.parts = parts;
+    t.part_sums = (float*)ws;
+    if (hipError_t err = launch_small_rows<kTN>(dtype, Tile::k128, t, E * K, s)) return err;
+    return join_parts(t, dtype, s);
   }
+  if (dtype == MOE_BF16 && outer_takes(E, (double)mean_rows(R, E), K, N)) return launch_outer(t, E * K, s);
+  if (tile != Tile::k256) return launch_small_rows<kTN>(dtype, tile, t, E * K, s);
   uint16_t* a_tail = (uint16_t*)ws;
   uint16_t* b_tail = a_tail + grouped_gemm_tn_tail_bytes(E, K) / 2;
   const TailRows ta = {(const uint4*)A, (uint4*)a_tail, gather, gather_rows, (int)(K / 8)}, tb = {(const uint4*)d, (uint4*)b_tail, nullptr, 0, (int)(N / 8)};

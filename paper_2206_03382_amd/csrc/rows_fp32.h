@@ -38,8 +38,13 @@ __global__ __launch_bounds__(256, 5) void rows_fp32_kernel(const TileArgs p) {
   }
   const int64_t m0 = (int64_t)mt * T, n0 = (int64_t)nt * T;
   if (m0 >= rows) return;
-  const int64_t kend = MODE == kTN ? live_rows_of<true>(e, p.K, p.kfill) : p.K;
-  const int64_t first = MODE == kTN ? first_row_of<true>(e, p.K, p.kfill) : first_row_of<true>(e, p.C, p.counts);      // of the expert's rows
+  int64_t kend = MODE == kTN ? live_rows_of<true>(e, p.K, p.kfill) : p.K;
+  int64_t first = MODE == kTN ? first_row_of<true>(e, p.K, p.kfill) : first_row_of<true>(e, p.C, p.counts);      // of the expert's rows
+  if (MODE == kTN && p.parts > 1) {                                 // this block's share of the reduction
+    const int64_t each = ((kend + BKE - 1) / BKE + p.parts - 1) / p.parts * BKE, from = blockIdx.z * each < kend ? blockIdx.z * each : kend;
+    first += from;
+    kend = kend - from < each ? kend - from : each;
+  }
   const int KT = kend > 0 ? (int)((kend + BKE - 1) / BKE) : 1;
 
   // ---- this lane's direct loads.  k-contiguous: block q * 4 + wave = 8 rows, lane l row + l / 8, position l % 8.  k-slow: pieces of 4 columns in order.
@@ -250,7 +255,7 @@ __global__ __launch_bounds__(256, 5) void rows_fp32_kernel(const TileArgs p) {
         for (int i = 0; i < R; ++i) acc[i][(4 * g + x) % R][(4 * g + x) / R] += b[x];
     }
   }
-  const int64_t out_at = ((MODE == kTN ? (int64_t)e * p.C : first) + m0 + wm * WT) * p.N;
+  const int64_t out_at = ((MODE == kTN ? ((p.parts > 1 ? (int64_t)blockIdx.z * p.E : 0) + e) * p.C : first) + m0 + wm * WT) * p.N;
   const float* with = MODE == kTN ? nullptr : (const float*)p.pre;
   auto write_rows = [&](auto act_tag, float* dst, const float* add) __attribute__((always_inline)) {
     constexpr int ACT = decltype(act_tag)::value;
@@ -274,7 +279,7 @@ __global__ __launch_bounds__(256, 5) void rows_fp32_kernel(const TileArgs p) {
     }
   };
   if (MODE == kNN && p.pre_out) write_rows(std::integral_constant<int, -1>{}, (float*)p.pre_out, nullptr);
-  if (MODE == kTN) write_rows(std::integral_constant<int, -1>{}, (float*)p.out, nullptr);
+  if (MODE == kTN) write_rows(std::integral_constant<int, -1>{}, p.parts > 1 ? p.part_sums : (float*)p.out, nullptr);
   else switch (p.act) {
     case MOE_ACT_RELU: write_rows(std::integral_constant<int, MOE_ACT_RELU>{}, (float*)p.out, with); break;
     case MOE_ACT_GELU: write_rows(std::integral_constant<int, MOE_ACT_GELU>{}, (float*)p.out, with); break;
@@ -286,6 +291,7 @@ __global__ __launch_bounds__(256, 5) void rows_fp32_kernel(const TileArgs p) {
 template <int MODE> hipError_t launch_rows_fp32(TileArgs p, int64_t total, hipStream_t s) {
   dim3 grid;
   if (!tile_launch(p, 64, 64, total, grid)) return hipErrorInvalidValue;
+  if (MODE == kTN && p.parts > 1) grid.z = (unsigned)p.parts;
   if (MODE == kTN && p.gather) rows_fp32_kernel<MODE, MODE == kTN><<<grid, dim3(256), 0, s>>>(p);
   else rows_fp32_kernel<MODE, false><<<grid, dim3(256), 0, s>>>(p);
   return hipGetLastError();
