@@ -294,7 +294,9 @@ static inline bool large_tile_supports_backward(int64_t E, int64_t C, int64_t M,
 // 32 rows: 39 us plain, 41 streamed).
 enum class Tile { k256, k128, k64x128, k64, k64x128_stream, k64_stream, kHalf };
 
-static inline double tile_cost(Tile tile, int mode, int64_t E, int64_t rows, double mean_rows, int64_t K, int64_t N, bool gathered) {
+// at_least_one (products of rows that lie one behind the other): fewer than six tiles count as the one round that they take.  Without, they count as none, and a dx of 1024 x 256 over 4096
+// columns took the large tile, 68 us; so 18.
+static inline double tile_cost(Tile tile, int mode, int64_t E, int64_t rows, double mean_rows, int64_t K, int64_t N, bool gathered, bool at_least_one = false) {
   const double ksteps = (mode == kTN ? mean_rows : (double)K) / 64 + 0.5;
   auto cost = [&](int bm, int bn, int per_unit, double base, double fix, double lat, double thr) {
     // an average fill ends in half a tile, but no expert has more row tiles than its slab (without this bound 24 experts x 256
@@ -303,6 +305,7 @@ static inline double tile_cost(Tile tile, int mode, int64_t E, int64_t rows, dou
     const double row_tiles = mode == kTN || some > full ? full : (some > 1.0 ? some : 1.0);
     double q = (double)E * row_tiles * (double)tiles_in(N, bn) / 256.0;             // tiles per compute unit
     q = q <= 4.0 * per_unit ? ceil(q - 0.02) : q + 0.5;
+    if (at_least_one && q < 1.0) q = 1.0;
     const double rounds = q > per_unit ? q / per_unit : 1.0;
     return base + fix * rounds + ksteps * (lat * rounds > thr * q ? lat * rounds : thr * q);
   };
@@ -317,9 +320,9 @@ static inline double tile_cost(Tile tile, int mode, int64_t E, int64_t rows, dou
 }
 
 // large_ok, half_ok: whether the launch may run on the large tile, and on its half.
-static inline Tile choose_tile(int mode, bool large_ok, bool half_ok, int64_t E, int64_t rows, double mean_rows, int64_t K, int64_t N, bool gathered) {
+static inline Tile choose_tile(int mode, bool large_ok, bool half_ok, int64_t E, int64_t rows, double mean_rows, int64_t K, int64_t N, bool gathered, bool at_least_one = false) {
   if (mode != kTN && mean_rows <= 48.0 && (double)E * K * N * 2 >= 48e6) return E * tiles_in(N, 128) >= 256 ? Tile::k64x128_stream : Tile::k64_stream;
-  auto estimate = [&](Tile t) { return tile_cost(t, mode, E, rows, mean_rows, K, N, gathered); };
+  auto estimate = [&](Tile t) { return tile_cost(t, mode, E, rows, mean_rows, K, N, gathered, at_least_one); };
   Tile best = Tile::k128;
   double least = estimate(best);
   auto consider = [&](Tile t) {

@@ -42,7 +42,7 @@ template <int MODE> hipError_t launch_small_rows(int dtype, Tile tile, const Til
 }
 
 Tile rows_tile(int mode, int dtype, bool large_ok, int64_t E, int64_t rows, double mean, int64_t K, int64_t N, bool gathered) {
-  return dtype == MOE_BF16 ? choose_tile(mode, large_ok, false, E, rows, mean, K, N, gathered) : Tile::k64;
+  return dtype == MOE_BF16 ? choose_tile(mode, large_ok, false, E, rows, mean, K, N, gathered, true) : Tile::k64;
 }
 
 }  // namespace
