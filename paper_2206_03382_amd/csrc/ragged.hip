@@ -25,6 +25,7 @@ namespace moe {
 #include "rows_thin.h"
 #include "rows_fp32.h"
 #include "rows_outer.h"
+#include "rows_short.h"
 
 namespace {
 
@@ -55,16 +56,14 @@ size_t rows_product_bytes(int dtype, int64_t R, int64_t K, int64_t N) {
 
 hipError_t launch_rows_product(const RowsProduct& p, void* ws, hipStream_t s) {
   const bool dual = p.pre && p.act >= 0;
+  const TileArgs t = {p.A, p.W, p.bias, p.offsets, p.gather, p.gather_rows, p.R, p.K, (int)p.N, (int)p.E, 0, 0, 0, p.out, nullptr, p.residual, p.pre, p.act, 0};
   if (p.dtype == MOE_BF16) {
     const ThinPlan plan = thin_plan(p.offsets != nullptr, p.E, p.R, p.K, p.N);
-    const TileArgs t = {p.A, p.W, p.bias, p.offsets, p.gather, p.gather_rows, p.R, p.K, (int)p.N, (int)p.E, 0, 0, 0, p.out, nullptr, p.residual, p.pre, p.act, 0};
     if (plan.ri > 0) return launch_thin(t, plan, (float*)ws, s);
   }
   const Tile tile = rows_tile(kNN, p.dtype, large_takes(p.E, p.K, p.N, p.gather ? p.gather_rows : 0, p.K), p.E, p.R, (double)mean_rows(p.R, p.E), p.K, p.N, p.gather != nullptr);
-  if (tile != Tile::k256) {
-    const TileArgs t = {p.A, p.W, p.bias, p.offsets, p.gather, p.gather_rows, p.R, p.K, (int)p.N, (int)p.E, 0, 0, 0, p.out, nullptr, p.residual, p.pre, p.act, 0};
-    return launch_small_rows<kNN>(p.dtype, tile, t, p.R, s);
-  }
+  if (p.dtype == MOE_BF16 && short_takes(tile, (p.R / 128) * tiles_in(p.N, 128), p.K, p.act >= 0, p.residual || p.pre)) return launch_short<kNN>(t, p.R, s);
+  if (tile != Tile::k256) return launch_small_rows<kNN>(p.dtype, tile, t, p.R, s);
   const int MT = (int)ceil_div(p.R, BM), NT = (int)(p.N / BN);
   const int64_t blocks = tile_grid(NT, live_row_tiles(p.E, p.R, p.R, BM), true, false);
   if (blocks >= kMaxBlocks) return hipErrorInvalidValue;
@@ -94,10 +93,9 @@ hipError_t launch_rows_product_nt(const void* d, const void* W, const void* x_pr
                                   int64_t N, void* dx, hipStream_t s) {
   if (x_act < 0) x_pre = nullptr;
   const Tile tile = rows_tile(kNT, dtype, large_takes(E, N, K, 0, 0), E, R, (double)mean_rows(R, E), N, K, false);
-  if (tile != Tile::k256) {
-    const TileArgs t = {d, W, nullptr, offsets, nullptr, 0, R, N, (int)K, (int)E, 0, 0, 0, dx, nullptr, x_pre, nullptr, x_pre ? x_act : -1, 0};
-    return launch_small_rows<kNT>(dtype, tile, t, R, s);
-  }
+  const TileArgs t = {d, W, nullptr, offsets, nullptr, 0, R, N, (int)K, (int)E, 0, 0, 0, dx, nullptr, x_pre, nullptr, x_pre ? x_act : -1, 0};
+  if (dtype == MOE_BF16 && short_takes(tile, (R / 128) * tiles_in(K, 128), N, x_pre != nullptr, false)) return launch_short<kNT>(t, R, s);
+  if (tile != Tile::k256) return launch_small_rows<kNT>(dtype, tile, t, R, s);
   const int MT = (int)ceil_div(R, BM), NT = (int)(K / BN);
   const int64_t blocks = tile_grid(NT, live_row_tiles(E, R, R, BM), true, false);
   if (blocks >= kMaxBlocks) return hipErrorInvalidValue;

@@ -88,7 +88,7 @@ PRODUCTS = [
     (513, 2, 320, 1024, "one", 9), (700, 9, 1000, 776, "skewed", 4), (1111, 17, 64, 256, "skewed", 13), (2048, 4, 512, 1024, "even", 0), (4099, 3, 128, 2560, "skewed", 5),
     (6000, 70, 192, 512, "skewed", 0), (5000, 140, 64, 512, "skewed", 1), (30000, 2, 64, 256, "skewed", 0), (20000, 4, 256, 512, "skewed", 0),
     (1, 3, 1024, 72, "one", 2), (8, 128, 1032, 1024, "even", 0), (16, 5, 1544, 136, "skewed", 2), (11, 2, 2048, 1032, "one", 1),
-    (4000, 3, 256, 264, "even", 3), (9001, 5, 136, 128, "skewed", 0), (5000, 40, 1024, 1032, "even", 0),                     # shared reductions over rows; many tiles, 125 rows each
+    (4000, 3, 256, 264, "even", 3), (9001, 5, 136, 128, "skewed", 0), (5000, 40, 1024, 1032, "even", 0), (9000, 3, 264, 520, "skewed", 5), (4097, 5, 256, 1288, "even", 0), (8200, 4, 768, 512, "skewed", 2),                     # shared reductions over rows; many tiles, 125 rows each
 ]
 
 
@@ -155,7 +155,7 @@ def test_ragged_product_and_gradients(moe, R, E, K, N, kind, behind, dtype):
 
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("act", ["relu", "gelu", "silu"])
-@pytest.mark.parametrize("R,E,K,N", [(5, 2, 72, 64), (130, 4, 256, 512), (700, 3, 328, 200), (3000, 4, 512, 256)])
+@pytest.mark.parametrize("R,E,K,N", [(5, 2, 72, 64), (130, 4, 256, 512), (700, 3, 328, 200), (3000, 4, 512, 256), (9001, 3, 520, 264), (8000, 3, 512, 776)])
 def test_gradient_of_the_projection_before(moe, R, E, K, N, act, dtype):
     """dx times the derivative of the activation that made x, in one rounding."""
     rng = np.random.default_rng(R + K)
@@ -177,7 +177,7 @@ def test_gradient_of_the_projection_before(moe, R, E, K, N, act, dtype):
 
 LINEAR = [(1, 8, 8), (1, 4096, 264), (1, 264, 4096), (2, 64, 64), (3, 1000, 776), (8, 2048, 512), (15, 72, 1032), (16, 1024, 1024), (17, 512, 256), (31, 776, 1544), (33, 4096, 136), (64, 256, 2048), (65, 64, 64),
           (100, 1024, 4096), (127, 128, 256), (256, 320, 512), (300, 776, 264), (1000, 512, 1024), (2049, 192, 256), (4100, 1024, 1280), (9000, 64, 512),
-          (1, 4096, 4096), (19, 2056, 1032), (50, 4096, 2056), (110, 2568, 4096), (290, 4096, 1000), (8193, 520, 264)]          # few rows, the reduction shared by blocks
+          (1, 4096, 4096), (19, 2056, 1032), (50, 4096, 2056), (110, 2568, 4096), (290, 4096, 1000), (8193, 520, 264), (20001, 264, 256), (10000, 512, 776)]          # few rows, the reduction shared by blocks
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
