@@ -863,17 +863,12 @@ class NormMoELayer8:
 # ---- experts' rows one behind the other, dense projections, dropout ------------------------------------------------------
 
 def _here(*tensors: Optional[torch.Tensor]) -> List[Optional[int]]:
-    """Their addresses.  The library launches on the current device's stream: all tensors have to be there, and contiguous."""
+    """Their addresses.  The library launches on the current device's stream: all tensors have to be there, and contiguous (results that the calls allocate like them are)."""
     device = torch._C._cuda_getDevice()
-    at = []
     for t in tensors:
-        if t is None:
-            at.append(None)
-        elif t.get_device() != device or not t.is_contiguous():
+        if t is not None and (t.get_device() != device or not t.is_contiguous()):
             raise ValueError("tensors must be contiguous and on the current device")
-        else:
-            at.append(t.data_ptr())
-    return at
+    return [None if t is None else t.data_ptr() for t in tensors]
 
 
 def _as_stored(t: torch.Tensor, like: torch.Tensor, what: str, *shape: int) -> None:
@@ -900,16 +895,14 @@ class RaggedRows(NamedTuple):
 
 def ragged_rows(idx: torch.Tensor, loc: torch.Tensor, counts: torch.Tensor, C: int = 0) -> RaggedRows:
     """The rows of the choices of gate_topk or gate_route, one expert's behind the other's; C: a capacity beyond which they are dropped (0: none is)."""
-    if idx.dim() != 2 or idx.dtype != torch.int32:
-        raise ValueError("idx must be int32 [T,k]")
-    T, k = idx.shape
-    E = counts.shape[0]
-    _check_int32(loc, T, k)
-    _check_int32(counts, E)
-    r = RaggedRows(counts.new_empty((E + 1,)), counts.new_empty((T * k,)), torch.empty_like(loc))
-    at = _here(idx, loc, counts, *r)
-    _check(lib().moe_ragged_rows(*at[:3], T, E, k, C, *at[3:], _stream()), "moe_ragged_rows")
-    return r
+    shape, i32 = idx.shape, torch.int32
+    if len(shape) != 2 or loc.shape != shape or counts.dim() != 1 or idx.dtype != i32 or loc.dtype != i32 or counts.dtype != i32:
+        raise ValueError("idx and loc must be int32 [T,k], counts int32 [E]")
+    (T, k), E = shape, counts.shape[0]
+    idx_, loc_, counts_ = _here(idx, loc, counts)
+    offsets, row_src, row_of = counts.new_empty((E + 1,)), counts.new_empty((T * k,)), torch.empty_like(loc)
+    _check(lib().moe_ragged_rows(idx_, loc_, counts_, T, E, k, C, offsets.data_ptr(), row_src.data_ptr(), row_of.data_ptr(), _stream()), "moe_ragged_rows")
+    return RaggedRows(offsets, row_src, row_of)
 
 
 def ragged_matmul(A: torch.Tensor, W: torch.Tensor, offsets: torch.Tensor, bias: Optional[torch.Tensor] = None, act: int = ACT_NONE,
@@ -1018,22 +1011,22 @@ def dropout(x: torch.Tensor, p: float, seed: torch.Tensor, residual: Optional[to
     _check_seed(seed)
     if residual is not None and (residual.shape != x.shape or residual.dtype != x.dtype):
         raise ValueError("residual must have x's shape and type")
+    if out is not None:
+        _check_out(out, x.shape, x.dtype)
+    x_, residual_, seed_, _ = _here(x, residual, seed, out)
     if out is None:
         if p == 0 and residual is None:
-            _here(x, seed)
             return x
         out = torch.empty_like(x)
-    else:
-        _check_out(out, x.shape, x.dtype)
-    x_, residual_, seed_, out_ = _here(x, residual, seed, out)
-    _check(lib().moe_dropout(x_, residual_, p, seed_, code, x.numel(), out_, _stream()), "moe_dropout")
+    _check(lib().moe_dropout(x_, residual_, p, seed_, code, x.numel(), out.data_ptr(), _stream()), "moe_dropout")
     return out
 
 
 def _check_combine(Y: torch.Tensor, row_of: torch.Tensor, gate_w: Optional[torch.Tensor], dropout: Optional[Tuple[float, torch.Tensor]]) -> Tuple[float, Optional[torch.Tensor]]:
-    if Y.dim() != 2 or row_of.dim() != 2 or row_of.dtype != torch.int32:
+    shape = row_of.shape
+    if Y.dim() != 2 or len(shape) != 2 or row_of.dtype != torch.int32:
         raise ValueError("Y must be [R,M] and row_of int32 [T,k]")
-    if gate_w is not None and (gate_w.dtype != torch.float32 or gate_w.shape != row_of.shape):
+    if gate_w is not None and (gate_w.shape != shape or gate_w.dtype != torch.float32):
         raise ValueError("gate_w must be float32 [T,k]")
     if dropout is None:
         return 0.0, None
@@ -1050,12 +1043,12 @@ def ragged_combine(Y: torch.Tensor, row_of: torch.Tensor, gate_w: Optional[torch
     code = _dtype_code(Y)
     if residual is not None:
         _as_stored(residual, Y, "residual", T, M)
+    if out is not None:
+        _check_out(out, (T, M), Y.dtype)
+    Y_, row_of_, gate_w_, residual_, seed_, _ = _here(Y, row_of, gate_w, residual, seed, out)
     if out is None:
         out = Y.new_empty((T, M)) if residual is None else torch.empty_like(residual)
-    else:
-        _check_out(out, (T, M), Y.dtype)
-    Y_, row_of_, gate_w_, residual_, seed_, out_ = _here(Y, row_of, gate_w, residual, seed, out)
-    _check(lib().moe_ragged_combine(Y_, R, row_of_, gate_w_, residual_, p, seed_, code, T, M, k, out_, _stream()), "moe_ragged_combine")
+    _check(lib().moe_ragged_combine(Y_, R, row_of_, gate_w_, residual_, p, seed_, code, T, M, k, out.data_ptr(), _stream()), "moe_ragged_combine")
     return out
 
 
@@ -1066,13 +1059,14 @@ def ragged_combine_backward(d_out: torch.Tensor, Y: torch.Tensor, row_of: torch.
     (T, k), (R, M) = row_of.shape, Y.shape
     code = _dtype_code(Y)
     _as_stored(d_out, Y, "d_out", T, M)
+    if dY is not None:
+        _check_out(dY, Y.shape, Y.dtype)
+    d_out_, Y_, row_of_, gate_w_, seed_, _ = _here(d_out, Y, row_of, gate_w, seed, dY)
     if dY is None:
         dY = torch.empty_like(Y)
-    else:
-        _check_out(dY, Y.shape, Y.dtype)
-    dgate_w = torch.empty((T, k), dtype=torch.float32, device=Y.device)
-    d_out_, Y_, row_of_, gate_w_, seed_, dY_, dgate_w_ = _here(d_out, Y, row_of, gate_w, seed, dY, dgate_w)
-    _check(lib().moe_ragged_combine_backward(d_out_, Y_, R, row_of_, gate_w_, p, seed_, code, T, M, k, dY_, dgate_w_, _stream()), "moe_ragged_combine_backward")
+    dgate_w = torch.empty((T, k), dtype=torch.float32, device=Y.device) if gate_w is None else torch.empty_like(gate_w)
+    _check(lib().moe_ragged_combine_backward(d_out_, Y_, R, row_of_, gate_w_, p, seed_, code, T, M, k, dY.data_ptr(), dgate_w.data_ptr(), _stream()),
+           "moe_ragged_combine_backward")
     return dY, dgate_w
 
 
