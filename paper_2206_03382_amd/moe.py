@@ -871,6 +871,10 @@ def _here(*tensors: Optional[torch.Tensor]) -> List[Optional[int]]:
     return [None if t is None else t.data_ptr() for t in tensors]
 
 
+def _at(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
 def _as_stored(t: torch.Tensor, like: torch.Tensor, what: str, *shape: int) -> None:
     if t.dtype != like.dtype or t.shape != shape:
         raise ValueError(f"{what}: expected {list(shape)} in {like.dtype}")
@@ -918,13 +922,13 @@ def ragged_matmul(A: torch.Tensor, W: torch.Tensor, offsets: torch.Tensor, bias:
     _check_offsets(offsets, E)
     if bias is not None:
         _as_stored(bias, W, "bias", E, N)
+    if out is not None:
+        _check_out(out, (R, N), W.dtype)
+    A_, gather_, W_, bias_, offsets_, _ = _here(A, gather, W, bias, offsets, out)
     if out is None:
         out = A.new_empty((R, N))
-    else:
-        _check_out(out, (R, N), W.dtype)
     pre = torch.empty_like(out) if keep_pre and act != ACT_NONE else None
-    A_, gather_, W_, bias_, offsets_, pre_, out_ = _here(A, gather, W, bias, offsets, pre, out)
-    _check(lib().moe_ragged_matmul(A_, gather_, rows, W_, bias_, act, code, offsets_, R, E, K, N, pre_, out_, _stream()), "moe_ragged_matmul")
+    _check(lib().moe_ragged_matmul(A_, gather_, rows, W_, bias_, act, code, offsets_, R, E, K, N, _at(pre), out.data_ptr(), _stream()), "moe_ragged_matmul")
     return (out, pre) if keep_pre else out
 
 
@@ -946,14 +950,14 @@ def ragged_matmul_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, o
         _as_stored(pre, W, "pre", R, N)
     if x_pre is not None:
         _as_stored(x_pre, W, "x_pre", R, K)
+    dy_, x_, gather_, W_, pre_, x_pre_, offsets_ = _here(dy, x, gather, W, pre, x_pre, offsets)
     nbytes = lib().moe_ragged_matmul_backward_workspace_bytes(R, E, K, N, act, code)
     if nbytes == 0:
         raise MoEError(UNSUPPORTED, "moe_ragged_matmul_backward_workspace_bytes")
     ws = torch.empty((nbytes,), dtype=torch.uint8, device=W.device)
     g = dict(dx=x.new_empty((R, K)) if want_dx else None, dW=torch.empty_like(W) if want_dW else None, db=W.new_empty((E, N)) if want_db else None)
-    dy_, x_, gather_, W_, pre_, x_pre_, offsets_, ws_, *out = _here(dy, x, gather, W, pre, x_pre, offsets, ws, *g.values())
-    _check(lib().moe_ragged_matmul_backward(dy_, x_, gather_, rows, W_, pre_, act, x_pre_, x_act, code, offsets_, R, E, K, N, ws_, nbytes, *out, _stream()),
-           "moe_ragged_matmul_backward")
+    _check(lib().moe_ragged_matmul_backward(dy_, x_, gather_, rows, W_, pre_, act, x_pre_, x_act, code, offsets_, R, E, K, N, ws.data_ptr(), nbytes, _at(g["dx"]), _at(g["dW"]),
+                                            _at(g["db"]), _stream()), "moe_ragged_matmul_backward")
     return g
 
 
@@ -968,15 +972,15 @@ def linear(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None
         _as_stored(bias, W, "bias", N)
     if residual is not None:
         _as_stored(residual, W, "residual", T, N)
+    if out is not None:
+        _check_out(out, (T, N), W.dtype)
+    x_, W_, bias_, residual_, _ = _here(x, W, bias, residual, out)
     if out is None:
         out = x.new_empty((T, N)) if residual is None else torch.empty_like(residual)
-    else:
-        _check_out(out, (T, N), W.dtype)
     pre = torch.empty_like(out) if keep_pre and act != ACT_NONE else None
     nbytes = lib().moe_linear_workspace_bytes(T, K, N, code)
     ws = torch.empty((nbytes,), dtype=torch.uint8, device=W.device) if nbytes else None
-    x_, W_, bias_, residual_, ws_, pre_, out_ = _here(x, W, bias, residual, ws, pre, out)
-    _check(lib().moe_linear(x_, W_, bias_, act, residual_, code, T, K, N, ws_, nbytes, pre_, out_, _stream()), "moe_linear")
+    _check(lib().moe_linear(x_, W_, bias_, act, residual_, code, T, K, N, _at(ws), nbytes, _at(pre), out.data_ptr(), _stream()), "moe_linear")
     return (out, pre) if keep_pre else out
 
 
@@ -989,13 +993,13 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, act: int
     _as_stored(dy, W, "dy", T, N)
     if pre is not None:
         _as_stored(pre, W, "pre", T, N)
+    dy_, x_, W_, pre_ = _here(dy, x, W, pre)
     nbytes = lib().moe_linear_backward_workspace_bytes(T, K, N, act, code)
     if nbytes == 0:
         raise MoEError(UNSUPPORTED, "moe_linear_backward_workspace_bytes")
     ws = torch.empty((nbytes,), dtype=torch.uint8, device=W.device)
     g = dict(dx=torch.empty_like(x) if want_dx else None, dW=torch.empty_like(W) if want_dW else None, db=W.new_empty((N,)) if want_db else None)
-    dy_, x_, W_, pre_, ws_, *out = _here(dy, x, W, pre, ws, *g.values())
-    _check(lib().moe_linear_backward(dy_, x_, W_, pre_, act, code, T, K, N, ws_, nbytes, *out, _stream()), "moe_linear_backward")
+    _check(lib().moe_linear_backward(dy_, x_, W_, pre_, act, code, T, K, N, ws.data_ptr(), nbytes, _at(g["dx"]), _at(g["dW"]), _at(g["db"]), _stream()), "moe_linear_backward")
     return g
 
 
