@@ -448,3 +448,71 @@ def test_in_a_graph_and_on_another_stream(moe, dtype):
         torch.cuda.synchronize()
         eager = step()
         assert all(torch.equal(a, b) for a, b in zip(captured, eager)), f"replay {i}"
+
+
+# Sizes whose launches share a reduction through a workspace, forward (few rows, many columns) and backward (many rows, few columns), and those of the tiles of one stage
+SHARED = [(40, 4096, 256), (6000, 256, 264), (3000, 264, 776)]
+
+
+def a_step(moe, x, W, b, res, dy, act):
+    out, pre = moe.linear(x, W, b, act, residual=res, keep_pre=True)
+    g = moe.linear_backward(dy, x, W, act, pre)
+    return [out, pre, g["dx"], g["dW"], g["db"]]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_two_graphs_and_eager_calls_in_between(moe, dtype):
+    """Two captured steps, replayed in turn on inputs that change, with eager steps and a synchronization in between: every replay has the eager result's bits."""
+    rng = np.random.default_rng(9)
+    for T, K, N in SHARED:
+        sets = [[draw(rng, s, dtype)[0] for s in ((T, K), (K, N), (N,), (T, N), (T, N))] for _ in range(2)]
+        for s in sets:
+            a_step(moe, *s, moe.ACT_SILU)
+        torch.cuda.synchronize()
+        graphs = []
+        for s in sets:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                graphs.append((graph, s, a_step(moe, *s, moe.ACT_SILU)))
+        for i in range(3):
+            for graph, s, _ in graphs:
+                s[0].mul_(1.0 + 0.125 * i)
+                graph.replay()
+            torch.cuda.synchronize()
+            for j, (_, s, captured) in enumerate(graphs):
+                assert all(torch.equal(a, b) for a, b in zip(captured, a_step(moe, *s, moe.ACT_SILU))), f"{T} x {K} x {N}: graph {j}, replay {i}"
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_two_streams_at_a_time(moe, dtype):
+    """Steps on two streams at once, several of each, have the bits of one by itself."""
+    rng = np.random.default_rng(10)
+    for T, K, N in SHARED:
+        sets = [[draw(rng, s, dtype)[0] for s in ((T, K), (K, N), (N,), (T, N), (T, N))] for _ in range(2)]
+        alone = [a_step(moe, *s, moe.ACT_GELU) for s in sets]
+        torch.cuda.synchronize()
+        streams = [torch.cuda.Stream() for _ in sets]
+        results = [[], []]
+        for _ in range(4):
+            for s, stream, r in zip(sets, streams, results):
+                with torch.cuda.stream(stream):
+                    r.append(a_step(moe, *s, moe.ACT_GELU))
+        torch.cuda.synchronize()
+        for want, r in zip(alone, results):
+            assert all(torch.equal(a, b) for got in r for a, b in zip(got, want)), f"{T} x {K} x {N}"
+
+
+@pytest.mark.parametrize("T", [1, 300, 9000])
+def test_nan_and_infinity_stay_in_their_rows(moe, T):
+    """A NaN or an infinity in one row of x reaches that row of the result and no other, at edges of tiles; ReLU keeps a NaN."""
+    K, N = 328, 264
+    x = torch.zeros((T, K), dtype=BF, device="cuda")
+    W = torch.ones((K, N), dtype=BF, device="cuda")
+    x[T - 1, K - 1] = float("nan")
+    x[T // 2, 0] = float("inf") if T > 1 else float("nan")
+    for act in (moe.ACT_NONE, moe.ACT_RELU, moe.ACT_GELU, moe.ACT_SILU):
+        out = moe.linear(x, W, act=act).float()
+        assert out[T - 1].isnan().all()
+        rest = torch.ones(T, dtype=torch.bool, device="cuda")
+        rest[T - 1] = rest[T // 2] = False
+        assert (out[rest] == 0).all() and (T == 1 or out[T // 2].isinf().all())
