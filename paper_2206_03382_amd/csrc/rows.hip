@@ -281,103 +281,152 @@ __global__ __launch_bounds__(256) void ragged_combine_backward_kernel(const uint
 }
 
 // ---- the activation's derivative and the bias gradient ---------------------------------------------------------------------
-// dp[r] = dy[r] * act'(pre[r]) and, in the same pass, db[e] = sum of dp over the expert's rows.  A block has a strip of 32 groups (512 bytes of bf16: 80 us for 32768 x
-// 2048, 8 experts, where strips of 256 and 1024 bytes take 94 and 86) and a slice of an expert's rows; 8 classes of rows, each summed in ascending order by one thread, then class by class, then, by a second launch, slice by slice: in an order that the sizes fix.  The sums are of
-// dp before its rounding.  dp is rounded to the storage type: the matrix cores take it as an operand.
+// dp[r] = dy[r] * act'(pre[r]) and, in the same pass, db[e] = sum of dp over the expert's rows.  A block has a strip of 32 groups (512 bytes of bf16: 80 us for 32768 x 2048, where strips of
+// 256 and 1024 bytes take 94 and 86) and a chunk of rows, whoever's they are, so that a gate that gives most rows to few experts costs nothing.  It goes through the experts' pieces of its
+// chunk: 8 classes of rows, each summed in ascending order by one thread, then class by class.  An expert whose rows all lie in one chunk has its sum; of one that goes on in
+// another, the chunk keeps the sum of the piece, `head` if the expert began before the chunk, `tail` if it begins in it, and a second launch adds those up in order.  The order is fixed by sizes and
+// offsets.  The sums are of dp before its rounding.  dp is rounded to the storage type: the matrix cores take it as an operand.
+// Slices of every expert's rows instead, however many there are, took 217 us for 32768 rows of 64 experts x 1024 under a Zipf-shaped gate where this takes 55.
 constexpr int kStrip = 32, kClasses = 8;
 
 __device__ __forceinline__ int64_t clamp_row(int64_t v, int64_t R) { return v < 0 ? 0 : (v < R ? v : R); }
 
-template <typename ET, int ACT, bool SUM>
-__global__ __launch_bounds__(256) void rows_act_backward_kernel(const uint4* __restrict__ dy, const uint4* __restrict__ pre, const int32_t* __restrict__ offsets, int64_t R, int groups,
-                                                                int slices, uint4* __restrict__ dp, float* __restrict__ sums, ET* __restrict__ db) {
-  constexpr int P = kPieces<ET>;
-  __shared__ float part[kClasses][kStrip * kGroup + 1];
-  const int e = blockIdx.y, slice = blockIdx.z;
-  const int64_t lo = offsets ? clamp_row(offsets[e], R) : 0, end = offsets ? clamp_row(offsets[e + 1], R) : R;
-  const int64_t each = (end - lo + slices - 1) / slices;
-  const int64_t from = lo + slice * each, to = from + each < end ? from + each : end;
-  const int cls = threadIdx.x / kStrip, g = blockIdx.x * kStrip + threadIdx.x % kStrip;
-  float s[kGroup];
-#pragma unroll
-  for (int i = 0; i < kGroup; ++i) s[i] = 0.f;
-  if (g < groups) {
-    constexpr int U = 4;                                            // rows of a class in flight
-    auto one = [&](int64_t at, const Group<ET>& a, const Group<ET>& b) __attribute__((always_inline)) {
-      float v[kGroup], p[kGroup];
-      unpack_group<ET>(a, v);
-      if (ACT >= 0) {
-        unpack_group<ET>(b, p);
-#pragma unroll
-        for (int i = 0; i < kGroup; ++i) v[i] *= rows_act_grad_as<ET, ACT>(p[i]);
-        store_group<ET>(dp + at, v);
-      }
-      if (SUM) {
-#pragma unroll
-        for (int i = 0; i < kGroup; ++i) s[i] += v[i];
-      }
-    };
-    int64_t r = from + cls;
-    for (; r + (U - 1) * kClasses < to; r += U * kClasses) {
-      Group<ET> a[U], b[U];
-#pragma unroll
-      for (int i = 0; i < U; ++i) a[i] = load_group<ET, false>(dy + ((r + i * kClasses) * groups + g) * P);
-#pragma unroll
-      for (int i = 0; i < U; ++i)
-        if (ACT >= 0) b[i] = load_group<ET, false>(pre + ((r + i * kClasses) * groups + g) * P);
-#pragma unroll
-      for (int i = 0; i < U; ++i) one(((r + i * kClasses) * groups + g) * P, a[i], b[i]);
-    }
-    for (; r < to; r += kClasses) {
-      const int64_t at = (r * groups + g) * P;
-      const Group<ET> a = load_group<ET, false>(dy + at);
-      Group<ET> b;
-      if (ACT >= 0) b = load_group<ET, false>(pre + at);
-      one(at, a, b);
-    }
+// The first expert from e on whose rows end behind `row`, the same in every lane, and where they lie; E if there is none.  Without offsets there is one expert.
+__device__ __forceinline__ int expert_behind(const int32_t* __restrict__ offsets, int e, int E, int64_t R, int64_t row, int64_t& lo, int64_t& hi) {
+  if (!offsets) {
+    lo = 0, hi = R;
+    return e < 1 && row < R ? 0 : 1;
   }
-  if (SUM) {
-#pragma unroll
-    for (int i = 0; i < kGroup; ++i) part[cls][threadIdx.x % kStrip * kGroup + i] = s[i];
-    __syncthreads();
-    const int col = blockIdx.x * kStrip * kGroup + threadIdx.x;
-    static_assert(kStrip * kGroup == 256, "a column to a thread");
-    if (col < groups * kGroup) {
-      float t = 0.f;
-#pragma unroll
-      for (int c = 0; c < kClasses; ++c) t += part[c][threadIdx.x];
-      if (slices == 1) store_from_f32<ET>(db + (int64_t)e * groups * kGroup + col, t);
-      else sums[((int64_t)slice * gridDim.y + e) * groups * kGroup + col] = t;
-    }
+  const int lane = threadIdx.x & 63;
+  for (; e < E; e += 64) {
+    const int x = e + lane < E ? e + lane : E - 1;
+    const int64_t end = clamp_row(offsets[x + 1], R), from = clamp_row(offsets[x], R);
+    const unsigned long long hit = __ballot(e + lane < E && end > row && end > from);
+    if (hit == 0) continue;
+    const int l = __builtin_ctzll(hit);
+    lo = __shfl(from, l, 64), hi = __shfl(end, l, 64);
+    return e + l;
   }
+  return E;
 }
 
-// db[i] = the sum of the slices' sums, n of them apart.  A block has 64 columns and a quarter of the slices to a wave: one thread for 64 slices was a chain of loads, 17 us for
-// 2048 columns.
-template <typename ET>
-__global__ __launch_bounds__(256) void slice_sum_kernel(const float* __restrict__ sums, int slices, int64_t n, ET* __restrict__ db) {
-  __shared__ float part[4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t i = (int64_t)blockIdx.x * 64 + lane;
+template <typename ET, int ACT, bool SUM>
+__global__ __launch_bounds__(256) void rows_act_backward_kernel(const uint4* __restrict__ dy, const uint4* __restrict__ pre, const int32_t* __restrict__ offsets, int64_t R, int E,
+                                                                int groups, int64_t chunk, uint4* __restrict__ dp, float* __restrict__ sums, ET* __restrict__ db) {
+  constexpr int P = kPieces<ET>;
+  static_assert(kStrip * kGroup == 256 && kStrip * kClasses == 256, "a column, and a group of a class, to a thread");
+  __shared__ float part[kClasses][kStrip * kGroup + 1];
+  const int64_t from = blockIdx.y * chunk, to = from + chunk < R ? from + chunk : R, N = (int64_t)groups * kGroup;
+  const int cls = threadIdx.x / kStrip, g = blockIdx.x * kStrip + threadIdx.x % kStrip;
+  const int64_t col = (int64_t)blockIdx.x * kStrip * kGroup + threadIdx.x;
+  int64_t lo, hi;
+  int e = 0, known = 0;                                             // experts below `known` have their sums, if all rows are in this chunk
+  for (int64_t row = from; row < to;) {
+    e = expert_behind(offsets, e, E, R, row, lo, hi);
+    if (e >= E) break;
+    const int64_t begin = lo > row ? lo : row, end = hi < to ? hi : to;
+    if (begin >= to) break;
+    float s[kGroup];
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i) s[i] = 0.f;
+    if (g < groups) {
+      constexpr int U = 4;                                          // rows of a class in flight
+      auto one = [&](int64_t at, const Group<ET>& a, const Group<ET>& b) __attribute__((always_inline)) {
+        float v[kGroup], p[kGroup];
+        unpack_group<ET>(a, v);
+        if (ACT >= 0) {
+          unpack_group<ET>(b, p);
+#pragma unroll
+          for (int i = 0; i < kGroup; ++i) v[i] *= rows_act_grad_as<ET, ACT>(p[i]);
+          store_group<ET>(dp + at, v);
+        }
+        if (SUM) {
+#pragma unroll
+          for (int i = 0; i < kGroup; ++i) s[i] += v[i];
+        }
+      };
+      int64_t r = begin + cls;
+      for (; r + (U - 1) * kClasses < end; r += U * kClasses) {
+        Group<ET> a[U], b[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) a[i] = load_group<ET, false>(dy + ((r + i * kClasses) * groups + g) * P);
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+          if (ACT >= 0) b[i] = load_group<ET, false>(pre + ((r + i * kClasses) * groups + g) * P);
+#pragma unroll
+        for (int i = 0; i < U; ++i) one(((r + i * kClasses) * groups + g) * P, a[i], b[i]);
+      }
+      for (; r < end; r += kClasses) {
+        const int64_t at = (r * groups + g) * P;
+        const Group<ET> a = load_group<ET, false>(dy + at);
+        Group<ET> b;
+        if (ACT >= 0) b = load_group<ET, false>(pre + at);
+        one(at, a, b);
+      }
+    }
+    if (SUM) {
+#pragma unroll
+      for (int i = 0; i < kGroup; ++i) part[cls][threadIdx.x % kStrip * kGroup + i] = s[i];
+      __syncthreads();
+      if (col < N) {
+        float t = 0.f;
+#pragma unroll
+        for (int c = 0; c < kClasses; ++c) t += part[c][threadIdx.x];
+        if (lo >= from && hi <= to) store_from_f32<ET>(db + e * N + col, t);
+        else sums[(blockIdx.y * 2 + (lo < from ? 0 : 1)) * N + col] = t;             // head, tail
+        if (gridDim.y == 1)                                         // no second launch: experts without rows
+          for (; known < e; ++known) store_from_f32<ET>(db + known * N + col, 0.f);
+        known = e + 1;
+      }
+      __syncthreads();
+    }
+    row = end;
+    ++e;
+  }
+  if (SUM && gridDim.y == 1 && col < N)
+    for (; known < E; ++known) store_from_f32<ET>(db + known * N + col, 0.f);
+}
+
+// db of the experts whose rows lie in several chunks, and of those without any.  A block has 64 columns of an expert and a part of its chunks to each of its waves: one thread for 64 was
+// a chain of loads, 17 us for 2048 columns.  16 waves where experts have more than 8 chunks in the mean (32768 rows x 256 of one expert, in all: 17 us, with 4 waves 30), 4 below (2048 rows
+// of 128 experts x 1024: 16 us, with 16 waves 21).
+template <typename ET, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void chunk_sum_kernel(const float* __restrict__ sums, const int32_t* __restrict__ offsets, int64_t R, int64_t chunk, int64_t N, ET* __restrict__ db) {
+  __shared__ float part[WAVES][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e = blockIdx.y;
+  const int64_t i = (int64_t)blockIdx.x * 64 + lane, lo = offsets ? clamp_row(offsets[e], R) : 0, hi = offsets ? clamp_row(offsets[e + 1], R) : R;
+  if (hi <= lo) {
+    if (wave == 0 && i < N) store_from_f32<ET>(db + e * N + i, 0.f);
+    return;
+  }
+  const int64_t first = lo / chunk, last = (hi - 1) / chunk, n = last - first + 1;
+  if (n == 1) return;
   float t = 0.f;
-  if (i < n) {
-    const int to = (wave + 1) * slices / 4;
+  if (i < N) {
+    const int64_t to = first + (wave + 1) * n / WAVES;
 #pragma unroll 8
-    for (int s = wave * slices / 4; s < to; ++s) t += sums[s * n + i];
+    for (int64_t c = first + wave * n / WAVES; c < to; ++c) t += sums[(c * 2 + (c * chunk <= lo ? 1 : 0)) * N + i];
   }
   part[wave][lane] = t;
   __syncthreads();
-  if (wave == 0 && i < n) store_from_f32<ET>(db + i, part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane]);
+  if (wave == 0 && i < N) {
+    t = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) t += part[w][lane];
+    store_from_f32<ET>(db + e * N + i, t);
+  }
 }
 
-// Slices of an expert's rows: about 32 blocks to a unit, no fewer than 8 rows on average, at most 128; one below 64 rows on average, which saves the second launch.  As many because a
-// skewed gate gives most rows to few experts, which the host cannot know: 32768 rows of 64 experts x 1024, Zipf-shaped 217 us with eight blocks to a unit, 72 so (an even gate of 8 x 4096 x
-// 2048 86 and 88); 3002 fp32 rows of 17 x 1544 with GeLU', 220 with no slice below 64 rows, 38 so.
-int act_backward_slices(int64_t R, int64_t E, int64_t N) {
-  const int64_t strips = ceil_div(N / kGroup, kStrip);
-  int64_t n = ceil_div(8192, strips * E), mean = ceil_div(R, E), most = mean < 64 ? 1 : mean / 8;
-  n = n < most ? n : most;
-  return (int)(n < 1 ? 1 : (n > 128 ? 128 : n));
+// Rows of a chunk: all of up to 128 with eight experts' pieces at most, which need no second launch (128 rows of one expert x 1024: 11.4 us, in two launches 14.6; but 128 rows of 128
+// experts x 2048, piece behind piece: 112 us, in chunks of 16 rows 23, of 4 15).  Else as few as leave the second launch little to add (8192 x 2048 of one expert: 16 rows to a chunk 24.8 us, 32 23.6, 64
+// 21.7, 256 26.7; 3002 rows of 17 experts x 1544, fp32: 22.7, 30, 38, 58) and the first about 4096 blocks.
+int64_t act_backward_chunk(int64_t R, int64_t E, int64_t N) {
+  if (R <= 128 && (R < E ? R : E) <= 8) return 128;
+  int64_t chunk = 4;
+  while (chunk < 16 && ceil_div(R, chunk) > 64) chunk *= 2;
+  while (chunk < 64 && ceil_div(R, chunk) > 192) chunk *= 2;
+  while ((chunk < 256 && ceil_div(R, chunk) * ceil_div(N / kGroup, kStrip) > 4096) || ceil_div(R, chunk) > 65535) chunk *= 2;      // and no more chunks than a grid's second dimension has
+  return chunk;
 }
 
 unsigned blocks_for(int64_t work, int64_t per_block, int64_t most) {
@@ -467,17 +516,18 @@ hipError_t launch_ragged_combine_backward(const void* d_out, const void* Y, int6
 }
 
 size_t rows_act_backward_bytes(int64_t R, int64_t E, int64_t N) {
-  const int slices = act_backward_slices(R, E, N);
-  return slices > 1 ? (size_t)slices * E * N * 4 : 0;
+  const int64_t chunks = ceil_div(R, act_backward_chunk(R, E, N));
+  return chunks > 1 ? (size_t)chunks * 2 * N * 4 : 0;
 }
 
 hipError_t launch_rows_act_backward(const void* dy, const void* pre, int act, int dtype, const int32_t* offsets, int64_t R, int64_t E, int64_t N, void* ws, void* dp,
                                     void* db, hipStream_t s) {
   if (act < 0 && !db) return hipSuccess;
-  const int groups = (int)(N / kGroup), slices = act_backward_slices(R, E, N);
-  const dim3 grid((unsigned)ceil_div(groups, kStrip), (unsigned)E, (unsigned)slices), block(256);
+  const int groups = (int)(N / kGroup);
+  const int64_t chunk = act_backward_chunk(R, E, N), chunks = ceil_div(R, chunk);
+  const dim3 grid((unsigned)ceil_div(groups, kStrip), (unsigned)chunks), block(256);
 #define MOE_LAUNCH_ACT(ET, ACT, SUM) \
-  rows_act_backward_kernel<ET, ACT, SUM><<<grid, block, 0, s>>>((const uint4*)dy, (const uint4*)pre, offsets, R, groups, slices, (uint4*)dp, (float*)ws, (ET*)db)
+  rows_act_backward_kernel<ET, ACT, SUM><<<grid, block, 0, s>>>((const uint4*)dy, (const uint4*)pre, offsets, R, (int)E, groups, chunk, (uint4*)dp, (float*)ws, (ET*)db)
 #define MOE_LAUNCH_ACT_SUM(ET, ACT)              \
   do {                                           \
     if (db) MOE_LAUNCH_ACT(ET, ACT, true);       \
@@ -498,10 +548,16 @@ hipError_t launch_rows_act_backward(const void* dy, const void* pre, int act, in
 #undef MOE_LAUNCH_ACT_SUM
 #undef MOE_LAUNCH_ACT
   if (hipError_t err = hipGetLastError()) return err;
-  if (!db || slices == 1) return hipSuccess;
-  const int64_t n = E * N;
-  if (dtype == MOE_F32) slice_sum_kernel<float><<<dim3((unsigned)ceil_div(n, 64)), dim3(256), 0, s>>>((const float*)ws, slices, n, (float*)db);
-  else slice_sum_kernel<uint16_t><<<dim3((unsigned)ceil_div(n, 64)), dim3(256), 0, s>>>((const float*)ws, slices, n, (uint16_t*)db);
+  if (!db || chunks == 1) return hipSuccess;
+  const dim3 sum_grid((unsigned)ceil_div(N, 64), (unsigned)E);
+#define MOE_LAUNCH_CHUNK_SUM(ET)                                                                                                                                  \
+  do {                                                                                                                                                            \
+    if (chunks > 8 * E) chunk_sum_kernel<ET, 16><<<sum_grid, dim3(1024), 0, s>>>((const float*)ws, offsets, R, chunk, N, (ET*)db);                                \
+    else chunk_sum_kernel<ET, 4><<<sum_grid, dim3(256), 0, s>>>((const float*)ws, offsets, R, chunk, N, (ET*)db);                                                 \
+  } while (0)
+  if (dtype == MOE_F32) MOE_LAUNCH_CHUNK_SUM(float);
+  else MOE_LAUNCH_CHUNK_SUM(uint16_t);
+#undef MOE_LAUNCH_CHUNK_SUM
   return hipGetLastError();
 }
 

@@ -5,7 +5,7 @@ the partial sum, 2^-23, each, then one addition of 2^-24 to the chain: (32 * 2^-
 rounded: K * 2^-24 of S, and four parts' sums more where the reduction is split.  An activation's slope is at most 1.13; its own error is 5e-5 of the value for bf16 results (GeLU's fit; SiLU 2e-6 + |v| 2^-23 of the exponential's
 argument), 16 roundings of fp32 for fp32 results, whose erfc is near 0 by way of its argument's rounding: |v| 2^-23 of the exponent v^2 / 2 more.  Each result is rounded once, half a step: 2^-8 or 2^-24 of it.
 Gradients go by the stored pre-activations.  dp is rounded to the storage type, so every term of a sum may be off by 2^-8 (2^-24) and the derivative's error, 2e-5 absolute for bf16, 16 * 2^-24 for fp32 on top of the
-exponent's; R rows are added like K products, in slices for db.
+exponent's; R rows are added like K products, in chunks for db.
 """
 import numpy as np
 import pytest
@@ -151,6 +151,35 @@ def test_ragged_product_and_gradients(moe, R, E, K, N, kind, behind, dtype):
         only = moe.ragged_matmul_backward(dy, A, W, off, ACT[act], None if act == "none" else pre, gather=gather, **{f"want_{w}": w == want for w in ("dx", "dW", "db")})
         rows = slice(0, R) if want == "dx" else slice(None)
         assert torch.equal(only[want][rows], g[want][rows]) and sum(t is not None for t in only.values()) == 1
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("kind", ["one", "even", "skewed", "gaps"])
+@pytest.mark.parametrize("R,E,N", [(1, 300, 64), (8, 40, 264), (9, 40, 264), (128, 8, 72), (128, 9, 72), (129, 2, 520), (257, 200, 64), (513, 5, 264), (2049, 33, 64), (12300, 70, 64), (50000, 3, 1288)])
+def test_bias_gradient_of_experts_that_share_or_cross_chunks(moe, R, E, N, kind, dtype):
+    """A few rows and many experts, a hot expert among small ones, experts without rows in front, between and behind; rows behind the last one are not read."""
+    rng = np.random.default_rng(R + 7 * E + N)
+    share = {"one": np.eye(1, E, E // 2)[0], "even": np.ones(E), "skewed": 1.0 / np.arange(1, E + 1) ** 2, "gaps": (np.arange(E) % 3 == 1) + 1e-9}[kind]
+    fills = np.bincount(rng.choice(E, R, p=share / share.sum()), minlength=E)
+    if kind == "even" and R >= E:
+        fills = np.full(E, R // E)                                   # borders on those of the chunks, where these divide
+    offsets = np.concatenate([[0], np.cumsum(fills)]).astype(np.int32)
+    used, behind = int(offsets[-1]), 70
+    off = torch.from_numpy(offsets).cuda()
+    dy, dy64 = draw(rng, (used + behind, N), dtype)
+    pre, p64 = draw(rng, (used + behind, N), dtype)
+    dy[used:], pre[used:] = float("nan"), float("nan")
+    A = torch.zeros(used + behind, 64, dtype=dtype, device="cuda")
+    W = torch.zeros(E, 64, N, dtype=dtype, device="cuda")
+    d64 = dy64[:used] * (p64[:used] > 0)                             # exact in the storage type
+    ids = np.repeat(np.arange(E), fills)
+    want, size = np.zeros((E, N)), np.zeros((E, N))
+    for e in np.unique(ids):
+        want[e], size[e] = d64[offsets[e]:offsets[e + 1]].sum(0), np.abs(d64[offsets[e]:offsets[e + 1]]).sum(0)
+    got = moe.ragged_matmul_backward(dy, A, W, off, ACT["relu"], pre, want_dx=False, want_dW=False)["db"]
+    assert_within(got, want, (int(fills.max()) / 8 + 96) * 2.0 ** -24 * size + HALF[dtype] * np.abs(want), "db")
+    again = moe.ragged_matmul_backward(dy, A, W, off, ACT["relu"], pre, want_dx=False, want_dW=False)["db"]
+    assert torch.equal(got, again)
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
