@@ -346,7 +346,8 @@ static inline Tile choose_tile(int mode, bool large_ok, bool half_ok, int64_t E,
 // N = 512: K = 32 4.8 us there, 5.5 here, 64 5.5 and 5.9, 96 6.0 and 6.0, 128 6.5 and 6.3, 256 8.6 and 7.7.  Only the sizes of the buffers
 // decide, so that every route to a product sums alike.
 constexpr int kSplitTile = 32, kSplitParts = 4;
-static inline bool fp32_split(int64_t E, int64_t C, int64_t K, int64_t N) { return K > 64 && E * tiles_in(C, kSplitTile) * tiles_in(N, kSplitTile) <= 512; }
+static inline bool fp32_split(int64_t row_tiles, int64_t K, int64_t N) { return K > 64 && row_tiles * tiles_in(N, kSplitTile) <= 512; }
+static inline bool fp32_split(int64_t E, int64_t C, int64_t K, int64_t N) { return fp32_split(E * tiles_in(C, kSplitTile), K, N); }
 
 // Rows an expert holds on average: the caller's hint, or all of them.
 static inline double mean_or(int64_t rows_hint, int64_t C) { return (double)(rows_hint > 0 && rows_hint < C ? rows_hint : C); }

@@ -36,9 +36,15 @@ bool large_takes(int64_t E, int64_t K, int64_t N, int64_t gather_rows, int64_t g
   return K % kLargeK == 0 && N % kLargeTile == 0 && E <= kMaxExperts && gather_rows * gather_width * 2 < ((int64_t)1 << 32);
 }
 
-// The products on tiles below the large one.  fp32 of few tiles: the reduction of 32 x 32 cut among a block's waves (fp32_split).
+// The products on tiles below the large one.  fp32 of few tiles that can have rows: the reduction of 32 x 32 cut among a block's waves (fp32_split).  168 rows of 6 experts, 2856 x 528,
+// which have 11 such row tiles at most: 53 us on the tiles of 64 x 64 that experts full of rows would want, 23 so.
 template <int MODE> hipError_t launch_small_rows(int dtype, Tile tile, const TileArgs& t, int64_t total, hipStream_t s) {
-  if (dtype == MOE_F32 && (MODE == kTN || !fp32_split(t.E, t.C, t.K, t.N))) return launch_rows_fp32<MODE>(t, total, s);
+  if (dtype == MOE_F32) {
+    if constexpr (MODE != kTN) {
+      if (fp32_split(live_row_tiles(t.E, t.C, total, kSplitTile), t.K, t.N)) return launch_tile<float, MODE, kSplitTile, kSplitTile, 2, false, kSplitParts, true>(t, total, s);
+    }
+    return launch_rows_fp32<MODE>(t, total, s);
+  }
   return launch_small<MODE, true>(dtype, tile, t, total, s);
 }
 
