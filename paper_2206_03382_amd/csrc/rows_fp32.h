@@ -45,7 +45,18 @@ __global__ __launch_bounds__(256, 5) void rows_fp32_kernel(const TileArgs p) {
     first += from;
     kend = kend - from < each ? kend - from : each;
   }
-  const int KT = kend > 0 ? (int)((kend + BKE - 1) / BKE) : 1;
+  const int64_t tile_at = (MODE == kTN ? ((p.parts > 1 ? (int64_t)blockIdx.z * p.E : 0) + e) * p.C : first) + m0;        // its first row among the results'
+  if (MODE == kTN && kend <= 0) {                                   // no rows: zeros, at once (16 such experts of 776 x 1544: 15 us, by way of a K-step of zeros 28)
+    float* out = p.parts > 1 ? p.part_sums : (float*)p.out;
+    const int64_t col = n0 + (threadIdx.x & 15) * 4;
+#pragma unroll
+    for (int q = 0; q < T / 16; ++q) {
+      const int r = q * 16 + (int)(threadIdx.x >> 4);
+      if (m0 + r < p.C && col < p.N) *reinterpret_cast<f32x4*>(out + (tile_at + r) * p.N + col) = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    return;
+  }
+  const int KT = (int)((kend + BKE - 1) / BKE);
 
   // ---- this lane's direct loads.  k-contiguous: block q * 4 + wave = 8 rows, lane l row + l / 8, position l % 8.  k-slow: pieces of 4 columns in order.
   auto fast_row = [&](int q) -> int { return (q * 4 + wave) * 8 + (lane >> 3); };
@@ -255,7 +266,7 @@ __global__ __launch_bounds__(256, 5) void rows_fp32_kernel(const TileArgs p) {
         for (int i = 0; i < R; ++i) acc[i][(4 * g + x) % R][(4 * g + x) / R] += b[x];
     }
   }
-  const int64_t out_at = ((MODE == kTN ? ((p.parts > 1 ? (int64_t)blockIdx.z * p.E : 0) + e) * p.C : first) + m0 + wm * WT) * p.N;
+  const int64_t out_at = (tile_at + wm * WT) * p.N;
   const float* with = MODE == kTN ? nullptr : (const float*)p.pre;
   auto write_rows = [&](auto act_tag, float* dst, const float* add) __attribute__((always_inline)) {
     constexpr int ACT = decltype(act_tag)::value;
