@@ -5,6 +5,7 @@
 #include "ffn_device.h"
 #include "rows.h"
 #include "rows_act.h"
+#include "rows_rules.h"
 
 namespace moe {
 namespace {
@@ -29,28 +30,16 @@ namespace moe {
 
 namespace {
 
-int64_t mean_rows(int64_t R, int64_t E) { return ceil_div(R, E); }
-
-// Whether the large tile takes a product of K x N weights; gather_rows > 0: of rows of so many elements that 32-bit offsets reach.
-bool large_takes(int64_t E, int64_t K, int64_t N, int64_t gather_rows, int64_t gather_width) {
-  return K % kLargeK == 0 && N % kLargeTile == 0 && E <= kMaxExperts && gather_rows * gather_width * 2 < ((int64_t)1 << 32);
-}
-
-// The products on tiles below the large one.  fp32 of few tiles that can have rows: the reduction of 32 x 32 cut among a block's waves (fp32_split).  168 rows of 6 experts, 2856 x 528,
-// which have 11 such row tiles at most: 53 us on the tiles of 64 x 64 that experts full of rows would want, 23 so.
-template <int MODE> hipError_t launch_small_rows(int dtype, Tile tile, const TileArgs& t, int64_t total, hipStream_t s) {
-  if (dtype == MOE_F32) {
-    if constexpr (MODE != kTN) {
-      if (fp32_split(live_row_tiles(t.E, t.C, total, kSplitTile), t.K, t.N)) return launch_tile<float, MODE, kSplitTile, kSplitTile, 2, false, kSplitParts, true>(t, total, s);
-    }
-    return launch_rows_fp32<MODE>(t, total, s);
+// The products on tiles below the large one.
+template <int MODE> hipError_t launch_small_rows(int dtype, const RowsPlan& plan, const TileArgs& t, int64_t total, hipStream_t s) {
+  if constexpr (MODE != kTN) {
+    if (plan.kernel == RowsKernel::kShort) return launch_short<MODE>(t, total, s);
+    if (plan.kernel == RowsKernel::kFp32Split) return launch_tile<float, MODE, kSplitTile, kSplitTile, 2, false, kSplitParts, true>(t, total, s);
   }
-  return launch_small<MODE, true>(dtype, tile, t, total, s);
+  if (dtype == MOE_F32) return launch_rows_fp32<MODE>(t, total, s);
+  return launch_small<MODE, true>(dtype, plan.tile, t, total, s);
 }
-
-Tile rows_tile(int mode, int dtype, bool large_ok, int64_t E, int64_t rows, double mean, int64_t K, int64_t N, bool gathered) {
-  return dtype == MOE_BF16 ? choose_tile(mode, large_ok, false, E, rows, mean, K, N, gathered, true) : Tile::k64;
-}
+bool is_large(const RowsPlan& plan) { return plan.kernel == RowsKernel::kTile && plan.tile == Tile::k256; }
 
 }  // namespace
 
@@ -63,13 +52,9 @@ size_t rows_product_bytes(int dtype, int64_t R, int64_t K, int64_t N) {
 hipError_t launch_rows_product(const RowsProduct& p, void* ws, hipStream_t s) {
   const bool dual = p.pre && p.act >= 0;
   const TileArgs t = {p.A, p.W, p.bias, p.offsets, p.gather, p.gather_rows, p.R, p.K, (int)p.N, (int)p.E, 0, 0, 0, p.out, nullptr, p.residual, p.pre, p.act, 0};
-  if (p.dtype == MOE_BF16) {
-    const ThinPlan plan = thin_plan(p.offsets != nullptr, p.E, p.R, p.K, p.N);
-    if (plan.ri > 0) return launch_thin(t, plan, (float*)ws, s);
-  }
-  const Tile tile = rows_tile(kNN, p.dtype, large_takes(p.E, p.K, p.N, p.gather ? p.gather_rows : 0, p.K), p.E, p.R, (double)mean_rows(p.R, p.E), p.K, p.N, p.gather != nullptr);
-  if (p.dtype == MOE_BF16 && short_takes(tile, (p.R / 128) * tiles_in(p.N, 128), p.K, p.act >= 0, p.residual || p.pre)) return launch_short<kNN>(t, p.R, s);
-  if (tile != Tile::k256) return launch_small_rows<kNN>(p.dtype, tile, t, p.R, s);
+  const RowsPlan plan = product_plan(p.dtype == MOE_BF16, p.offsets != nullptr, p.E, p.R, p.K, p.N, p.gather ? p.gather_rows : 0, p.act >= 0, p.residual || p.pre);
+  if (plan.kernel == RowsKernel::kThin) return launch_thin(t, plan, (float*)ws, s);
+  if (!is_large(plan)) return launch_small_rows<kNN>(p.dtype, plan, t, p.R, s);
   const int MT = (int)ceil_div(p.R, BM), NT = (int)(p.N / BN);
   const int64_t blocks = tile_grid(NT, live_row_tiles(p.E, p.R, p.R, BM), true, false);
   if (blocks >= kMaxBlocks) return hipErrorInvalidValue;
@@ -98,10 +83,9 @@ hipError_t launch_rows_product(const RowsProduct& p, void* ws, hipStream_t s) {
 hipError_t launch_rows_product_nt(const void* d, const void* W, const void* x_pre, int x_act, int dtype, const int32_t* offsets, int64_t R, int64_t E, int64_t K,
                                   int64_t N, void* dx, hipStream_t s) {
   if (x_act < 0) x_pre = nullptr;
-  const Tile tile = rows_tile(kNT, dtype, large_takes(E, N, K, 0, 0), E, R, (double)mean_rows(R, E), N, K, false);
   const TileArgs t = {d, W, nullptr, offsets, nullptr, 0, R, N, (int)K, (int)E, 0, 0, 0, dx, nullptr, x_pre, nullptr, x_pre ? x_act : -1, 0};
-  if (dtype == MOE_BF16 && short_takes(tile, (R / 128) * tiles_in(K, 128), N, x_pre != nullptr, false)) return launch_short<kNT>(t, R, s);
-  if (tile != Tile::k256) return launch_small_rows<kNT>(dtype, tile, t, R, s);
+  const RowsPlan plan = product_nt_plan(dtype == MOE_BF16, E, R, K, N, x_pre != nullptr);
+  if (!is_large(plan)) return launch_small_rows<kNT>(dtype, plan, t, R, s);
   const int MT = (int)ceil_div(R, BM), NT = (int)(K / BN);
   const int64_t blocks = tile_grid(NT, live_row_tiles(E, R, R, BM), true, false);
   if (blocks >= kMaxBlocks) return hipErrorInvalidValue;
@@ -119,41 +103,26 @@ hipError_t launch_rows_product_nt(const void* d, const void* W, const void* x_pr
   return hipGetLastError();
 }
 
-namespace {
-
-bool weight_grad_large(int64_t E, int64_t K, int64_t N, int64_t gather_rows) {
-  return K % kLargeTile == 0 && N % kLargeTile == 0 && large_takes(E, K, N, gather_rows, K);
-}
-Tile weight_grad_tile(int dtype, int64_t R, int64_t E, int64_t K, int64_t N, bool gathered, int64_t gather_rows) {
-  return rows_tile(kTN, dtype, weight_grad_large(E, K, N, gathered ? gather_rows : 0), E, K, (double)mean_rows(R, E), R, N, gathered);
-}
-int weight_grad_shares(int dtype, int64_t R, int64_t E, int64_t K, int64_t N) {
-  return weight_grad_parts(dtype, weight_grad_large(E, K, N, 0), E, (double)mean_rows(R, E), K, N);
-}
-
-}  // namespace
-
-// Sums of the blocks that share a tile; or the large tile's last K-step of 64 rows, which comes from side buffers of both operands.
+// Sums of the blocks that share a tile; or the large tile's last K-step of 64 rows, which comes from side buffers of both operands.  Enough whether rows are gathered or not.
 size_t rows_weight_grad_bytes(int dtype, int64_t R, int64_t E, int64_t K, int64_t N) {
-  const int parts = weight_grad_shares(dtype, R, E, K, N);
-  if (parts > 1) return (size_t)parts * E * K * N * 4;
-  if (weight_grad_tile(dtype, R, E, K, N, false, 0) != Tile::k256 && weight_grad_tile(dtype, R, E, K, N, true, 1) != Tile::k256) return 0;
+  const RowsPlan in_place = weight_grad_plan(dtype == MOE_BF16, E, R, K, N, 0);
+  if (in_place.parts > 1) return (size_t)in_place.parts * E * K * N * 4;
+  if (!is_large(in_place) && !is_large(weight_grad_plan(dtype == MOE_BF16, E, R, K, N, 1))) return 0;
   return grouped_gemm_tn_tail_bytes(E, K) + grouped_gemm_tn_tail_bytes(E, N);
 }
 
 hipError_t launch_rows_weight_grad(const void* A, const int32_t* gather, int64_t gather_rows, const void* d, int dtype, const int32_t* offsets, int64_t R, int64_t E,
                                    int64_t K, int64_t N, void* ws, void* dW, hipStream_t s) {
-  const int parts = weight_grad_shares(dtype, R, E, K, N);
-  const Tile tile = weight_grad_tile(dtype, R, E, K, N, gather != nullptr, gather_rows);
+  const RowsPlan plan = weight_grad_plan(dtype == MOE_BF16, E, R, K, N, gather ? gather_rows : 0);
   TileArgs t = {A, d, nullptr, nullptr, gather, gather_rows, K, R, (int)N, (int)E, 0, 0, 0, dW, offsets, nullptr, nullptr, -1, 0};
-  if (parts > 1) {
-    t.parts = parts;
+  if (plan.parts > 1) {
+    t.parts = plan.parts;
     t.part_sums = (float*)ws;
-    if (hipError_t err = launch_small_rows<kTN>(dtype, Tile::k128, t, E * K, s)) return err;
+    if (hipError_t err = launch_small_rows<kTN>(dtype, plan, t, E * K, s)) return err;
     return join_parts(t, dtype, s);
   }
-  if (dtype == MOE_BF16 && outer_takes(E, (double)mean_rows(R, E), K, N)) return launch_outer(t, E * K, s);
-  if (tile != Tile::k256) return launch_small_rows<kTN>(dtype, tile, t, E * K, s);
+  if (plan.kernel == RowsKernel::kOuter) return launch_outer(t, E * K, s);
+  if (!is_large(plan)) return launch_small_rows<kTN>(dtype, plan, t, E * K, s);
   uint16_t* a_tail = (uint16_t*)ws;
   uint16_t* b_tail = a_tail + grouped_gemm_tn_tail_bytes(E, K) / 2;
   const TailRows ta = {(const uint4*)A, (uint4*)a_tail, gather, gather_rows, (int)(K / 8)}, tb = {(const uint4*)d, (uint4*)b_tail, nullptr, 0, (int)(N / 8)};

@@ -137,38 +137,4 @@ hipError_t join_parts(const TileArgs& p, int dtype, hipStream_t s) {
   return hipGetLastError();
 }
 
-// How many blocks share the reduction over an expert's rows: where the tiles of dW are too few to fill the chip.  Times in us, fitted to some 400 launches of this and of other numbers of
-// parts (E = 1 to 32, 256 to 4096 columns, 512 to 65536 rows): a launch 6; a K-step 0.46 of a 128 x 128 bf16 tile alone on its unit, 0.86 of two, 0.5 of a 64 x 64 fp32 tile, 0.45 for each of
-// several; the second launch 3.5; the sums, written and read once, at 5 TB/s and 0.05 a part of a chain of loads.  A 256 x 256 tile takes 1.1 a K-step of 64, 1.65 where all units have one.
-// Measured: 32768 rows, 512 x 512 552 (16 large tiles' fourth) -> 37, 8192 rows 147 -> 17, 8192 rows, 1024 x 1024 63 -> 32, 4 experts of 16384 rows, 512 x 512 123 -> 47.
-inline int weight_grad_parts(int dtype, bool large_ok, int64_t E, double mean, int64_t K, int64_t N) {
-  const bool half = dtype == MOE_BF16;
-  const int64_t tiles = E * tiles_in(K, half ? 128 : 64) * tiles_in(N, half ? 128 : 64), k = (int64_t)ceil(mean / (half ? 64 : 32));
-  const double sums = (double)E * K * N * 8.0 / 5e6;
-  auto cost = [&](int64_t parts) -> double {
-    const int64_t blocks = tiles * parts, steps = ceil_div(k, parts);
-    double t = 6.0;
-    if (half) t += (double)steps * (blocks <= 256 ? 0.46 : 0.86 * (double)ceil_div(blocks, 512));
-    else t += (double)steps * (blocks <= 256 ? 0.5 : 0.45 * (double)ceil_div(blocks, 256));
-    return parts > 1 ? t + 3.5 + (double)parts * (sums + 0.05) : t;
-  };
-  double other = cost(1);
-  if (half && large_ok) {
-    const double t256 = (double)(E * tiles_in(K, 256) * tiles_in(N, 256)), one = 6.0 + (double)k * ceil(t256 / 256.0) * (1.1 + 0.55 * (t256 < 256.0 ? t256 / 256.0 : 1.0));
-    other = one < other ? one : other;
-  }
-  int best = 1;
-  double least = 0.93 * other;
-  for (int parts = 2; parts <= 32 && parts * 2 <= k && tiles * parts <= 2048; ++parts) {
-    const double c = cost(parts);
-    if (c < least) { least = c; best = parts; }
-  }
-  return best;
-}
-
-// Whether the tile with one stage takes a bf16 product that is not shared: few rows, or few enough for many tiles.
-inline bool outer_takes(int64_t E, double mean, int64_t K, int64_t N) {
-  return mean <= 64.0 || (mean <= 256.0 && E * tiles_in(K, 128) * tiles_in(N, 128) >= 512);
-}
-
 }  // namespace

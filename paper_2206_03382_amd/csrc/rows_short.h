@@ -170,13 +170,6 @@ __global__ __launch_bounds__(256, 4) void rows_short_kernel(const TileArgs p) {
   }
 }
 
-// Whether it takes a product that choose_tile would give `tile`, of at least so many tiles of 128 x 128: by the reduction's length and what comes behind it (0.93 to 1.5 times as fast over
-// 200 launches of 256 to 2048 columns; on average 1.17 with an activation, 1.10 with a residual alone, 1.12 without either).
-inline bool short_takes(Tile tile, int64_t tiles, int64_t K, bool act, bool joined) {
-  if ((tile != Tile::k128 && tile != Tile::k256) || tiles < 256) return false;
-  return K <= (act ? (tile == Tile::k256 ? 776 : 1024) : joined ? 512 : 256);
-}
-
 template <int MODE> hipError_t launch_short(TileArgs p, int64_t total, hipStream_t s) {
   dim3 grid;
   if (!tile_launch(p, 128, 128, total, grid)) return hipErrorInvalidValue;

@@ -16,7 +16,7 @@
 // read's four k rows lie in different 64-byte windows modulo 256 and the two blocks of lanes that share a cycle, 8 k apart, in different halves of them.
 namespace {
 
-constexpr int kThinK = 64, kThinColumns = 64, kThinWaves = 4, kThinStages = 2;
+constexpr int kThinStages = 2;
 
 __device__ __forceinline__ int thin_swz(int kr) { return (4 * ((kr >> 1) & 1)) ^ (2 * ((kr >> 3) & 1)); }        // piece c of k row kr is at c ^ thin_swz(kr)
 
@@ -179,27 +179,6 @@ __global__ __launch_bounds__(kThinWaves * 64) void rows_thin_kernel(const TileAr
   }
 }
 
-// Rows and parts of a thin launch's tiles; ri = 0: the other tiles are the faster.
-struct ThinPlan { int ri, parts; };
-
-// The sizes that the tests and figures above are at decide nothing but these borders.  Experts: where those that can have a row leave units without a block (the measured 2 to 8 rows); with
-// all experts live the streaming tiles win (16 rows of 128 experts 26.4 and 24.5, 32 rows 55 and 41).  One matrix: as few rows to a tile as leave two blocks to share its reduction
-// beyond 2048 k (48 x 4096 x 4096: 16 rows, not shared 18.8, 32 rows, two blocks 15.8), one block up to there (a second launch costs more than 8 K-steps of a wave: 16 x 2048 x
-// 2048 8.0 and 9.4).
-inline ThinPlan thin_plan(bool experts, int64_t E, int64_t R, int64_t K, int64_t N) {
-  if (K < 1024) return {0, 1};                                      // no chain to be cut: 6.9 and 7.2 at 776 x 1544
-  const int64_t strips = ceil_div(N, kThinColumns);
-  if (experts) return {(E < R ? E : R) * strips <= 128 && R <= 16 ? 1 : 0, 1};
-  const bool cut = K > 2048;
-  for (int ri = 1; ri <= (cut ? 4 : 2); ri *= 2) {
-    const int64_t tiles = ceil_div(R, 16 * ri) * strips, turns = ceil_div(K, kThinK * kThinWaves * 2);
-    if (tiles > (cut ? 128 : 256)) continue;
-    const int64_t parts = cut ? (256 / tiles < turns ? 256 / tiles : turns) : 1;
-    return {ri, (int)(parts < 16 ? parts : 16)};
-  }
-  return {0, 1};
-}
-
 template <int RI> hipError_t launch_thin_as(TileArgs t, int parts, float* part_sums, hipStream_t s) {
   t.MT = (int)ceil_div(t.C, 16 * RI);
   t.NT = (int)ceil_div(t.N, kThinColumns);
@@ -213,7 +192,7 @@ template <int RI> hipError_t launch_thin_as(TileArgs t, int parts, float* part_s
   return hipGetLastError();
 }
 
-hipError_t launch_thin(const TileArgs& t, ThinPlan plan, float* part_sums, hipStream_t s) {
+hipError_t launch_thin(const TileArgs& t, const RowsPlan& plan, float* part_sums, hipStream_t s) {
   if (plan.ri == 1) return launch_thin_as<1>(t, plan.parts, part_sums, s);
   if (plan.ri == 2) return launch_thin_as<2>(t, plan.parts, part_sums, s);
   return launch_thin_as<4>(t, plan.parts, part_sums, s);
