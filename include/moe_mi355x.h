@@ -432,7 +432,7 @@ int moe_layer_forward_few(const void* x, const void* Wg, const float* gate_bias,
 /* Experts' rows one behind the other, without slabs or a capacity: a layer that drops nothing holds T * k rows whatever its routing is.
  * Expert e's rows are offsets[e] up to offsets[e+1] (offsets [E+1] int32 on the device, ascending from 0) of a matrix of R rows; R is what the caller has memory for, and rows
  * behind the last expert's are neither read nor written.  E <= 512, R < 2^30, widths multiples of 8 and at most 2^20.  Results have memory of their own, but where it says what
- * they may be; one that starts where an input does is refused.
+ * they may be; one that starts where an input, another result or the workspace does is refused, and so is a workspace that starts where any of them does.
  *
  * The rows of a router's choices, from moe_gate_topk's (or moe_gate_route's) idx, loc and counts:
  *   expert e has min(counts[e], C) rows, or counts[e] if C is 0, in the order of loc;  offsets [E+1]: where they start;  row_of [T,k]: the row of a choice, -1 if it has none (loc

@@ -19,10 +19,15 @@ bool all_aligned(std::initializer_list<const void*> ps, size_t a) {
   return true;
 }
 
-// whether a result would go onto one of what it is made of
-bool among(const void* out, std::initializer_list<const void*> ps) {
-  for (const void* p : ps)
-    if (out && p == out) return true;
+// whether a result would go onto an input, or onto another result
+bool clash(std::initializer_list<const void*> results, std::initializer_list<const void*> inputs) {
+  for (const void* const* r = results.begin(); r != results.end(); ++r) {
+    if (!*r) continue;
+    for (const void* const* o = r + 1; o != results.end(); ++o)
+      if (*o == *r) return true;
+    for (const void* p : inputs)
+      if (p == *r) return true;
+  }
   return false;
 }
 
@@ -88,12 +93,13 @@ int moe_ragged_rows(const int32_t* idx, const int32_t* loc, const int32_t* count
   if (!idx || !loc || !counts || !offsets || !row_src || !row_of || T < 1 || E < 1 || k < 1 || k > E || C < 0) return MOE_INVALID_ARG;
   if (E > kMaxExperts || T * k >= kMaxRows || T >= kMaxRows) return MOE_UNSUPPORTED;
   if (!all_aligned({idx, loc, counts, offsets, row_src, row_of}, 4)) return MOE_UNSUPPORTED;
+  if (clash({offsets, row_src, row_of}, {idx, loc, counts})) return MOE_INVALID_ARG;             // blocks write offsets while others add up the counts
   return status_of(launch_ragged_rows(idx, loc, counts, T, E, k, C, offsets, row_src, row_of, (hipStream_t)stream));
 }
 
 int moe_ragged_matmul(const void* A, const int32_t* gather, int64_t A_rows, const void* W, const void* bias, int act, int dtype, const int32_t* offsets, int64_t R,
                       int64_t E, int64_t K, int64_t N, void* pre, void* out, void* stream) {
-  if (!A || !W || !offsets || !out || !dtype_ok(dtype) || !any_act(act) || (gather && A_rows < 1) || among(out, {A, W, bias}) || among(pre, {A, W, bias, out}))
+  if (!A || !W || !offsets || !out || !dtype_ok(dtype) || !any_act(act) || (gather && A_rows < 1) || clash({out, pre}, {A, gather, W, bias, offsets}))
     return MOE_INVALID_ARG;
   if (int st = product_status(R, E, K, N)) return st;
   if ((gather && A_rows >= kMaxRows) || !all_aligned({A, W, bias, pre, out}, 16) || !all_aligned({gather, offsets}, 4)) return MOE_UNSUPPORTED;
@@ -110,12 +116,12 @@ int moe_ragged_matmul_backward(const void* dy, const void* x, const int32_t* gat
                                int dtype, const int32_t* offsets, int64_t R, int64_t E, int64_t K, int64_t N, void* ws, size_t ws_bytes, void* dx, void* dW, void* db,
                                void* stream) {
   if (!dy || !offsets || !dtype_ok(dtype) || !any_act(act) || !any_act(x_act) || (act >= 0) != (pre != nullptr) || (x_act >= 0) != (x_pre != nullptr) || (!dx && !dW && !db) ||
-      (dx && !W) || (dW && !x) || (gather && x_rows < 1) || !ws || (x_pre && !dx) || among(dx, {dy, x, W, pre, dW, db}) || among(dW, {dy, x, W, pre, x_pre, db}) ||
-      among(db, {dy, x, W, pre, x_pre}))
+      (dx && !W) || (dW && !x) || (gather && x_rows < 1) || !ws || (x_pre && !dx) || clash({dx, dW, db}, {dy, x, gather, W, pre, x_pre, offsets, ws}))
     return MOE_INVALID_ARG;
   if (int st = product_status(R, E, K, N)) return st;
   if ((gather && x_rows >= kMaxRows) || !all_aligned({dy, x, W, pre, x_pre, dx, dW, db}, 16) || !all_aligned({gather, offsets}, 4) || !aligned(ws, 256)) return MOE_UNSUPPORTED;
   if (ws_bytes < backward_layout(R, E, K, N, act, dtype).total) return MOE_WORKSPACE_TOO_SMALL;
+  if (clash({ws}, {dy, x, gather, W, pre, x_pre, offsets})) return MOE_INVALID_ARG;
   return backward(dy, x, gather, x_rows, W, pre, act, x_pre, x_act, dtype, offsets, R, E, K, N, (char*)ws, dx, dW, db, (hipStream_t)stream);
 }
 
@@ -125,12 +131,13 @@ size_t moe_linear_workspace_bytes(int64_t T, int64_t K, int64_t N, int dtype) {
 
 int moe_linear(const void* x, const void* W, const void* bias, int act, const void* residual, int dtype, int64_t T, int64_t K, int64_t N, void* ws, size_t ws_bytes,
                void* pre, void* out, void* stream) {
-  if (!x || !W || !out || !dtype_ok(dtype) || !any_act(act) || among(out, {x, W, bias}) || among(pre, {x, W, bias, residual, out})) return MOE_INVALID_ARG;
+  if (!x || !W || !out || !dtype_ok(dtype) || !any_act(act) || clash({out, pre}, {x, W, bias}) || (pre && pre == residual)) return MOE_INVALID_ARG;
   if (int st = product_status(T, 1, K, N)) return st;
   const size_t need = rows_product_bytes(dtype, T, K, N);
   if (need > 0 && !ws) return MOE_INVALID_ARG;
   if (!all_aligned({x, W, bias, residual, pre, out}, 16) || !all_aligned({ws}, 256)) return MOE_UNSUPPORTED;
   if (need > ws_bytes) return MOE_WORKSPACE_TOO_SMALL;
+  if (need > 0 && clash({ws}, {x, W, bias, residual, pre, out})) return MOE_INVALID_ARG;
   const RowsProduct p = {x, W, bias, residual, nullptr, nullptr, 0, T, 1, K, N, act, dtype, out, pre};
   return status_of(launch_rows_product(p, ws, (hipStream_t)stream));
 }
@@ -142,17 +149,18 @@ size_t moe_linear_backward_workspace_bytes(int64_t T, int64_t K, int64_t N, int 
 int moe_linear_backward(const void* dy, const void* x, const void* W, const void* pre, int act, int dtype, int64_t T, int64_t K, int64_t N, void* ws, size_t ws_bytes,
                         void* dx, void* dW, void* db, void* stream) {
   if (!dy || !dtype_ok(dtype) || !any_act(act) || (act >= 0) != (pre != nullptr) || (!dx && !dW && !db) || (dx && !W) || (dW && !x) || !ws ||
-      among(dx, {dy, x, W, pre, dW, db}) || among(dW, {dy, x, W, pre, db}) || among(db, {dy, x, W, pre}))
+      clash({dx, dW, db}, {dy, x, W, pre, ws}))
     return MOE_INVALID_ARG;
   if (int st = product_status(T, 1, K, N)) return st;
   if (!all_aligned({dy, x, W, pre, dx, dW, db}, 16) || !aligned(ws, 256)) return MOE_UNSUPPORTED;
   if (ws_bytes < backward_layout(T, 1, K, N, act, dtype).total) return MOE_WORKSPACE_TOO_SMALL;
+  if (clash({ws}, {dy, x, W, pre})) return MOE_INVALID_ARG;
   return backward(dy, x, nullptr, 0, W, pre, act, nullptr, -1, dtype, nullptr, T, 1, K, N, (char*)ws, dx, dW, db, (hipStream_t)stream);
 }
 
 int moe_dropout(const void* x, const void* residual, double p, const uint64_t* seed, int dtype, int64_t n, void* out, void* stream) {
   Dropout d;
-  if (!x || !out || !dtype_ok(dtype) || n < 1 || !dropout_of(p, seed, d)) return MOE_INVALID_ARG;
+  if (!x || !out || !dtype_ok(dtype) || n < 1 || !dropout_of(p, seed, d) || clash({out}, {seed})) return MOE_INVALID_ARG;
   if (n % 8 != 0 || n >= ((int64_t)1 << 40) || !all_aligned({x, residual, out}, 16) || !all_aligned({seed}, 8)) return MOE_UNSUPPORTED;
   return status_of(launch_dropout(x, residual, d, dtype, n, out, (hipStream_t)stream));
 }
@@ -167,7 +175,7 @@ static int combine_status(int64_t T, int64_t M, int k, int64_t R) {
 int moe_ragged_combine(const void* Y, int64_t R, const int32_t* row_of, const float* gate_w, const void* residual, double p, const uint64_t* seed, int dtype, int64_t T,
                        int64_t M, int k, void* out, void* stream) {
   Dropout d;
-  if (!Y || !row_of || !out || !dtype_ok(dtype) || !dropout_of(p, seed, d) || out == Y) return MOE_INVALID_ARG;
+  if (!Y || !row_of || !out || !dtype_ok(dtype) || !dropout_of(p, seed, d) || clash({out}, {Y, row_of, gate_w, seed})) return MOE_INVALID_ARG;
   if (int st = combine_status(T, M, k, R)) return st;
   if (!all_aligned({Y, residual, out}, 16) || !all_aligned({seed}, 8) || !all_aligned({row_of, gate_w}, 4)) return MOE_UNSUPPORTED;
   return status_of(launch_ragged_combine(Y, R, row_of, gate_w, residual, d, dtype, T, M, k, out, (hipStream_t)stream));
@@ -176,7 +184,7 @@ int moe_ragged_combine(const void* Y, int64_t R, const int32_t* row_of, const fl
 int moe_ragged_combine_backward(const void* d_out, const void* Y, int64_t R, const int32_t* row_of, const float* gate_w, double p, const uint64_t* seed, int dtype,
                                 int64_t T, int64_t M, int k, void* dY, float* dgate_w, void* stream) {
   Dropout d;
-  if (!d_out || !Y || !row_of || !dY || !dgate_w || !dtype_ok(dtype) || !dropout_of(p, seed, d) || dY == d_out || dY == Y) return MOE_INVALID_ARG;
+  if (!d_out || !Y || !row_of || !dY || !dgate_w || !dtype_ok(dtype) || !dropout_of(p, seed, d) || clash({dY, dgate_w}, {d_out, Y, row_of, gate_w, seed})) return MOE_INVALID_ARG;
   if (int st = combine_status(T, M, k, R)) return st;
   if (!all_aligned({d_out, Y, dY}, 16) || !all_aligned({seed}, 8) || !all_aligned({row_of, gate_w, dgate_w}, 4)) return MOE_UNSUPPORTED;
   return status_of(launch_ragged_combine_backward(d_out, Y, R, row_of, gate_w, d, dtype, T, M, k, dY, dgate_w, (hipStream_t)stream));
