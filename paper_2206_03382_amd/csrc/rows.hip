@@ -1,5 +1,6 @@
 // Operators around the products of experts' rows that lie one behind the other: the rows of a router's choices, the weighted combine of their results, dropout,
 // the activation's derivative with the bias gradient.  All of them move memory once, 16 bytes a lane; what bounds them is HBM.
+#include "philox.h"
 #include "rows.h"
 #include "rows_act.h"
 
@@ -7,33 +8,8 @@ namespace moe {
 namespace {
 
 // ---- dropout -------------------------------------------------------------------------------------------------------------
-// Philox4x32-10 (Salmon, Moraes, Dror, Shaw, SC 2011), key = seed[0], counter = (number of the group of eight elements, seed[1]).  16 of the 128 bits for an element: a group is one
-// 16-byte piece of bf16, and ten rounds of four 32-bit products serve eight elements, which HBM takes longer for than the rounds do (32 bits for an element would not be).
-// The probability is therefore a multiple of 2^-16.  Seed and offset are read on the device, so that a captured step can be given others.
+// The generator: philox.h.  The probability is a multiple of 2^-16.  Seed and offset are read on the device, so that a captured step can be given others.
 constexpr int kGroup = 8;
-
-struct Philox {
-  uint32_t k0, k1, o0, o1;
-  __device__ __forceinline__ explicit Philox(const uint64_t* seed) {
-    const uint64_t s = seed[0], o = seed[1];
-    k0 = (uint32_t)s, k1 = (uint32_t)(s >> 32), o0 = (uint32_t)o, o1 = (uint32_t)(o >> 32);
-  }
-  // the 16-bit numbers of group g, the lower one of a word first
-  __device__ __forceinline__ void bits(uint64_t g, uint32_t (&w)[4]) const {
-    uint32_t c0 = (uint32_t)g, c1 = (uint32_t)(g >> 32), c2 = o0, c3 = o1, a = k0, b = k1;
-#pragma unroll
-    for (int i = 0; i < 10; ++i) {
-      const uint64_t p0 = (uint64_t)0xD2511F53u * c0, p1 = (uint64_t)0xCD9E8D57u * c2;
-      c0 = (uint32_t)(p1 >> 32) ^ c1 ^ a;
-      c1 = (uint32_t)p1;
-      c2 = (uint32_t)(p0 >> 32) ^ c3 ^ b;
-      c3 = (uint32_t)p0;
-      a += 0x9E3779B9u;
-      b += 0xBB67AE85u;
-    }
-    w[0] = c0, w[1] = c1, w[2] = c2, w[3] = c3;
-  }
-};
 
 // v of group g: dropped elements become zero whatever they were.
 __device__ __forceinline__ void drop(float (&v)[kGroup], const Philox& rng, uint64_t g, uint32_t below, float scale) {
@@ -82,7 +58,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(const uint4* __restrict__ 
                                                       int64_t groups, uint4* out) {
   constexpr int P = kPieces<ET>;
   const int64_t stride = (int64_t)gridDim.x * 256;
-  const Philox rng = DROP ? Philox(seed) : Philox((const uint64_t*)nullptr);
+  const Philox rng = DROP ? Philox(seed) : Philox();
   for (int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x; g < groups; g += stride) {
     float v[kGroup], r[kGroup];
     const Group<ET> a = load_group<ET, false>(x + g * P);
@@ -161,7 +137,7 @@ __global__ __launch_bounds__(256) void ragged_combine_kernel(const uint4* __rest
                                                              int groups, int k, uint4* out) {
   constexpr int P = kPieces<ET>;
   const int lane = threadIdx.x & 63;
-  const Philox rng = DROP ? Philox(seed) : Philox((const uint64_t*)nullptr);
+  const Philox rng = DROP ? Philox(seed) : Philox();
   for (int64_t u = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6))); u < units; u += (int64_t)gridDim.x * 4) {
     const int64_t t = u / per_row;
     const int g = (int)(u - t * per_row) * 64 + lane;
@@ -217,7 +193,7 @@ __global__ __launch_bounds__(256) void ragged_combine_backward_kernel(const uint
   constexpr int P = kPieces<ET>;
   __shared__ float part[4][8];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Philox rng = DROP ? Philox(seed) : Philox((const uint64_t*)nullptr);
+  const Philox rng = DROP ? Philox(seed) : Philox();
   const int64_t step = (int64_t)gridDim.x * (4 / W);
   for (int64_t t = (int64_t)blockIdx.x * (4 / W) + (W == 4 ? 0 : wave); t < T; t += step) {
     for (int j0 = 0; j0 < k; j0 += 8) {
