@@ -1010,7 +1010,7 @@ def _check_seed(seed: torch.Tensor) -> None:
 
 def dropout(x: torch.Tensor, p: float, seed: torch.Tensor, residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """residual + dropout(x) with probability p: the mask comes from the numbers in seed (int64 [2] on the device: seed and offset) and an element's place, and is never stored.
-    dropout(dy, p, seed) is the gradient of x.  out may be x or residual.  With p = 0, no residual and no out the result is x itself."""
+    dropout(dy, p, seed) is the gradient of x.  out may be x or residual.  With p = 0, no residual and no out the result is x itself, not a copy."""
     code = _dtype_code(x)
     _check_seed(seed)
     if residual is not None and (residual.shape != x.shape or residual.dtype != x.dtype):
@@ -1020,6 +1020,9 @@ def dropout(x: torch.Tensor, p: float, seed: torch.Tensor, residual: Optional[to
     x_, residual_, seed_, _ = _here(x, residual, seed, out)
     if out is None:
         if p == 0 and residual is None:
+            n = x.numel()
+            if n < 1 or n % 8 or n >= 1 << 40 or x_ % 16:            # as the library would
+                raise MoEError(INVALID_ARG if n < 1 else UNSUPPORTED, "dropout")
             return x
         out = torch.empty_like(x)
     _check(lib().moe_dropout(x_, residual_, p, seed_, code, x.numel(), out.data_ptr(), _stream()), "moe_dropout")
