@@ -437,7 +437,8 @@ int moe_layer_forward_few(const void* x, const void* Wg, const float* gate_bias,
  * The rows of a router's choices, from moe_gate_topk's (or moe_gate_route's) idx, loc and counts:
  *   expert e has min(counts[e], C) rows, or counts[e] if C is 0, in the order of loc;  offsets [E+1]: where they start;  row_of [T,k]: the row of a choice, -1 if it has none (loc
  *   beyond the expert's rows, idx not an expert);  row_src [T*k]: the token of a row, -1 behind the last expert's.
- * Rows that counts announces and no choice has hold unspecified tokens; products read row 0 for tokens out of range. */
+ * Rows that counts announces and no choice has (choices of padding, marked by an idx that is no expert) keep what row_src held, tokens of no meaning; products read row 0 for tokens out of
+ * range.  Their results are nobody's; for weight gradients their rows of dY are to be cleared, see moe_ragged_combine_backward, and the tokens that they read to be finite. */
 int moe_ragged_rows(const int32_t* idx, const int32_t* loc, const int32_t* counts, int64_t T, int64_t E, int k, int64_t C, int32_t* offsets, int32_t* row_src,
                     int32_t* row_of, void* stream);
 
@@ -482,7 +483,7 @@ int moe_dropout(const void* x, const void* residual, double p, const uint64_t* s
  *   Y [R,M], residual [T,M] or NULL (it may be out), out [T,M] in `dtype`; row_of [T,k] (choices whose row is not one of R are left out); gate_w [T,k] fp32, or NULL: ones.
  *   p, seed as moe_dropout for an [T,M] matrix; p = 0: nothing is dropped, seed may be NULL.
  * Backward, with d = dropout(d_out):  dY[row_of[t,j]] = gate_w[t,j] * d[t];  dgate_w[t,j] = <d[t], Y[row_of[t,j]]>, 0 for a choice without a row.  Rows that no choice has
- * are left untouched. */
+ * are left untouched: where offsets give an expert such rows (padding, see moe_ragged_rows), the caller clears dY before, or moe_ragged_matmul_backward adds what it held to dW and db. */
 int moe_ragged_combine(const void* Y, int64_t R, const int32_t* row_of, const float* gate_w, const void* residual, double p, const uint64_t* seed, int dtype, int64_t T,
                        int64_t M, int k, void* out, void* stream);
 int moe_ragged_combine_backward(const void* d_out, const void* Y, int64_t R, const int32_t* row_of, const float* gate_w, double p, const uint64_t* seed, int dtype,

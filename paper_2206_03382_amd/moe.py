@@ -898,7 +898,8 @@ class RaggedRows(NamedTuple):
 
 
 def ragged_rows(idx: torch.Tensor, loc: torch.Tensor, counts: torch.Tensor, C: int = 0) -> RaggedRows:
-    """The rows of the choices of gate_topk or gate_route, one expert's behind the other's; C: a capacity beyond which they are dropped (0: none is)."""
+    """The rows of the choices of gate_topk or gate_route, one expert's behind the other's; C: a capacity beyond which they are dropped (0: none is).  An idx that is no expert (padding) has
+    no row; rows that counts announces all the same hold tokens of no meaning, see ragged_combine_backward."""
     shape, i32 = idx.shape, torch.int32
     if len(shape) != 2 or loc.shape != shape or counts.dim() != 1 or idx.dtype != i32 or loc.dtype != i32 or counts.dtype != i32:
         raise ValueError("idx and loc must be int32 [T,k], counts int32 [E]")
@@ -1061,7 +1062,8 @@ def ragged_combine(Y: torch.Tensor, row_of: torch.Tensor, gate_w: Optional[torch
 
 def ragged_combine_backward(d_out: torch.Tensor, Y: torch.Tensor, row_of: torch.Tensor, gate_w: Optional[torch.Tensor], dropout: Optional[Tuple[float, torch.Tensor]] = None,
                             dY: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
-    """(dY [R,M], dgate_w [T,k]) of ragged_combine, with the same dropout; the residual's gradient is d_out.  Rows that no choice has hold whatever dY's memory did."""
+    """(dY [R,M], dgate_w [T,k]) of ragged_combine, with the same dropout; the residual's gradient is d_out.  Rows that no choice has hold whatever dY's memory did: with padded
+    choices, whose rows counts still announces, pass dY=torch.zeros_like(Y), or ragged_matmul_backward adds that to dW and db."""
     p, seed = _check_combine(Y, row_of, gate_w, dropout)
     (T, k), (R, M) = row_of.shape, Y.shape
     code = _dtype_code(Y)
