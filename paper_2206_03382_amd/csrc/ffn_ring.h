@@ -48,13 +48,13 @@ __global__ __launch_bounds__(256, 2 * ring_bytes(TM, TN) <= 163840 ? 2 : 1) void
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1, kq = lane >> 4;
   int e, mt, nt, rows;
-  if (!p.plain) {
+  if (ROWS || !p.plain) {
     if (!find_tile<TM, MODE == kTN, 0, false, ROWS>(blockIdx.x, lane, p.E, p.C, p.counts, p.NT, e, mt, nt, rows)) return;
   } else {
     e = blockIdx.y;
     mt = blockIdx.x / p.NT;
     nt = blockIdx.x % p.NT;
-    rows = MODE == kTN ? live_rows_of(e, p.C, p.counts) : live_rows_of<ROWS>(e, p.C, p.counts);
+    rows = live_rows_of(e, p.C, p.counts);
   }
   const int64_t m0 = (int64_t)mt * TM, n0 = (int64_t)nt * TN;
   if (m0 >= rows) return;
@@ -457,7 +457,7 @@ __global__ __launch_bounds__(256, 2 * ring_bytes(TM, TN) <= 163840 ? 2 : 1) void
 template <int MODE, int TM, int TN, bool ROWS = false>
 static hipError_t launch_ring(TileArgs p, int64_t total, hipStream_t s) {
   dim3 grid;
-  if (!tile_launch(p, TM, TN, total, grid)) return hipErrorInvalidValue;
+  if (!tile_launch(p, TM, TN, total, grid) || (ROWS && p.plain)) return hipErrorInvalidValue;
   if (MODE == kTN && ROWS && p.parts > 1) grid.z = (unsigned)p.parts;
   if (MODE == kTN && p.gather) grouped_gemm_ring_kernel<MODE, TM, TN, MODE == kTN, ROWS><<<grid, dim3(256), 0, s>>>(p);
   else grouped_gemm_ring_kernel<MODE, TM, TN, false, ROWS><<<grid, dim3(256), 0, s>>>(p);

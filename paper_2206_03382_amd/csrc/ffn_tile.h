@@ -42,7 +42,7 @@ template <int MOST, int L> __device__ __forceinline__ void wait_for_loads(int la
 // (no barrier until their sums meet, which the first wave adds up in order).  For fp32 launches of few tiles, whose time is one chain
 // of matrix instructions per wave on a part of the units: see fp32_split.  Two stages (64 KB, two blocks to a unit): three or four
 // leave room for one block, 4 experts x 256 rows, 256 x 512, two products: 15.4 us against 19.4 and 19.7.
-// ROWS: as in ffn_ring.h.
+// ROWS: as in ffn_ring.h, kNN and kNT.
 template <typename ET, int MODE, int BM, int BN, int WR, int WC, int NS, bool GK = false, bool PART = false, bool STREAM = false, int KS = 1, bool ROWS = false>
 __global__ __launch_bounds__(WR * WC * KS * 64, 2) void grouped_gemm_tile_kernel(const TileArgs p) {
   constexpr int ES = (int)sizeof(ET), EC = 16 / ES;                 // elements per 16-byte piece
@@ -68,21 +68,21 @@ __global__ __launch_bounds__(WR * WC * KS * 64, 2) void grouped_gemm_tile_kernel
 
   // ---- which tile: the search of the large kernel, or plain numbering where that does not do ---------------------
   int e, mt, nt, rows;
-  if (!p.plain) {
-    if (!find_tile<BM, MODE == kTN, 0, false, ROWS && MODE != kTN>(blockIdx.x, lane, p.E, p.C, p.counts, p.NT, e, mt, nt, rows)) return;
+  static_assert(!ROWS || MODE != kTN, "weight gradients of rows: ffn_ring.h, rows_fp32.h");
+  if (ROWS || !p.plain) {
+    if (!find_tile<BM, MODE == kTN, 0, false, ROWS>(blockIdx.x, lane, p.E, p.C, p.counts, p.NT, e, mt, nt, rows)) return;
   } else {
     e = blockIdx.y;
     mt = blockIdx.x / p.NT;
     nt = blockIdx.x % p.NT;
-    rows = MODE == kTN ? live_rows_of(e, p.C, p.counts) : live_rows_of<ROWS>(e, p.C, p.counts);
+    rows = live_rows_of(e, p.C, p.counts);
   }
   const int64_t m0 = (int64_t)mt * BM;
   if (m0 >= rows) return;
   const int64_t n0 = (int64_t)nt * BN;
   int64_t kend = p.K;                                               // k that exist
-  if (MODE == kTN && ROWS) kend = live_rows_of<ROWS>(e, p.K, p.kfill);
-  else if (MODE == kTN && p.kfill) { const int64_t c = p.kfill[e]; kend = c < p.K ? (c > 0 ? c : 0) : p.K; }
-  const int64_t first = MODE == kTN ? first_row_of<ROWS>(e, p.K, p.kfill) : first_row_of<ROWS>(e, p.C, p.counts);   // of the expert's rows
+  if (MODE == kTN && p.kfill) { const int64_t c = p.kfill[e]; kend = c < p.K ? (c > 0 ? c : 0) : p.K; }
+  const int64_t first = MODE == kTN ? (int64_t)e * p.K : first_row_of<ROWS>(e, p.C, p.counts);   // of the expert's rows
   if (PART) { const int64_t left = p.ktotal - (int64_t)e * p.K; kend = left < p.K ? (left > 0 ? left : 0) : p.K; }
   const int KT_all = kend > 0 ? (int)((kend + BKE - 1) / BKE) : 1;
   const int KT = KS > 1 ? (KT_all - part + KS - 1) / KS : KT_all;   // K-steps of this wave (none where there are fewer than waves)
@@ -151,8 +151,8 @@ __global__ __launch_bounds__(WR * WC * KS * 64, 2) void grouped_gemm_tile_kernel
     if constexpr (GK) {
 #pragma unroll
       for (int i = 0; i < LA; ++i) {
-        const int64_t slot = (int64_t)t * BKE + a_k[i], last = ROWS ? p.K - 1 - first : p.K - 1;
-        g[i] = p.gather[first + (slot < last ? slot : last)];
+        const int64_t slot = (int64_t)t * BKE + a_k[i];
+        g[i] = p.gather[first + (slot < p.K ? slot : p.K - 1)];
       }
     }
   };
@@ -475,10 +475,9 @@ __global__ __launch_bounds__(WR * WC * KS * 64, 2) void grouped_gemm_tile_kernel
       }
       __builtin_amdgcn_wave_barrier();
     };
-    const OT* with = MODE == kTN ? nullptr : (const OT*)p.pre;
+    const OT* with = (const OT*)p.pre;
     if (MODE == kNN && p.pre_out) write_rows(std::integral_constant<int, -1>{}, (OT*)p.pre_out, nullptr);
-    if (MODE == kTN) write_rows(std::integral_constant<int, -1>{}, (OT*)p.out, nullptr);
-    else switch (p.act) {
+    switch (p.act) {
       case MOE_ACT_RELU: write_rows(std::integral_constant<int, MOE_ACT_RELU>{}, (OT*)p.out, with); break;
       case MOE_ACT_GELU: write_rows(std::integral_constant<int, MOE_ACT_GELU>{}, (OT*)p.out, with); break;
       case MOE_ACT_SILU: write_rows(std::integral_constant<int, MOE_ACT_SILU>{}, (OT*)p.out, with); break;
@@ -505,10 +504,10 @@ __global__ __launch_bounds__(WR * WC * KS * 64, 2) void grouped_gemm_tile_kernel
 template <typename ET, int MODE, int BM, int BN, int NS, bool STREAM = false, int KS = 1, bool ROWS = false>
 static hipError_t launch_tile(TileArgs p, int64_t total, hipStream_t s) {
   dim3 grid;
-  if (!tile_launch(p, BM, BN, total, grid)) return hipErrorInvalidValue;
+  if (!tile_launch(p, BM, BN, total, grid) || (ROWS && p.plain)) return hipErrorInvalidValue;
   if constexpr (MODE == kTN) {
     if (p.gather) {
-      grouped_gemm_tile_kernel<ET, MODE, BM, BN, 2, 2, NS, true, false, false, 1, ROWS><<<grid, dim3(256), 0, s>>>(p);
+      grouped_gemm_tile_kernel<ET, MODE, BM, BN, 2, 2, NS, true><<<grid, dim3(256), 0, s>>>(p);
       return hipGetLastError();
     }
   }

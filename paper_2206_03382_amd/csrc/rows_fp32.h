@@ -28,14 +28,7 @@ __global__ __launch_bounds__(256, 5) void rows_fp32_kernel(const TileArgs p) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1, kq = lane >> 4, l16 = lane & 15;
   int e, mt, nt, rows;
-  if (!p.plain) {
-    if (!find_tile<T, MODE == kTN, 0, false, MODE != kTN>(blockIdx.x, lane, p.E, p.C, p.counts, p.NT, e, mt, nt, rows)) return;
-  } else {
-    e = blockIdx.y;
-    mt = blockIdx.x / p.NT;
-    nt = blockIdx.x % p.NT;
-    rows = MODE == kTN ? (int)p.C : live_rows_of<true>(e, p.C, p.counts);
-  }
+  if (!find_tile<T, MODE == kTN, 0, false, MODE != kTN>(blockIdx.x, lane, p.E, p.C, p.counts, p.NT, e, mt, nt, rows)) return;
   const int64_t m0 = (int64_t)mt * T, n0 = (int64_t)nt * T;
   if (m0 >= rows) return;
   int64_t kend = MODE == kTN ? live_rows_of<true>(e, p.K, p.kfill) : p.K;
@@ -301,7 +294,7 @@ __global__ __launch_bounds__(256, 5) void rows_fp32_kernel(const TileArgs p) {
 
 template <int MODE> hipError_t launch_rows_fp32(TileArgs p, int64_t total, hipStream_t s) {
   dim3 grid;
-  if (!tile_launch(p, 64, 64, total, grid)) return hipErrorInvalidValue;
+  if (!tile_launch(p, 64, 64, total, grid) || p.plain) return hipErrorInvalidValue;
   if (MODE == kTN && p.parts > 1) grid.z = (unsigned)p.parts;
   if (MODE == kTN && p.gather) rows_fp32_kernel<MODE, MODE == kTN><<<grid, dim3(256), 0, s>>>(p);
   else rows_fp32_kernel<MODE, false><<<grid, dim3(256), 0, s>>>(p);

@@ -14,13 +14,7 @@ __global__ __launch_bounds__(256, 4) void rows_outer_kernel(const TileArgs p) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1, kq = lane >> 4;
   int e, mt, nt, rows;
-  if (!p.plain) {
-    if (!find_tile<T, true>(blockIdx.x, lane, p.E, p.C, nullptr, p.NT, e, mt, nt, rows)) return;
-  } else {
-    e = blockIdx.y;
-    mt = blockIdx.x / p.NT;
-    nt = blockIdx.x % p.NT;
-  }
+  if (!find_tile<T, true>(blockIdx.x, lane, p.E, p.C, nullptr, p.NT, e, mt, nt, rows)) return;
   const int64_t m0 = (int64_t)mt * T, n0 = (int64_t)nt * T;
   const int64_t first = first_row_of<true>(e, p.K, p.kfill);        // of the expert's rows
   const int kend = live_rows_of<true>(e, p.K, p.kfill);
@@ -106,7 +100,7 @@ __global__ __launch_bounds__(256, 4) void rows_outer_kernel(const TileArgs p) {
 
 hipError_t launch_outer(TileArgs p, int64_t total, hipStream_t s) {
   dim3 grid;
-  if (!tile_launch(p, 128, 128, total, grid)) return hipErrorInvalidValue;
+  if (!tile_launch(p, 128, 128, total, grid) || p.plain) return hipErrorInvalidValue;
   if (p.gather) rows_outer_kernel<true><<<grid, dim3(256), 0, s>>>(p);
   else rows_outer_kernel<false><<<grid, dim3(256), 0, s>>>(p);
   return hipGetLastError();

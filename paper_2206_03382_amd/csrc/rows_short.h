@@ -15,14 +15,7 @@ __global__ __launch_bounds__(256, 4) void rows_short_kernel(const TileArgs p) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1, kq = lane >> 4;
   int e, mt, nt, rows;
-  if (!p.plain) {
-    if (!find_tile<T, false, 0, false, true>(blockIdx.x, lane, p.E, p.C, p.counts, p.NT, e, mt, nt, rows)) return;
-  } else {
-    e = blockIdx.y;
-    mt = blockIdx.x / p.NT;
-    nt = blockIdx.x % p.NT;
-    rows = live_rows_of<true>(e, p.C, p.counts);
-  }
+  if (!find_tile<T, false, 0, false, true>(blockIdx.x, lane, p.E, p.C, p.counts, p.NT, e, mt, nt, rows)) return;
   const int64_t m0 = (int64_t)mt * T, n0 = (int64_t)nt * T;
   if (m0 >= rows) return;
   const int64_t first = first_row_of<true>(e, p.C, p.counts), live = rows - m0 - wm * WT, nw = n0 + wn * WT;
@@ -172,7 +165,7 @@ __global__ __launch_bounds__(256, 4) void rows_short_kernel(const TileArgs p) {
 
 template <int MODE> hipError_t launch_short(TileArgs p, int64_t total, hipStream_t s) {
   dim3 grid;
-  if (!tile_launch(p, 128, 128, total, grid)) return hipErrorInvalidValue;
+  if (!tile_launch(p, 128, 128, total, grid) || p.plain) return hipErrorInvalidValue;
   rows_short_kernel<MODE><<<grid, dim3(256), 0, s>>>(p);
   return hipGetLastError();
 }

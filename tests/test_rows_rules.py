@@ -102,3 +102,21 @@ def test_shared_reductions_are_the_same_for_gathered_rows(rules):
         for half in (0, 1):
             got = {rules("weight_grad", half, E, R, K, N, g) == "parts" for g in (0, 1, R, 1 << 29)}
             assert len(got) == 1
+
+
+def test_every_launch_fits_a_grid(ffn_rules):
+    """Up to the limits that the entry points check, (ceil(R / 64) + E) * ceil(width / 64) and E * ceil(K / 64) * ceil(N / 64) below 2^23, no tiling asks for 2^24 blocks, so that a block's number is all that
+    finds its tile."""
+    half = 1 << 23
+    for E in (1, 2, 63, 64, 65, 511, 512):
+        for tiles in (1, 2, 3, 100, 1 << 10, 1 << 14):                 # 64-wide column tiles
+            R = min((half // tiles - 1 - E) * 64, (1 << 30) - 1)       # the most rows
+            for rows in {1, 63, R // 2, R} if R > 0 else ():
+                for tile in (64, 128, 256):
+                    NT = -(-tiles * 64 // tile)
+                    for shorts_last in (0, 1):
+                        assert 0 < ffn_rules.grid(E, rows, tile, NT, rows, shorts_last) < 1 << 24
+            most = (half // E - 1) // tiles                            # the most row tiles of weight gradients
+            for tile in (64, 128, 256):
+                if most > 0:
+                    assert ffn_rules.grid(E, most * 64, tile, -(-tiles * 64 // tile), E * most * 64, 0) < 1 << 24
