@@ -445,7 +445,8 @@ int moe_ragged_rows(const int32_t* idx, const int32_t* loc, const int32_t* count
 /* A projection of the experts on such rows:  out[r] = act(A[r] W[e] + bias[e])  for the rows r of expert e.
  *   A [R,K], or with gather [R] int32 row r is A[gather[r]] of [A_rows,K] (row_src: the tokens themselves); W [E,K,N]; bias [E,N] or NULL; out [R,N], all in `dtype`.
  *   pre [R,N] or NULL: the values before the activation as well, rounded once (what the backward takes).
- * act: MOE_ACT_*, or MOE_ACT_NONE; ReLU keeps a NaN.  fp32 sums, activation and one rounding; K * N < 2^31. */
+ * act: MOE_ACT_*, or MOE_ACT_NONE; ReLU keeps a NaN.  fp32 sums, activation and one rounding; K * N < 2^31.
+ * bf16 rows gathered from a matrix of 4 GiB or more, here and in the weight gradients, take smaller tiles, which are slower (128 x 128 at most). */
 int moe_ragged_matmul(const void* A, const int32_t* gather, int64_t A_rows, const void* W, const void* bias, int act, int dtype, const int32_t* offsets, int64_t R,
                       int64_t E, int64_t K, int64_t N, void* pre, void* out, void* stream);
 
@@ -473,8 +474,8 @@ int moe_linear_backward(const void* dy, const void* x, const void* W, const void
 
 /* Dropout from a counter-based generator, whose mask is never stored:  out = residual + keep * x / (1 - p), elementwise; dropped elements add 0 whatever x is.
  *   x, residual (or NULL), out: n elements in `dtype`, n a multiple of 8; out may be x or residual.
- *   seed [2] on the device, 8-byte aligned: the generator's seed and an offset (another one for every call that is to have a mask of its own).  With dy for x and no residual the
- *   same call is the gradient of x; that of the residual is dy.
+ *   seed [2] on the device, 8-byte aligned: the generator's seed and an offset (another one for every call that is to have a mask of its own).  With dy for x, the same numbers in seed and
+ *   no residual the same call is the gradient of x; that of the residual is dy.
  * Philox4x32-10 with the key seed[0] and, for the group i / 8 of element i, the counter (low and high word of i / 8, of seed[1]); element i has 16 bits of the result, the half i % 2
  * (low one first) of word i % 8 / 2, and is dropped if they are below p * 2^16 rounded to a whole number; p in that rounding also gives 1 / (1 - p).  0 <= p <= 1. */
 int moe_dropout(const void* x, const void* residual, double p, const uint64_t* seed, int dtype, int64_t n, void* out, void* stream);

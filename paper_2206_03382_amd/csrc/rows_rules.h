@@ -80,7 +80,7 @@ struct RowsPlan {
 
 static inline int64_t mean_rows(int64_t R, int64_t E) { return tiles_in(R, E); }
 
-// Whether the large tile takes a product of K x N weights; gather_rows > 0: of rows of so many elements that 32-bit offsets reach.
+// Whether the large tile takes a product of K x N weights; gather_rows > 0: of rows of a matrix that its 32-bit offsets reach, below 4 GiB (beyond, 128 x 128 at most).
 static inline bool large_takes(int64_t E, int64_t K, int64_t N, int64_t gather_rows, int64_t gather_width) {
   return K % kLargeK == 0 && N % kLargeTile == 0 && E <= kMaxExperts && gather_rows * gather_width * 2 < ((int64_t)1 << 32);
 }

@@ -3,8 +3,8 @@
 // With a short reduction a tile is mostly the way to its first operands and its results, and what it needs is other tiles on the unit meanwhile: one stage of 64 k, 32 KB of LDS, four
 // blocks to a unit, as in rows_outer.h; K-steps follow each other without a load in advance.  Above all one block's results (activation, what they are joined with, stores) hide behind the
 // others' products, which blocks of the large tiles, one or two to a unit, do one after the other.  us, with the tile that choose_tile names and here: 90820 rows of 16 experts,
-// 256 x 512 44.6 and 37.8, with GeLU and kept values 79.8 and 54.7, times GeLU' 87.2 and 59.1; 512 x 512 57.0 and 57.5, 97.7 and 89.5, 107 and 89.5; 32768 x 776 x 2048 of 8 experts with GeLU
-// and kept values 198 and 173; with 1536 columns 250 and 269.
+// 256 x 512 47.1 and 43.6, with GeLU and kept values 84.8 and 60.9, times GeLU' 93.8 and 64.3; 512 x 512 64.1 and 64.0, 102 and 91.3, 111 and 92.7; 32768 x 776 x 2048 of 8 experts with GeLU
+// and kept values 196 and 170; with 1536 columns 250 and 269.
 namespace {
 
 template <int MODE>

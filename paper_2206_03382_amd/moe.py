@@ -1115,7 +1115,7 @@ class DroplessLayer:
         self.k, self.normalize, self.act, self.code = k, int(normalize), int(act), code
 
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None, dropout: Optional[Tuple[float, torch.Tensor]] = None, keep: bool = False):
-        """out [T,M]; keep: (out, what backward takes).  dropout: (p, seed) as in dropout()."""
+        """out [T,M]; keep: (out, what backward takes).  dropout: (p, seed) as in dropout(); seed is read again by backward: change its numbers only after that."""
         if x.dim() != 2 or x.shape[1] != self.M or _dtype_code(x) != self.code:
             raise ValueError(f"x must be [T,{self.M}] in the weights' type")
         r = gate_route(x, self.Wg, self.gate_bias, self.k, 1, self.normalize)          # its slots are not used: one to an expert
