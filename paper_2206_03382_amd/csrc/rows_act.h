@@ -6,11 +6,11 @@ namespace moe {
 namespace {
 
 // Phi(-y) = erfc(y / sqrt 2) / 2 = 2^-(P(y) + 1) for y >= 0, with a polynomial of degree 9 and P(0) = 0, fitted to equal ripple in P over [0, 13.2], where v Phi(v) reaches
-// the smallest normal number: 2.1e-5 of Phi(-y) in exact arithmetic, 5e-5 (1/78 of a bf16 rounding) with the fp32 evaluation, so that GeLU is exact to that also where it is small itself.  Up to 13.4,
-// where its derivative reaches that number and Phi(-y) is 1/180 of it, 1.4e-4.  One exponential, no division.  The hardware's exponential gives zero instead of results below 2^-126, and
-// Phi(-12.95) is there already: the exponent is raised by 10 and taken out again in the product with y.
+// the smallest normal number: 2.1e-5 of Phi(-y) in exact arithmetic, 5e-5 (1/78 of a bf16 rounding) with the fp32 evaluation, so that GeLU is exact to that also where it is small itself.  Up to 13.5,
+// where its derivative is past that number and Phi(-y) 1/180 of it, 2e-4.  One exponential, no division.  The hardware's exponential gives zero instead of results below 2^-126, and
+// Phi(-12.95) is there already: the exponent is raised by 10 and taken out again in the product with y.  From 13.47 on it is zero all the same.
 constexpr float kPhi[9] = {1.151095026e+00f, 4.586445080e-01f, 5.404893616e-02f, -8.699391121e-03f, 1.027744177e-03f, -8.451740843e-05f, 4.530642880e-06f, -1.413703882e-07f, 1.939663995e-09f};
-constexpr float kPhiEnd = 13.4f, kPhiUnit = 0x1p-10f;
+constexpr float kPhiEnd = 14.0f, kPhiUnit = 0x1p-10f;
 __device__ __forceinline__ float normal_tail(float y) {             // Phi(-y) / kPhiUnit, 0 <= y <= kPhiEnd
   float p = kPhi[8];
 #pragma unroll

@@ -73,3 +73,18 @@ def test_every_value(moe, act, top, dtype):   # noqa: F811
         over = np.abs(got - want) - (off + HALF[dtype] * (np.abs(want) + off) + SMALLEST)
         worst = int(over.argmax())
         assert over[worst] <= 0, f"{what} at {v[worst]}: {got[worst]} for {want[worst]}; {(over > 0).sum()} beyond the bound, from {v[over > 0].min()} to {v[over > 0].max()}"
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("act", ["gelu", "silu", "relu"])
+def test_far_values(moe, act, dtype):   # noqa: F811
+    """Where nothing is left of one of the two parts: zero and the value itself, derivatives zero and one."""
+    v = np.array([110.0, 1e4, 1e30, 3e38], dtype=np.float32)
+    v = torch.from_numpy(v).to(dtype).float().numpy()
+    out, slope = through(moe, np.concatenate([v, -v]), act, dtype)
+    assert (out == np.concatenate([v, 0 * v])).all() and (slope == [1] * 4 + [0] * 4).all()
+    at = torch.zeros((2, 8), dtype=dtype, device="cuda")
+    at[0, 0], at[1, 0] = float("inf"), float("nan")
+    first = torch.ones((8, 8), dtype=dtype, device="cuda")
+    got = moe.linear(at, first, act=ACT[act])
+    assert (got[0] == float("inf")).all() and got[1].isnan().all()

@@ -5,6 +5,7 @@ import subprocess
 
 import pytest
 
+import test_dropless_large_gpu as layers
 import test_rows_gpu as small
 import test_rows_large_gpu as large
 
@@ -86,6 +87,13 @@ def test_large_tile_in_every_form():
     of = lambda cases: [c for c in cases if c.kernel == "256x256"]   # noqa: E731
     assert {c.act for c in of(large.FORWARD) if c.tokens} == {c.act for c in of(large.FORWARD) if not c.tokens} == {c.act for c in of(large.DENSE)} == {c.act for c in of(large.BACK)} == acts
     assert {bool(c.tokens) for c in of(large.WEIGHTS)} == {True, False}
+
+
+def test_a_layer_on_the_large_tile(rules):
+    for T, E, k, M, H in layers.LAYERS:
+        R = T * k
+        assert {rules("product", 1, 1, E, R, M, H, T, 1, 1), rules("product", 1, 1, E, R, H, M, 0, 0, 0), rules("product_nt", 1, E, R, H, M, 1), rules("product_nt", 1, E, R, M, H, 0),
+                rules("weight_grad", 1, E, R, M, H, T), rules("weight_grad", 1, E, R, H, M, 0)} == {"256x256"}
 
 
 def test_rows_of_a_large_token_matrix(rules):
